@@ -12,9 +12,13 @@
  * Eq. softmax_gradient and Eq. attention_backward).  A ring worker's share
  * (Section 4.2, Algorithm 2) is one call per ring step with a msparse_ring
  * descriptor, and partial results are combined by msparse_merge_out_lse
- * (merge_out_and_lse of Algorithm 2).
+ * (merge_out_and_lse of Algorithm 2).  Beside it stand attention with a static
+ * window-and-sinks pattern (forward and backward, any length, packed documents)
+ * and a paged 8-bit cache for decoding after the prefill (append with rotation,
+ * attention over the pages).
  *
- * Conventions shared by every entry point
+ * Conventions shared by every entry point (the static pattern and the cache say
+ * where theirs differ: strides, lengths, gradient types)
  *   - Tensors are device pointers to contiguous row-major arrays, 16-byte
  *     aligned: Q, O, dO bf16 [B, Hq, Nq, d]; K, V bf16 [B, Hkv, Nk, d];
  *     lse fp32 [B, Hq, Nq] (natural log); dQ fp32 [B, Hq, Nq, d];
@@ -371,6 +375,132 @@ MSPARSE_API msparse_status msparse_attn_bwd(const msparse_dims* dims, const void
                                 const void* out, const float* out_f32, const void* dout, const float* lse,
                                 const msparse_index* index, float* dq, float* dk, float* dv,
                                 int32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Attention with a static pattern: a sliding window and a few first tokens that
+ * stay visible (sinks), the pattern that a sparse layer gives the heads whose
+ * estimated one is no better.  Row i of a sequence sees the keys j <= i with
+ *   i - j < window   or   j < sinks;
+ * window = 0 (or at least the length) is plain causal attention.  Every row sees
+ * itself.  Lengths are free (no multiple of 64), from one token on.
+ *
+ * Tensors are bf16 [batch, heads, tokens, head_dim] with strides of their own
+ * (msparse_tensor), gradients included; lse is fp32, contiguous.  Sequences are
+ * either a batch of equal lengths, or documents packed one behind the other:
+ *   tokens = 0   batch sequences of seq tokens; lse [batch, heads_q, seq]
+ *   tokens > 0   every tensor has `tokens` rows per head and no batch axis (its
+ *                batch stride is not used); sequence b is the rows starts[b] to
+ *                starts[b + 1] - 1, starts int32 [batch + 1] on the device,
+ *                ascending, none longer than seq; lse [heads_q, tokens].  A
+ *                sequence may be empty.  Rows of no sequence are left as they
+ *                were, in every output.  (Starts outside [0, tokens] are cut to
+ *                it, and a longer sequence to its first seq rows.)
+ * All values of a sequence have to be finite: a row that is not may spread to
+ * rows of the same sequence that do not see it, but never to another sequence. */
+typedef struct {
+    void* data;                  /* 16-byte aligned */
+    int64_t batch, head, token;  /* strides in elements, multiples of 8; the head_dim elements of a row are
+                                    contiguous.  Inputs may repeat rows (stride 0), outputs may not, nor
+                                    share memory with another argument unless said. */
+} msparse_tensor;
+
+typedef struct {
+    int32_t batch;    /* sequences */
+    int32_t seq;      /* tokens of each; packed: of the longest, at most */
+    int32_t heads_q;
+    int32_t heads_kv; /* query head h reads KV head h / (heads_q / heads_kv) */
+    int32_t head_dim; /* 64 or 128 */
+    int32_t window;   /* 0: no limit */
+    int32_t sinks;
+    float scale;      /* <= 0: 1 / sqrt(head_dim) */
+    int64_t tokens;   /* 0, or the rows of packed tensors */
+} msparse_window;
+
+/* Forward: out_n = sum_m P[n, m] v_m and lse_n as in msparse_attn_fwd.  The
+ * weights P are rounded to bf16 before their product with v (fp32 sums).
+ * starts: packed only, else NULL.  No workspace. */
+MSPARSE_API msparse_status msparse_window_fwd(const msparse_window* win, const int32_t* starts,
+                                              const msparse_tensor* q, const msparse_tensor* k,
+                                              const msparse_tensor* v, const msparse_tensor* out, float* lse,
+                                              void* stream);
+
+/* Backward, from the forward's out and lse (formulas as msparse_attn_bwd, the
+ * pattern is a constant): dq, dk, dv bf16, overwritten, dk and dv summed over the
+ * query heads of each KV head in fp32.  P and dZ are rounded to bf16 before their
+ * products (fp32 sums).  No atomics: equal inputs give equal bits. */
+MSPARSE_API size_t msparse_window_bwd_workspace(const msparse_window* win);
+MSPARSE_API msparse_status msparse_window_bwd(const msparse_window* win, const int32_t* starts,
+                                              const msparse_tensor* q, const msparse_tensor* k,
+                                              const msparse_tensor* v, const msparse_tensor* out,
+                                              const msparse_tensor* dout, const float* lse, const msparse_tensor* dq,
+                                              const msparse_tensor* dk, const msparse_tensor* dv, void* workspace,
+                                              size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Paged 8-bit cache of keys and values, for decoding after a prefill.  A page
+ * holds 64 tokens of every KV head as e4m3 codes (OCP float8, 4 exponent and 3
+ * mantissa bits), with an fp32 scale per page and head for keys and one for
+ * values: value = code * scale.  All memory is the caller's:
+ *   k        e4m3 [pages, heads_kv, 64, head_dim]
+ *   v        e4m3 [pages, heads_kv, head_dim, 64]   (tokens contiguous)
+ *   k_scale, v_scale  fp32 [pages, heads_kv]
+ *   page_table int32 [batch, width]: page of the tokens 64 i .. 64 i + 63 of
+ *            sequence b at [b, i].  Sequences may share pages that neither
+ *            appends to.  Entries that no token needs are not read.
+ *   lens     int32 [batch]: tokens in the cache (0: none)
+ * An entry outside [0, pages), and a token at or beyond 64 width, has no page: it
+ * is not written by an append and not seen by the attention. */
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    const int32_t* page_table;
+    const int32_t* lens;
+    int32_t pages;
+    int32_t width;    /* 1 to 2^24 */
+    int32_t batch;
+    int32_t heads_kv;
+    int32_t head_dim; /* 64 or 128 */
+} msparse_cache;
+
+/* Appends counts[b] <= tokens tokens to each sequence (counts int32 [batch] on
+ * the device; NULL: `tokens` each): token t gets position lens[b] + t.  lens is
+ * read, not written: add the counts afterwards.
+ *   k, v     bf16 [batch, heads_kv, tokens, head_dim]
+ *   q, q_out bf16 [batch, heads_q, tokens, head_dim] or both NULL: the same
+ *            tokens' queries, rotated; q_out may be q (same strides).  Rows past
+ *            counts[b] are left as they were.
+ *   inv_freq fp32 [head_dim / 2] on the device, or NULL for no rotation: columns
+ *            (i, i + head_dim / 2) of a query or key at position p turn by the
+ *            angle p inv_freq[i] (reduced in 64 bits)
+ * A page's scale is the smallest power of two s >= 2^-126 with |x| <= 448 s for
+ * its tokens of the head so far, and codes are x / s to the nearest, ties to
+ * even.  Tokens that an earlier call wrote move to a larger scale when a later
+ * one needs it (exact, but for values below 2^-6 of the new scale, which round
+ * again).  A key or value that is not finite becomes NaN and does not count for
+ * the scale.  Slots of other tokens keep their codes.  Two calls that append to
+ * one page must not overlap. */
+MSPARSE_API msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q, int32_t tokens,
+                                                const msparse_tensor* q, const msparse_tensor* k,
+                                                const msparse_tensor* v, const msparse_tensor* q_out,
+                                                const float* inv_freq, const int32_t* counts, void* stream);
+
+/* Attention of the newest `tokens` tokens of every sequence over its cached keys
+ * and values (their own included: append first, then add the counts to lens):
+ * row t of sequence b has position lens[b] - tokens + t and sees what a row of
+ * msparse_window_fwd at that position sees.  A row before the sequence's start
+ * (lens[b] < tokens) or without a key gets out = 0 and lse = -inf.
+ *   q, out   bf16 [batch, heads_q, tokens, head_dim]
+ *   lse      fp32 [batch, heads_q, tokens] (natural log) or NULL
+ * Codes of free slots, and of tokens that no row of the call sees, may hold
+ * anything.  A NaN among a call's own tokens may reach its other rows.
+ * The workspace depends on the sizes alone, never on lens. */
+MSPARSE_API size_t msparse_cache_attn_workspace(const msparse_cache* cache, int32_t heads_q, int32_t tokens);
+MSPARSE_API msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens,
+                                              int32_t window, int32_t sinks, float scale, const msparse_tensor* q,
+                                              const msparse_tensor* out, float* lse, void* workspace,
+                                              size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Kernel-level tracing for measurement.  While enabled, every kernel the

@@ -8,6 +8,7 @@ implementation: if libmsparse.so is missing the first call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -45,6 +46,20 @@ class IndexStruct(ctypes.Structure):
                 ("world", c_i32)]
 
 
+class Tensor(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("batch", c_i64), ("head", c_i64), ("token", c_i64)]
+
+
+class Window(ctypes.Structure):
+    _fields_ = [("batch", c_i32), ("seq", c_i32), ("heads_q", c_i32), ("heads_kv", c_i32), ("head_dim", c_i32),
+                ("window", c_i32), ("sinks", c_i32), ("scale", c_f32), ("tokens", c_i64)]
+
+
+class CacheStruct(ctypes.Structure):
+    _fields_ = [("k", c_vp), ("v", c_vp), ("k_scale", c_vp), ("v_scale", c_vp), ("page_table", c_vp), ("lens", c_vp),
+                ("pages", c_i32), ("width", c_i32), ("batch", c_i32), ("heads_kv", c_i32), ("head_dim", c_i32)]
+
+
 class TraceEntry(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", c_i32), ("total_ms", ctypes.c_double)]
 
@@ -76,6 +91,14 @@ _SIGS = {
                                        c_sz, c_vp]),
     "msparse_merge_out_lse": (c_i32, [_P(Dims), c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_vp]),
     "msparse_attn_bwd_workspace": (c_sz, [_P(Dims), c_i64]),
+    "msparse_window_fwd": (c_i32, [_P(Window), c_vp] + [_P(Tensor)] * 4 + [c_vp, c_vp]),
+    "msparse_window_bwd_workspace": (c_sz, [_P(Window)]),
+    "msparse_window_bwd": (c_i32, [_P(Window), c_vp] + [_P(Tensor)] * 5 + [c_vp] + [_P(Tensor)] * 3 +
+                           [c_vp, c_sz, c_vp]),
+    "msparse_cache_append": (c_i32, [_P(CacheStruct), c_i32, c_i32] + [_P(Tensor)] * 4 + [c_vp, c_vp, c_vp]),
+    "msparse_cache_attn_workspace": (c_sz, [_P(CacheStruct), c_i32, c_i32]),
+    "msparse_cache_attn": (c_i32, [_P(CacheStruct), c_i32, c_i32, c_i32, c_i32, c_f32, _P(Tensor), _P(Tensor), c_vp,
+                                   c_vp, c_sz, c_vp]),
     "msparse_attn_bwd": (c_i32, [_P(Dims), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, _P(IndexStruct), c_vp, c_vp,
                                  c_vp, c_i32, c_vp, c_sz, c_vp]),
 }
@@ -338,6 +361,202 @@ def attn_bwd(dims, q, k, v, out, dout, lse, index: SparseIndex, dq=None, dk=None
                                   int(bool(dq_accumulate)) | (2 if reuse_qrows else 0),
                                   _p(workspace), workspace.numel(), _stream(stream)))
     return dq, dk, dv
+
+
+# ------------------------------------------------------------------ static pattern, cache: arguments
+def _refuse(msg):
+    raise MsparseError(-1, f"invalid argument: {msg}")
+
+
+def _arg(t, name, shape, dtype, device):
+    """A contiguous tensor argument of this shape, type and device."""
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
+                f"expected contiguous {dtype} {shape} on {device}")
+    return c_vp(t.data_ptr())
+
+
+def _rows(t, name, shape, device):
+    """A bf16 tensor [batch, heads, tokens, head_dim] of any strides with contiguous rows, as an msparse_tensor."""
+    if t.dtype != torch.bfloat16 or t.device != device or tuple(t.shape) != shape:
+        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}; expected {torch.bfloat16} {shape} on {device}")
+    st = t.stride()
+    if st[3] != 1:
+        _refuse(f"{name} has rows of stride {st[3]}")
+    return Tensor(t.data_ptr(), *(0 if n == 1 else x for n, x in zip(shape[:3], st)))
+
+
+def _on(device, stream):
+    """The context and stream pointer of a launch on `device`: what the call allocates belongs to that stream."""
+    if device.type != "cuda":
+        _refuse(f"tensors on {device}")
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+        if device.index == torch.cuda.current_device():
+            return contextlib.nullcontext(), c_vp(stream.cuda_stream)
+    elif stream.device != device:
+        _refuse(f"stream on {stream.device}, tensors on {device}")
+    return torch.cuda.stream(stream), c_vp(stream.cuda_stream)
+
+
+def _room(workspace, nbytes, device):
+    """A workspace of at least nbytes: the caller's, or a new one."""
+    if workspace is None:
+        workspace = _workspace(nbytes, device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        _refuse(f"workspace on {workspace.device}")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+# ------------------------------------------------------------------ window attention
+def make_window(batch, seq, heads_q, heads_kv, head_dim, window=0, sinks=0, scale=0.0, tokens=0) -> Window:
+    """msparse_window: rows see the last `window` keys (0: all) and the first `sinks`.  tokens > 0: `batch` sequences
+    of up to `seq` tokens packed into tensors of `tokens` rows."""
+    return Window(batch, seq, heads_q, heads_kv, head_dim, window, sinks, scale, tokens)
+
+
+def _window_shapes(win):
+    """Shapes of the query-side and the key-side tensors."""
+    B, N = (1, win.tokens) if win.tokens > 0 else (win.batch, win.seq)
+    return (B, win.heads_q, N, win.head_dim), (B, win.heads_kv, N, win.head_dim)
+
+
+def _starts(win, starts, device):
+    return None if starts is None else _arg(starts, "starts", (win.batch + 1,), torch.int32, device)
+
+
+def window_fwd(win: Window, q, k, v, starts=None, out=None, lse=None, stream=None):
+    """msparse_window_fwd: returns (out bf16 like q, lse fp32 [B, Hq, N]).  Packed sequences (win.tokens > 0): tensors
+    [1, heads, tokens, d], lse [1, Hq, tokens], starts int32 [batch + 1]; rows of no sequence keep their contents."""
+    dev = q.device
+    qs, ks = _window_shapes(win)
+    ctx, s = _on(dev, stream)
+    with ctx:
+        if out is None:
+            out = torch.empty(qs, dtype=torch.bfloat16, device=dev)
+        if lse is None:
+            lse = torch.empty(qs[:3], dtype=torch.float32, device=dev)
+        _check(lib().msparse_window_fwd(win, _starts(win, starts, dev), _rows(q, "q", qs, dev), _rows(k, "k", ks, dev),
+                                        _rows(v, "v", ks, dev), _rows(out, "out", qs, dev),
+                                        _arg(lse, "lse", qs[:3], torch.float32, dev), s))
+    return out, lse
+
+
+def window_bwd_workspace_bytes(win: Window) -> int:
+    return int(lib().msparse_window_bwd_workspace(win))
+
+
+def window_bwd(win: Window, q, k, v, out, dout, lse, starts=None, dq=None, dk=None, dv=None, workspace=None,
+               stream=None):
+    """msparse_window_bwd: returns (dq, dk, dv) bf16, from window_fwd's out and lse."""
+    dev = q.device
+    qs, ks = _window_shapes(win)
+    bf = torch.bfloat16
+    ctx, s = _on(dev, stream)
+    with ctx:
+        dq = torch.empty(qs, dtype=bf, device=dev) if dq is None else dq
+        dk = torch.empty(ks, dtype=bf, device=dev) if dk is None else dk
+        dv = torch.empty(ks, dtype=bf, device=dev) if dv is None else dv
+        workspace, room = _room(workspace, window_bwd_workspace_bytes(win), dev)
+        _check(lib().msparse_window_bwd(win, _starts(win, starts, dev), _rows(q, "q", qs, dev), _rows(k, "k", ks, dev),
+                                        _rows(v, "v", ks, dev), _rows(out, "out", qs, dev),
+                                        _rows(dout, "dout", qs, dev), _arg(lse, "lse", qs[:3], torch.float32, dev),
+                                        _rows(dq, "dq", qs, dev), _rows(dk, "dk", ks, dev), _rows(dv, "dv", ks, dev),
+                                        _p(workspace), room, s))
+    return dq, dk, dv
+
+
+# ------------------------------------------------------------------ paged cache
+@dataclass
+class Cache:
+    """A pool of pages of 64 tokens: k [pages, Hkv, 64, d] and v [pages, Hkv, d, 64] float8_e4m3fn codes,
+    k_scale and v_scale fp32 [pages, Hkv]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def make_cache(pages, heads_kv, head_dim, device) -> Cache:
+    f8 = torch.float8_e4m3fn
+    return Cache(torch.empty((pages, heads_kv, 64, head_dim), dtype=f8, device=device),
+                 torch.empty((pages, heads_kv, head_dim, 64), dtype=f8, device=device),
+                 torch.empty((pages, heads_kv), dtype=torch.float32, device=device),
+                 torch.empty((pages, heads_kv), dtype=torch.float32, device=device))
+
+
+def _cache(cache, page_table, lens, device):
+    if cache.k.dim() != 4 or page_table.dim() != 2:
+        _refuse(f"cache.k is {tuple(cache.k.shape)}, page_table {tuple(page_table.shape)}")
+    pages, heads, page, d = cache.k.shape
+    B, width = page_table.shape
+    if page != 64:
+        _refuse(f"pages of {page} tokens (64)")
+    f8, f32, i32 = torch.float8_e4m3fn, torch.float32, torch.int32
+    return CacheStruct(_arg(cache.k, "cache.k", (pages, heads, 64, d), f8, device),
+                       _arg(cache.v, "cache.v", (pages, heads, d, 64), f8, device),
+                       _arg(cache.k_scale, "cache.k_scale", (pages, heads), f32, device),
+                       _arg(cache.v_scale, "cache.v_scale", (pages, heads), f32, device),
+                       _arg(page_table, "page_table", (B, width), i32, device), _arg(lens, "lens", (B,), i32, device),
+                       pages, width, B, heads, d)
+
+
+def cache_append(cache: Cache, page_table, lens, k, v, q=None, inv_freq=None, counts=None, q_out=None, stream=None):
+    """msparse_cache_append: k, v bf16 [B, Hkv, T, d] after the lens [B] tokens that the sequences hold (counts [B] of
+    the T tokens; None: all); returns the rotated q (bf16 [B, Hq, T, d]), None without one.  lens is not changed."""
+    dev = k.device
+    ctx, s = _on(dev, stream)
+    c = _cache(cache, page_table, lens, dev)
+    if k.dim() != 4:
+        _refuse(f"k is {tuple(k.shape)}")
+    T = k.shape[2]
+    ks = (c.batch, c.heads_kv, T, c.head_dim)
+    with ctx:
+        tq = tqo = None
+        heads_q = c.heads_kv
+        if q is not None:
+            heads_q = q.shape[1]
+            qs = (c.batch, heads_q, T, c.head_dim)
+            if q_out is None:
+                q_out = torch.empty(qs, dtype=torch.bfloat16, device=dev)
+            tq, tqo = _rows(q, "q", qs, dev), _rows(q_out, "q_out", qs, dev)
+        elif q_out is not None:
+            _refuse("q_out without q")
+        freq = None if inv_freq is None else _arg(inv_freq, "inv_freq", (c.head_dim // 2,), torch.float32, dev)
+        cnt = None if counts is None else _arg(counts, "counts", (c.batch,), torch.int32, dev)
+        _check(lib().msparse_cache_append(c, heads_q, T, tq, _rows(k, "k", ks, dev), _rows(v, "v", ks, dev), tqo, freq,
+                                          cnt, s))
+    return q_out
+
+
+def cache_attn_workspace_bytes(cache: Cache, page_table, heads_q, tokens=1) -> int:
+    pages, heads, _, d = cache.k.shape
+    B, width = page_table.shape
+    return int(lib().msparse_cache_attn_workspace(CacheStruct(None, None, None, None, None, None, pages, width, B, heads,
+                                                              d), heads_q, tokens))
+
+
+def cache_attn(cache: Cache, page_table, lens, q, window=0, sinks=0, scale=0.0, out=None, lse=None, workspace=None,
+               stream=None):
+    """msparse_cache_attn: the newest T tokens' queries (bf16 [B, Hq, T, d], rotated) over the first lens [B] tokens of
+    their sequences, themselves included; returns (out bf16, lse fp32 [B, Hq, T])."""
+    dev = q.device
+    ctx, s = _on(dev, stream)
+    c = _cache(cache, page_table, lens, dev)
+    if q.dim() != 4:
+        _refuse(f"q is {tuple(q.shape)}")
+    heads_q, T = q.shape[1], q.shape[2]
+    qs = (c.batch, heads_q, T, c.head_dim)
+    with ctx:
+        if out is None:
+            out = torch.empty(qs, dtype=torch.bfloat16, device=dev)
+        if lse is None:
+            lse = torch.empty(qs[:3], dtype=torch.float32, device=dev)
+        workspace, room = _room(workspace, lib().msparse_cache_attn_workspace(c, heads_q, T), dev)
+        _check(lib().msparse_cache_attn(c, heads_q, T, window, sinks, scale, _rows(q, "q", qs, dev),
+                                        _rows(out, "out", qs, dev), _arg(lse, "lse", qs[:3], torch.float32, dev),
+                                        _p(workspace), room, s))
+    return out, lse
 
 
 def default_scale(head_dim: int) -> float:

@@ -16,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libmsparse.so")
-SOURCES = ["api.hip", "index.hip", "attn_fwd.hip", "attn_bwd.hip", "estimate.hip", "trace.hip", "peak.hip"]
+SOURCES = ["api.hip", "index.hip", "attn_fwd.hip", "attn_bwd.hip", "estimate.hip", "window_fwd.hip", "window_bwd.hip",
+           "cache_append.hip", "cache_attn.hip", "trace.hip", "peak.hip"]
 ARCH = "gfx950"
 
 

@@ -1,6 +1,7 @@
 // C ABI of libmsparse: argument validation, workspace carve-up and launches.
 // Every check runs on the host before the first launch, so an error return
 // leaves the stream untouched.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -10,9 +11,11 @@
 #include <mutex>
 #include <string>
 
+#include "cache.h"
 #include "common.h"
 #include "kernels.h"
 #include "operands.h"
+#include "window.h"
 
 using namespace msparse;
 
@@ -35,6 +38,13 @@ msparse_status fail(msparse_status st, const char* fmt, ...) {
 bool misaligned(std::initializer_list<const void*> ps) {
     for (const void* p : ps)
         if (reinterpret_cast<uintptr_t>(p) & 15u) return true;
+    return false;
+}
+
+// arrays of 32-bit words that are read one by one
+bool odd_words(std::initializer_list<const void*> ps) {
+    for (const void* p : ps)
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return true;
     return false;
 }
 
@@ -757,6 +767,285 @@ msparse_status msparse_estimate_topp(const msparse_dims* dims, const void* q, co
     if (!v_cnt || !s_cnt) return fail(MSPARSE_ERR_INVALID, "budget output pointer is NULL");
     return estimate_impl(dims, q, k, last_q, kmax_v, kmax_s, p_v, p_s, v_idx, s_idx, v_cnt, s_cnt, v_score, s_score,
                          ws, ws_bytes, stream);
+}
+
+// ------------------------------------------------------------------ window attention
+// A tensor argument: strides multiples of 8 elements (rows 16-byte aligned), and
+// for an output no two rows in the same place.
+static msparse_status check_tensor(const msparse_tensor* t, const char* name, int64_t batch, int64_t heads, int64_t rows,
+                                   int32_t head_dim, bool output) {
+    if (!t || !t->data) return fail(MSPARSE_ERR_INVALID, "%s is NULL", name);
+    if (misaligned({t->data})) return fail(MSPARSE_ERR_INVALID, "%s is not 16-byte aligned", name);
+    const int64_t size[3] = {batch, heads, rows}, stride[3] = {t->batch, t->head, t->token};
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int x, int y) { return stride[x] < stride[y]; });
+    int64_t span = head_dim;   // elements that the axes so far take
+    for (int x : order) {
+        if (size[x] <= 1) continue;
+        if (stride[x] < 0 || stride[x] % 8)
+            return fail(MSPARSE_ERR_INVALID, "%s has stride %lld (multiples of 8, >= 0)", name, (long long)stride[x]);
+        if (stride[x] > (int64_t(1) << 60) / size[x])
+            return fail(MSPARSE_ERR_INVALID, "%s has stride %lld", name, (long long)stride[x]);
+        if (output && stride[x] < span) return fail(MSPARSE_ERR_INVALID, "%s overlaps itself", name);
+        span += (size[x] - 1) * stride[x];
+    }
+    return MSPARSE_OK;
+}
+
+static RowView row_view(const msparse_tensor* t) {
+    return RowView{static_cast<uint16_t*>(t->data), t->batch, t->head, t->token};
+}
+
+// Most workgroups of a launch: 512 threads each stay below 2^32
+constexpr int64_t kMaxGroups = int64_t(1) << 22;
+
+static msparse_status check_window(const msparse_window* w, const int32_t* starts) {
+    if (!w) return fail(MSPARSE_ERR_INVALID, "window is NULL");
+    if (w->batch < 1 || w->heads_q < 1 || w->heads_kv < 1 || w->seq < 0 || w->tokens < 0)
+        return fail(MSPARSE_ERR_INVALID, "batch, heads must be >= 1 and lengths >= 0");
+    if (w->heads_q % w->heads_kv != 0)
+        return fail(MSPARSE_ERR_INVALID, "heads_q (%d) is not a multiple of heads_kv (%d)", w->heads_q, w->heads_kv);
+    if (w->head_dim != 64 && w->head_dim != 128)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", w->head_dim);
+    if (w->window < 0 || w->sinks < 0) return fail(MSPARSE_ERR_INVALID, "window %d, sinks %d", w->window, w->sinks);
+    if (!std::isfinite(w->scale)) return fail(MSPARSE_ERR_INVALID, "scale is not finite");
+    if (w->tokens > 0 && !starts) return fail(MSPARSE_ERR_INVALID, "packed sequences without starts");
+    if (w->tokens == 0 && starts) return fail(MSPARSE_ERR_INVALID, "starts without packed tokens");
+    if (odd_words({starts})) return fail(MSPARSE_ERR_INVALID, "starts not 4-byte aligned");
+    const int64_t rows = w->tokens > 0 ? w->tokens : int64_t(w->batch) * w->seq;
+    if (rows > ((int64_t(1) << 31) - 1) / w->heads_q || w->seq > (1 << 30))
+        return fail(MSPARSE_ERR_UNSUPPORTED, "heads * tokens exceeds 2^31 rows");
+    if (int64_t(w->batch) * w->heads_q > kMaxGroups / std::max<int64_t>(1, (int64_t(w->seq) + 63) / 64))
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%d sequences of up to %d tokens exceed 2^22 blocks of 64 rows", w->batch,
+                    w->seq);
+    return MSPARSE_OK;
+}
+
+static WindowArgs window_args(const msparse_window* w, const int32_t* starts) {
+    WindowArgs a{};
+    a.starts = starts;
+    a.tokens = w->tokens;
+    a.B = w->batch;
+    a.Hq = w->heads_q;
+    a.Hkv = w->heads_kv;
+    a.seq = w->seq;
+    a.d = w->head_dim;
+    // a window or sinks over the whole sequence leave the causal mask alone
+    const bool all = w->window == 0 || w->window >= w->seq || w->sinks >= w->seq;
+    a.W = all ? INT32_MAX : w->window;
+    a.S = all ? 0 : w->sinks;
+    a.scale = w->scale > 0.f ? w->scale : 1.0f / std::sqrt(float(w->head_dim));
+    return a;
+}
+
+// lse log2(e) and Delta of every row, the sink keys' partial gradients.
+static size_t carve_window_bwd(WindowArgs* a, char* base) {
+    const SinkPlan p = sink_plan(a->B, a->Hkv, a->Hq / a->Hkv, a->seq, a->W, a->S);
+    a->sink_pairs = p.pairs;
+    a->slots = p.slots;
+    a->chunk = p.chunk;
+    a->rows_pad = a->tokens > 0 ? padded_rows(a->tokens) + 64 * (int64_t(a->B) + 1) : a->B * padded_rows(a->seq);
+    Carve c{base};
+    a->rows = c.take<float>(size_t(2) * a->Hq * a->rows_pad);
+    a->part = c.take<float>(size_t(a->B) * a->Hkv * p.pairs * p.slots * 2 * 128 * a->d);
+    return c.off;
+}
+
+msparse_status msparse_window_fwd(const msparse_window* win, const int32_t* starts, const msparse_tensor* q,
+                                  const msparse_tensor* k, const msparse_tensor* v, const msparse_tensor* out,
+                                  float* lse, void* stream) {
+    msparse_status st = check_window(win, starts);
+    if (st || win->seq == 0) return st;
+    const int64_t B = win->tokens > 0 ? 1 : win->batch, N = win->tokens > 0 ? win->tokens : win->seq;
+    const int32_t d = win->head_dim;
+    if ((st = check_tensor(q, "q", B, win->heads_q, N, d, false))) return st;
+    if ((st = check_tensor(k, "k", B, win->heads_kv, N, d, false))) return st;
+    if ((st = check_tensor(v, "v", B, win->heads_kv, N, d, false))) return st;
+    if ((st = check_tensor(out, "out", B, win->heads_q, N, d, true))) return st;
+    if (!lse) return fail(MSPARSE_ERR_INVALID, "lse is NULL");
+    if (misaligned({lse})) return fail(MSPARSE_ERR_INVALID, "lse is not 16-byte aligned");
+    WindowArgs a = window_args(win, starts);
+    a.q = row_view(q);
+    a.k = row_view(k);
+    a.v = row_view(v);
+    a.out = row_view(out);
+    a.lse = lse;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return check_hip(launch_window_fwd(a, s), s, "window fwd");
+}
+
+size_t msparse_window_bwd_workspace(const msparse_window* win) {
+    static const int32_t present = 0;   // only whether starts are given counts
+    if (check_window(win, win && win->tokens > 0 ? &present : nullptr)) return 0;
+    WindowArgs a = window_args(win, nullptr);
+    return carve_window_bwd(&a, nullptr);
+}
+
+msparse_status msparse_window_bwd(const msparse_window* win, const int32_t* starts, const msparse_tensor* q,
+                                  const msparse_tensor* k, const msparse_tensor* v, const msparse_tensor* out,
+                                  const msparse_tensor* dout, const float* lse, const msparse_tensor* dq,
+                                  const msparse_tensor* dk, const msparse_tensor* dv, void* ws, size_t ws_bytes,
+                                  void* stream) {
+    msparse_status st = check_window(win, starts);
+    if (st || win->seq == 0) return st;
+    const int64_t B = win->tokens > 0 ? 1 : win->batch, N = win->tokens > 0 ? win->tokens : win->seq;
+    const int32_t d = win->head_dim;
+    if ((st = check_tensor(q, "q", B, win->heads_q, N, d, false))) return st;
+    if ((st = check_tensor(k, "k", B, win->heads_kv, N, d, false))) return st;
+    if ((st = check_tensor(v, "v", B, win->heads_kv, N, d, false))) return st;
+    if ((st = check_tensor(out, "out", B, win->heads_q, N, d, false))) return st;
+    if ((st = check_tensor(dout, "dout", B, win->heads_q, N, d, false))) return st;
+    if ((st = check_tensor(dq, "dq", B, win->heads_q, N, d, true))) return st;
+    if ((st = check_tensor(dk, "dk", B, win->heads_kv, N, d, true))) return st;
+    if ((st = check_tensor(dv, "dv", B, win->heads_kv, N, d, true))) return st;
+    if (!lse) return fail(MSPARSE_ERR_INVALID, "lse is NULL");
+    if (misaligned({lse, ws})) return fail(MSPARSE_ERR_INVALID, "lse or workspace is not 16-byte aligned");
+    WindowArgs a = window_args(win, starts);
+    const size_t need = carve_window_bwd(&a, static_cast<char*>(ws));
+    if (need && (!ws || ws_bytes < need))
+        return fail(MSPARSE_ERR_WORKSPACE, "window bwd workspace %zu < %zu bytes", ws_bytes, need);
+    a.q = row_view(q);
+    a.k = row_view(k);
+    a.v = row_view(v);
+    a.out = row_view(out);
+    a.dout = row_view(dout);
+    a.lse = const_cast<float*>(lse);
+    a.dq = row_view(dq);
+    a.dk = row_view(dk);
+    a.dv = row_view(dv);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return check_hip(launch_window_bwd(a, s), s, "window bwd");
+}
+
+// ------------------------------------------------------------------ paged cache
+static msparse_status check_cache(const msparse_cache* c, int32_t heads_q, int32_t tokens) {
+    if (!c) return fail(MSPARSE_ERR_INVALID, "cache is NULL");
+    if (c->batch < 1 || c->heads_kv < 1 || heads_q < 1 || tokens < 0)
+        return fail(MSPARSE_ERR_INVALID, "batch, heads must be >= 1 and tokens >= 0");
+    if (heads_q % c->heads_kv != 0)
+        return fail(MSPARSE_ERR_INVALID, "heads_q (%d) is not a multiple of heads_kv (%d)", heads_q, c->heads_kv);
+    if (c->head_dim != 64 && c->head_dim != 128)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", c->head_dim);
+    if (c->pages < 1 || c->width < 1) return fail(MSPARSE_ERR_INVALID, "pages %d, width %d", c->pages, c->width);
+    if (c->width > kMaxWidth) return fail(MSPARSE_ERR_UNSUPPORTED, "width %d > 2^24", c->width);
+    if (tokens > (1 << 30) || int64_t(c->batch) * tokens > ((int64_t(1) << 31) - 1) / heads_q)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "batch * heads * tokens exceeds 2^31 rows");
+    return MSPARSE_OK;
+}
+static msparse_status check_cache_memory(const msparse_cache* c) {
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->page_table || !c->lens)
+        return fail(MSPARSE_ERR_INVALID, "cache array is NULL");
+    if (misaligned({c->k, c->v})) return fail(MSPARSE_ERR_INVALID, "cache codes not 16-byte aligned");
+    if (odd_words({c->k_scale, c->v_scale, c->page_table, c->lens}))
+        return fail(MSPARSE_ERR_INVALID, "cache array not 4-byte aligned");
+    return MSPARSE_OK;
+}
+static CacheView cache_view(const msparse_cache* c) {
+    return CacheView{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_scale, c->v_scale, c->page_table,
+                     c->lens, c->pages, c->width, c->batch, c->heads_kv, c->head_dim};
+}
+static void set_strides(int64_t* s, const msparse_tensor* t) {
+    s[0] = t->batch;
+    s[1] = t->head;
+    s[2] = t->token;
+}
+
+msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q, int32_t tokens, const msparse_tensor* q,
+                                    const msparse_tensor* k, const msparse_tensor* v, const msparse_tensor* q_out,
+                                    const float* inv_freq, const int32_t* counts, void* stream) {
+    msparse_status st = check_cache(cache, heads_q, tokens);
+    if (st) return st;
+    if ((st = check_cache_memory(cache)) || tokens == 0) return st;
+    const int64_t B = cache->batch;
+    const int32_t d = cache->head_dim;
+    if ((st = check_tensor(k, "k", B, cache->heads_kv, tokens, d, false))) return st;
+    if ((st = check_tensor(v, "v", B, cache->heads_kv, tokens, d, false))) return st;
+    if (odd_words({inv_freq, counts})) return fail(MSPARSE_ERR_INVALID, "inv_freq or counts not 4-byte aligned");
+    if (!q != !q_out) return fail(MSPARSE_ERR_INVALID, "q and q_out go together");
+    if (q) {
+        if ((st = check_tensor(q, "q", B, heads_q, tokens, d, false))) return st;
+        if ((st = check_tensor(q_out, "q_out", B, heads_q, tokens, d, true))) return st;
+        const bool same = (B <= 1 || q->batch == q_out->batch) && (heads_q <= 1 || q->head == q_out->head) &&
+                          (tokens <= 1 || q->token == q_out->token);
+        if (q->data == q_out->data && !same)
+            return fail(MSPARSE_ERR_INVALID, "q rotated in place with other strides");
+    }
+    AppendArgs a{};
+    a.c = cache_view(cache);
+    a.k = static_cast<const uint16_t*>(k->data);
+    a.v = static_cast<const uint16_t*>(v->data);
+    set_strides(a.ks, k);
+    set_strides(a.vs, v);
+    if (q) {
+        a.q = static_cast<const uint16_t*>(q->data);
+        a.qout = static_cast<uint16_t*>(q_out->data);
+        set_strides(a.qs, q);
+        set_strides(a.qos, q_out);
+    }
+    a.freq = inv_freq;
+    a.counts = counts;
+    a.Hq = heads_q;
+    a.T = tokens;
+    const int64_t P = (int64_t(tokens) + 2 * kPage - 2) / kPage;   // the most pages that tokens in a row touch
+    if (B * P > kMaxGroups) return fail(MSPARSE_ERR_UNSUPPORTED, "%lld pages in one call", (long long)(B * P));
+    a.P = int32_t(P);
+    a.split = append_split(B * P, q ? heads_q : cache->heads_kv);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return check_hip(launch_cache_append(a, s), s, "cache append");
+}
+
+static size_t carve_cache_attn(const msparse_cache* c, const CacheAttnPlan& p, char* base, CacheAttnArgs* a) {
+    if (p.items == 0) return 0;
+    Carve w{base};
+    a->info = w.take<int32_t>(size_t(2) * c->batch * p.tiles);
+    a->pml = w.take<float>(size_t(p.slots) * c->heads_kv * p.rows * 2);
+    a->po = w.take<float>(size_t(p.slots) * c->heads_kv * p.rows * c->head_dim);
+    return w.off;
+}
+
+size_t msparse_cache_attn_workspace(const msparse_cache* cache, int32_t heads_q, int32_t tokens) {
+    if (check_cache(cache, heads_q, tokens) || tokens == 0) return 0;
+    CacheAttnArgs a{};
+    return carve_cache_attn(cache, cache_attn_plan(cache->batch, heads_q, cache->heads_kv, tokens, cache->width), nullptr,
+                            &a);
+}
+
+msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens, int32_t window,
+                                  int32_t sinks, float scale, const msparse_tensor* q, const msparse_tensor* out,
+                                  float* lse, void* ws, size_t ws_bytes, void* stream) {
+    msparse_status st = check_cache(cache, heads_q, tokens);
+    if (st) return st;
+    if ((st = check_cache_memory(cache)) || tokens == 0) return st;
+    if (window < 0 || sinks < 0) return fail(MSPARSE_ERR_INVALID, "window %d, sinks %d", window, sinks);
+    if (!std::isfinite(scale)) return fail(MSPARSE_ERR_INVALID, "scale is not finite");
+    const int64_t B = cache->batch;
+    const int32_t d = cache->head_dim;
+    if ((st = check_tensor(q, "q", B, heads_q, tokens, d, false))) return st;
+    if ((st = check_tensor(out, "out", B, heads_q, tokens, d, true))) return st;
+    if (misaligned({lse, ws})) return fail(MSPARSE_ERR_INVALID, "lse or workspace is not 16-byte aligned");
+    const CacheAttnPlan p = cache_attn_plan(B, heads_q, cache->heads_kv, tokens, cache->width);
+    if (p.items == 0 && B * p.tiles > kMaxGroups / cache->heads_kv)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%lld row tiles", (long long)(B * p.tiles * cache->heads_kv));
+    CacheAttnArgs a{};
+    const size_t need = carve_cache_attn(cache, p, static_cast<char*>(ws), &a);
+    if (need && (!ws || ws_bytes < need))
+        return fail(MSPARSE_ERR_WORKSPACE, "cache attn workspace %zu < %zu bytes", ws_bytes, need);
+    a.c = cache_view(cache);
+    a.q = static_cast<const uint16_t*>(q->data);
+    a.out = static_cast<uint16_t*>(out->data);
+    set_strides(a.qs, q);
+    set_strides(a.os, out);
+    a.lse = lse;
+    a.Hq = heads_q;
+    a.T = tokens;
+    a.W = window == 0 ? INT32_MAX : window;
+    a.S = window == 0 ? 0 : sinks;
+    a.scale = scale > 0.f ? scale : 1.0f / std::sqrt(float(d));
+    a.tiles = p.tiles;
+    a.items = p.items;
+    a.slots = p.slots;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return check_hip(launch_cache_attn(a, p, s), s, "cache attn");
 }
 
 }  // extern "C"

@@ -1,0 +1,81 @@
+// Paged 8-bit cache of keys and values: what the append and the attention over
+// it share.
+//
+// A page holds 64 tokens of every KV head: K codes [64][d] (a token's row is
+// contiguous, as its key is read whole) and V codes [d][64] (a column's 64 tokens
+// are contiguous: the operand of P V^T runs over tokens, so the attention reads
+// either from memory straight into registers, 16 bytes a lane, without LDS).
+// Codes are e4m3 (OCP: bias 7, no infinities, 0x7f NaN), with one fp32 scale per
+// page and head for K and one for V: value = code * scale.
+#pragma once
+
+#include <algorithm>
+
+#include "common.h"
+
+namespace msparse {
+
+constexpr int kPage = 64;
+constexpr int kMaxWidth = 1 << 24;   // pages of a sequence: positions stay below 2^30
+
+struct CacheView {
+    uint8_t* k;           // [pages, Hkv, 64, d]
+    uint8_t* v;           // [pages, Hkv, d, 64]
+    float* ks;            // [pages, Hkv]
+    float* vs;
+    const int32_t* table; // [B, width]: page of each 64 tokens of a sequence
+    const int32_t* lens;  // [B]
+    int32_t pages, width;
+    int32_t B, Hkv, d;
+};
+// the page of tokens 64 p .. 64 p + 63 of sequence b, -1 if there is none
+__device__ __forceinline__ int32_t cache_page(const CacheView& c, int b, int p) {
+    if (p >= c.width) return -1;
+    const int32_t x = ldc(c.table, int64_t(b) * c.width + p);
+    return uint32_t(x) < uint32_t(c.pages) ? x : -1;
+}
+
+struct AppendArgs {
+    CacheView c;
+    const uint16_t *q, *k, *v;                // bf16 [B, heads, T, d]
+    int64_t qs[3], ks[3], vs[3], qos[3];      // strides: sequence, head, token
+    uint16_t* qout;
+    const float* freq;                        // [d / 2] or NULL: no rotation
+    const int32_t* counts;                    // [B] or NULL: T
+    int32_t Hq, T;
+    int32_t P;                                // pages that T tokens can touch
+    int32_t split;                            // workgroups that share a page's heads
+};
+// Workgroups that share a page's heads: as many as bring the grid to about four
+// a CU, each head in one of them.
+inline int32_t append_split(int64_t pages, int64_t heads) {
+    return int32_t(std::max<int64_t>(1, std::min<int64_t>(heads, 1024 / pages)));
+}
+hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
+
+struct CacheAttnArgs {
+    CacheView c;
+    const uint16_t* q;      // bf16 [B, Hq, T, d]
+    int64_t qs[3], os[3];
+    uint16_t* out;
+    float* lse;             // [B, Hq, T] or NULL
+    int32_t Hq, T, W, S;    // W = INT32_MAX: no window
+    float scale;
+    int32_t tiles;          // row tiles of a (sequence, KV head): its G T rows
+    int32_t items;          // chunks aimed at per KV head (0: one workgroup per row tile)
+    // workspace (items > 0)
+    int32_t* info;          // [B tiles][2]: first chunk, chunks
+    float* po;              // [slots, Hkv, rows, d]: sums of the weighted values
+    float* pml;             // [slots, Hkv, rows, 2]: running maximum (log2 units), sum of the weights
+    int32_t slots;
+};
+// Row tiles and chunks of a call.  rows = G T rows of a (sequence, KV head).
+struct CacheAttnPlan {
+    int32_t rt, wr;         // 16-row tiles per wave; waves of a workgroup over rows (1: over pages)
+    int32_t rows;           // rows of a workgroup
+    int32_t tiles, items, slots;
+};
+CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width);
+hipError_t launch_cache_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
+
+}  // namespace msparse

@@ -1,0 +1,161 @@
+// Attention with a sliding window and a few first tokens that stay visible
+// (sinks): what its forward and backward kernels share.
+//
+// Row i of a sequence of n tokens sees the keys j <= i with i - j < window or
+// j < sinks.  Every row sees itself, so no row is empty.  Rows and keys are
+// walked in tiles of 64 whose borders lie at multiples of 64 from the
+// sequence's start; a tile is either seen in full by a wave's rows, not at all,
+// or in part, and only then masked, from positions alone (no lists, no mask in
+// memory).  Tensors are read where they lie (bf16, any batch, head and token
+// stride): the tile loads take an address per lane anyway, and copies in another
+// type or order would cost two passes over memory.
+#pragma once
+
+#include <algorithm>
+
+#include "common.h"
+#include "tiles.h"
+
+namespace msparse {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// A bf16 tensor [batch, heads, tokens, d], rows contiguous; strides in elements.
+struct RowView {
+    uint16_t* p;
+    int64_t batch, head, token;
+};
+
+struct WindowArgs {
+    RowView q, k, v, out, dout, dq, dk, dv;
+    float* lse;            // [batch, Hq, seq], packed: [Hq, tokens]
+    const int32_t* starts; // packed: [batch + 1] first rows of the sequences (NULL: batch x seq)
+    int64_t tokens;        // packed: rows of every tensor
+    int32_t B, Hq, Hkv, seq, d;
+    int32_t W, S;          // W = INT32_MAX: no window
+    float scale;
+    // backward workspace
+    float* rows;           // [Hq][2][rows_pad]: lse log2(e) and Delta of every row, sequences from a multiple of 64 on
+    int64_t rows_pad;
+    float* part;           // sink keys' partial gradients: [B Hkv sink_pairs][slots][2][128][d]
+    int32_t sink_pairs;    // pairs of key blocks that hold sinks
+    int32_t slots;         // partials of such a pair: its window's, then `slots - 1` chunks of the rows beyond
+    int32_t chunk;         // query tiles of a chunk
+};
+
+// Where sequence b lies: `row` its first row (packed), n its length.  Starts out
+// of order or beyond the tensors are cut to [0, tokens], lengths to `seq`.
+struct Sequence {
+    int64_t row;
+    int32_t b, n;
+};
+__device__ __forceinline__ Sequence sequence(const WindowArgs& a, int b) {
+    Sequence s{0, b, a.seq};
+    if (a.starts) {
+        const int64_t r0 = min(max(int64_t(ldc(a.starts, b)), int64_t(0)), a.tokens);
+        const int64_t r1 = min(max(int64_t(ldc(a.starts, b + 1)), r0), a.tokens);
+        s.row = r0;
+        s.n = int32_t(min(r1 - r0, int64_t(a.seq)));
+    }
+    return s;
+}
+__device__ __forceinline__ uint16_t* head_rows(const WindowArgs& a, const RowView& v, const Sequence& s, int h) {
+    return v.p + (a.starts ? s.row * v.token : s.b * v.batch) + h * v.head;
+}
+__device__ __forceinline__ int64_t lse_row(const WindowArgs& a, const Sequence& s, int h) {
+    return a.starts ? h * a.tokens + s.row : (int64_t(s.b) * a.Hq + h) * a.seq;
+}
+// First row of a sequence in the backward's row values.  Packed sequences take
+// whole blocks of 64: the next multiple of 64 plus one block for each sequence
+// before, so that two never share one.
+__host__ __device__ inline int64_t padded_rows(int64_t n) { return (n + 63) / 64 * 64; }
+__device__ __forceinline__ int64_t value_row(const WindowArgs& a, const Sequence& s) {
+    return a.starts ? padded_rows(s.row) + 64 * int64_t(s.b) : s.b * padded_rows(a.seq);
+}
+
+// The key tiles that the rows i0 .. i1 see: those of the window from the
+// diagonal down (the running maximum is set early), then the sinks'.
+struct KeyWalk {
+    int32_t hi, window_tiles, tiles, sink_tiles;
+    __device__ __forceinline__ int32_t tile(int t) const {
+        return t < window_tiles ? hi - t : tiles - 1 - t;
+    }
+};
+__device__ __forceinline__ KeyWalk key_walk(int i0, int i1, int W, int S) {
+    KeyWalk k;
+    k.hi = i1 >> 6;
+    const int lo = max(i0 - W + 1, 0) >> 6;   // W <= INT32_MAX: no overflow for i0 >= 0
+    k.window_tiles = k.hi - lo + 1;
+    k.sink_tiles = min((S + 63) >> 6, lo);
+    k.tiles = k.window_tiles + k.sink_tiles;
+    return k;
+}
+
+// How rows i0 .. i1 see keys j0 .. j1.
+enum Sight { kNone, kPart, kFull };
+__device__ __forceinline__ Sight sight(int i0, int i1, int j0, int j1, int W, int S) {
+    if (j0 > i1 || (j1 <= i0 - W && j0 >= S)) return kNone;
+    if (j1 <= i0 && (j0 > i1 - W || j1 < S)) return kFull;
+    return kPart;
+}
+// i sees j; lim = min(S - 1, i)
+__device__ __forceinline__ bool sees(int i, int j, int W, int lim) {
+    return uint32_t(i - j) < uint32_t(W) || j <= lim;
+}
+
+// 64 rows from row0 on (rows past the end: the last one) into a DMA tile.
+template <int D, int P, int NW>
+__device__ __forceinline__ void dma_sequence(uint16_t* tile, const uint16_t* src, int64_t stride, int row0, int last,
+                                             int wave, int lane) {
+    using T = DmaTile<D, P>;
+    constexpr int NC = D / 8;
+    static_assert(T::kGroups % NW == 0, "whole instructions per wave");
+#pragma unroll
+    for (int j = 0; j < T::kGroups / NW; ++j) {
+        const int g = wave + NW * j;
+        const int r = min(row0 + g + T::kGroups * (lane / NC), last);
+        dma16(src + r * stride + (lane % NC) * 8, lds_addr(tile + T::goff(g) / 2));
+    }
+}
+
+// 8 consecutive accumulator values to bf16 x 8
+template <int BASE>
+__device__ __forceinline__ u32x4 pack8_bf16(const f32x16& acc) {
+    u32x4 r;
+    r.x = pack_bf16x2(acc[BASE + 0], acc[BASE + 1]);
+    r.y = pack_bf16x2(acc[BASE + 2], acc[BASE + 3]);
+    r.z = pack_bf16x2(acc[BASE + 4], acc[BASE + 5]);
+    r.w = pack_bf16x2(acc[BASE + 6], acc[BASE + 7]);
+    return r;
+}
+
+// (head, tile of rows) of workgroup t, as query_tile_of; tiles = tiles per head
+__device__ __forceinline__ void window_tile_of(const WindowArgs& a, int64_t t, int tiles, int& b, int& h, int& tile) {
+    int bh;
+    query_tile_of(t, a.B, a.Hq, a.Hkv, tiles, bh, tile);
+    b = bh / a.Hq;
+    h = bh % a.Hq;
+}
+
+hipError_t launch_window_fwd(const WindowArgs& a, hipStream_t s);
+hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s);
+
+// Sizes of the backward's partial gradients of the sink keys (0 sink_pairs: none).
+struct SinkPlan {
+    int32_t pairs, slots, chunk;
+};
+inline SinkPlan sink_plan(int64_t B, int64_t Hkv, int64_t G, int64_t seq, int64_t W, int64_t S) {
+    SinkPlan p{0, 0, 0};
+    const int64_t tiles = (seq + 63) / 64;
+    const int64_t first = W / 64;             // the rows of tiles before are inside the window of key 0
+    if (S <= 0 || W >= seq || first >= tiles) return p;
+    p.pairs = int32_t((std::min(S, seq) + 127) / 128);
+    const int64_t beyond = G * (tiles - first);      // query tiles beyond a pair's window, at most
+    const int64_t items = std::max<int64_t>(1, std::min<int64_t>(256, 1024 / (B * Hkv * p.pairs)));
+    p.chunk = int32_t(std::max<int64_t>(16, (beyond + items - 1) / items));
+    p.slots = int32_t(1 + (beyond + p.chunk - 1) / p.chunk);
+    return p;
+}
+
+}  // namespace msparse

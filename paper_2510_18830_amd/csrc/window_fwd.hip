@@ -1,0 +1,215 @@
+// Forward of the attention with a sliding window and sinks.
+//
+// One workgroup of four wavefronts per (sequence, query head, 128 rows), 32 rows
+// a wave.  Key tiles of 64 are staged by direct global->LDS loads, the next one
+// in flight while the current one is computed.  Per tile and wave:
+//   S^T = K Q^T    (A = K rows from LDS, B = the wave's Q rows in registers)
+//   online softmax (a lane owns a query row, lane l ^ 32 the other half of its keys)
+//   O^T += V^T P^T (A = V^T read transposed from LDS, B = P from the S^T registers)
+// Both products take bf16 operands: P is rounded to V's type (8 significant bits,
+// the rounding that the output itself gets), and the sum that normalises O is
+// that of the rounded weights, so a row with nearly all its weight on one key
+// keeps that key's value exactly; lse is made from the unrounded sum.
+#include "window.h"
+#include "trace.h"
+
+namespace msparse {
+
+namespace {
+
+constexpr float kSlack = 8.f;        // log2 units
+constexpr int kFwdRows = 128;        // query rows per workgroup
+constexpr int kFwdThreads = 256;
+
+template <int D>
+struct WinRows {
+    static constexpr int KD = D / 16;   // k-steps over head_dim
+    static constexpr int ND = D / 32;   // 32-wide output column blocks
+    u32x4 q[KD];
+    f32x16 o[ND];
+    float m = -INFINITY;        // running maximum (log2 units)
+    float l = 0.f, lr = 0.f;    // sums of the weights and of the rounded weights
+};
+
+// Sum of the bf16 weights in four packed operands, both halves of the row.
+__device__ __forceinline__ float row_sum_bf16(const u32x4* pb) {
+    const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+    float a = 0.f, b = 0.f;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const uint32_t w0 = pb[g].x, w1 = pb[g].y, w2 = pb[g].z, w3 = pb[g].w;
+        a = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w0), one, a, false);
+        b = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w1), one, b, false);
+        a = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w2), one, a, false);
+        b = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w3), one, b, false);
+    }
+    return half_swap_sum(a + b);
+}
+
+// One tile of the keys j0 .. j0 + 63; i = this lane's row.  c2 = scale log2(e).
+template <int D>
+__device__ __forceinline__ void win_tile(const uint16_t* kt, const uint16_t* vt, bool masked, int i, int j0, int W,
+                                         int S, WinRows<D>& st, int lane, float c2) {
+    constexpr int KD = WinRows<D>::KD, ND = WinRows<D>::ND;
+    const int h = lane >> 5, l32 = lane & 31;
+    // operands in groups of two k-steps, read one group ahead of their MFMAs
+    f32x16 sacc[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) sacc[c] = f32x16{};
+    u32x4 fk[2][2][2];   // [set][k-step of group][c]
+    auto read_group = [&](int set, int s0) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) fk[set][j][c] = dma_read16<D, kRowPad>(kt, 32 * c + l32, h + 2 * (s0 + j));
+    };
+    read_group(0, 0);
+#pragma unroll
+    for (int s0 = 0; s0 < KD; s0 += 2) {
+        const int set = (s0 >> 1) & 1;
+        if (s0 + 2 < KD) read_group(set ^ 1, s0 + 2);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) sacc[c] = mfma32(fk[set][j][c], st.q[s0 + j], sacc[c]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    u32x4 av[2][4];   // V^T operands of one d block, read one block ahead
+    auto read_tr = [&](int set, int b) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) av[set][g] = dma_read_tr<D, kTrPad>(vt, 16 * g, 32 * b, lane);
+    };
+    read_tr(0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    if (masked) {
+        keep_branch();
+        const int lim = min(S - 1, i);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (!sees(i, j0 + 32 * c + 8 * (r >> 2) + 4 * h + (r & 3), W, lim)) sacc[c][r] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[c][r]);
+    mx = half_swap_max(mx) * c2;
+    // lazy rescaling: the weights stay below 2^kSlack, so the accumulators move
+    // only where a tile raises a row's maximum by more than that
+    const bool raise = mx > st.m + kSlack;
+    if (__any(raise)) {
+        const float m = raise ? mx : st.m;
+        const float alpha = st.m == -INFINITY ? 0.f : fast_exp2(st.m - m);
+        st.l *= alpha;
+        st.lr *= alpha;
+#pragma unroll
+        for (int b = 0; b < ND; ++b) st.o[b] *= alpha;
+        st.m = m;
+    }
+    const float m_use = st.m == -INFINITY ? 0.f : st.m;
+    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        sacc[0][r] = fast_exp2(__builtin_fmaf(sacc[0][r], c2, -m_use));
+        sacc[1][r] = fast_exp2(__builtin_fmaf(sacc[1][r], c2, -m_use));
+        l0 += sacc[0][r];
+        l1 += sacc[1][r];
+    }
+    st.l += half_swap_sum(l0 + l1);
+    u32x4 pb[4];
+    pb[0] = pack8_bf16<0>(sacc[0]);
+    pb[1] = pack8_bf16<8>(sacc[0]);
+    pb[2] = pack8_bf16<0>(sacc[1]);
+    pb[3] = pack8_bf16<8>(sacc[1]);
+    st.lr += row_sum_bf16(pb);
+#pragma unroll
+    for (int b = 0; b < ND; ++b) {
+        const int set = b & 1;
+        if (b + 1 < ND) read_tr(set ^ 1, b + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) st.o[b] = mfma32(av[set][g], pb[g], st.o[b]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// Two waves per SIMD at head dim 128 (256 registers), three at 64.
+template <int D>
+__global__ void __launch_bounds__(kFwdThreads) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 3 : 2)))
+window_fwd_kernel(WindowArgs a) {
+    constexpr int KD = WinRows<D>::KD, ND = WinRows<D>::ND;
+    constexpr int KE = DmaTile<D, kRowPad>::kElems, VE = DmaTile<D, kTrPad>::kElems;
+    __shared__ uint16_t k0s[KE], v0s[VE], k1s[KE], v1s[VE];
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int b, hq, tile;
+    window_tile_of(a, blockIdx.x, (a.seq + kFwdRows - 1) / kFwdRows, b, hq, tile);
+    const Sequence sq = sequence(a, b);
+    const int i0 = tile * kFwdRows;
+    if (i0 >= sq.n) return;
+    const int last = sq.n - 1;
+    const int hk = hq / (a.Hq / a.Hkv);
+    const uint16_t* kp = head_rows(a, a.k, sq, hk);
+    const uint16_t* vp = head_rows(a, a.v, sq, hk);
+    const int w0 = i0 + 32 * w, i = w0 + l32;    // the wave's first row, this lane's row
+    WinRows<D> st;
+    {
+        const uint16_t* qp = head_rows(a, a.q, sq, hq) + min(i, last) * a.q.token;
+#pragma unroll
+        for (int s = 0; s < KD; ++s) st.q[s] = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * h);
+    }
+#pragma unroll
+    for (int x = 0; x < ND; ++x) st.o[x] = f32x16{};
+    const float c2 = a.scale * kLog2e;
+    const KeyWalk walk = key_walk(i0, min(i0 + kFwdRows - 1, last), a.W, a.S);
+    auto load = [&](uint16_t* kt, uint16_t* vt, int t) {
+        const int row0 = 64 * walk.tile(t);
+        dma_sequence<D, kRowPad, 4>(kt, kp, a.k.token, row0, last, w, lane);
+        dma_sequence<D, kTrPad, 4>(vt, vp, a.v.token, row0, last, w, lane);
+    };
+    load(k0s, v0s, 0);
+    wait_vmem();
+    __syncthreads();
+    auto step = [&](int t, const uint16_t* ck, const uint16_t* cv, uint16_t* nk, uint16_t* nv) {
+        if (t + 1 < walk.tiles) load(nk, nv, t + 1);
+        const int j0 = 64 * walk.tile(t);
+        const Sight seen = sight(w0, w0 + 31, j0, j0 + 63, a.W, a.S);
+        if (seen != kNone && w0 <= last) win_tile<D>(ck, cv, seen == kPart, i, j0, a.W, a.S, st, lane, c2);
+        __builtin_amdgcn_sched_barrier(0);
+        wait_vmem();
+        __syncthreads();
+    };
+    for (int t = 0; t < walk.tiles; t += 2) {
+        step(t, k0s, v0s, k1s, v1s);
+        if (t + 1 < walk.tiles) step(t + 1, k1s, v1s, k0s, v0s);
+    }
+    if (i > last) return;
+    const float inv = 1.f / st.lr;
+    uint16_t* op = head_rows(a, a.out, sq, hq) + i * a.out.token;
+#pragma unroll
+    for (int x = 0; x < ND; ++x)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            u32x2 pk;
+            pk.x = pack_bf16x2(st.o[x][4 * g + 0] * inv, st.o[x][4 * g + 1] * inv);
+            pk.y = pack_bf16x2(st.o[x][4 * g + 2] * inv, st.o[x][4 * g + 3] * inv);
+            *reinterpret_cast<u32x2*>(op + 32 * x + 8 * g + 4 * h) = pk;
+        }
+    if (h == 0) a.lse[lse_row(a, sq, hq) + i] = (st.m + fast_log2(st.l)) * kLn2;
+}
+
+}  // namespace
+
+hipError_t launch_window_fwd(const WindowArgs& a, hipStream_t s) {
+    const int64_t tiles = (a.seq + kFwdRows - 1) / kFwdRows;
+    TraceScope _t("window_fwd", s);
+    const dim3 g(unsigned(tiles * a.B * a.Hq)), t(kFwdThreads);
+    if (a.d == 128) hipLaunchKernelGGL(window_fwd_kernel<128>, g, t, 0, s, a);
+    else hipLaunchKernelGGL(window_fwd_kernel<64>, g, t, 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace msparse
