@@ -469,8 +469,8 @@ typedef struct {
  * read, not written: add the counts afterwards.
  *   k, v     bf16 [batch, heads_kv, tokens, head_dim]
  *   q, q_out bf16 [batch, heads_q, tokens, head_dim] or both NULL: the same
- *            tokens' queries, rotated; q_out may be q (same strides).  Rows past
- *            counts[b] are left as they were.
+ *            tokens' queries, rotated, all `tokens` rows whatever the counts;
+ *            q_out may be q (same strides)
  *   inv_freq fp32 [head_dim / 2] on the device, or NULL for no rotation: columns
  *            (i, i + head_dim / 2) of a query or key at position p turn by the
  *            angle p inv_freq[i] (reduced in 64 bits)

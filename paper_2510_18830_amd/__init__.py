@@ -8,7 +8,6 @@ implementation: if libmsparse.so is missing the first call raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -364,48 +363,56 @@ def attn_bwd(dims, q, k, v, out, dout, lse, index: SparseIndex, dq=None, dk=None
 
 
 # ------------------------------------------------------------------ static pattern, cache: arguments
+_BF16, _F32, _I32, _F8 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+
+
 def _refuse(msg):
     raise MsparseError(-1, f"invalid argument: {msg}")
 
 
 def _arg(t, name, shape, dtype, device):
-    """A contiguous tensor argument of this shape, type and device."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+    """The address of a contiguous tensor argument of this shape, type and device."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
-                f"expected contiguous {dtype} {shape} on {device}")
-    return c_vp(t.data_ptr())
+                f"expected contiguous {dtype} {tuple(shape)} on {device}")
+    return t.data_ptr()
 
 
 def _rows(t, name, shape, device):
     """A bf16 tensor [batch, heads, tokens, head_dim] of any strides with contiguous rows, as an msparse_tensor."""
-    if t.dtype != torch.bfloat16 or t.device != device or tuple(t.shape) != shape:
-        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}; expected {torch.bfloat16} {shape} on {device}")
-    st = t.stride()
-    if st[3] != 1:
-        _refuse(f"{name} has rows of stride {st[3]}")
-    return Tensor(t.data_ptr(), *(0 if n == 1 else x for n, x in zip(shape[:3], st)))
+    if t.dtype != _BF16 or t.shape != shape or t.device != device:
+        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}; expected {_BF16} {tuple(shape)} on {device}")
+    batch, head, token, column = t.stride()
+    if column != 1:
+        _refuse(f"{name} has rows of stride {column}")
+    return Tensor(t.data_ptr(), batch, head, token)
 
 
-def _on(device, stream):
-    """The context and stream pointer of a launch on `device`: what the call allocates belongs to that stream."""
+def _elsewhere(device, stream):
+    """Whether a call has to enter a stream (or a device) that is not the current one."""
     if device.type != "cuda":
         _refuse(f"tensors on {device}")
+    return stream is not None or device.index != torch.cuda.current_device()
+
+
+def _enter(device, stream):
+    """The context of a call on `stream` (None: the device's current one): what it allocates belongs to that stream."""
     if stream is None:
         stream = torch.cuda.current_stream(device)
-        if device.index == torch.cuda.current_device():
-            return contextlib.nullcontext(), c_vp(stream.cuda_stream)
     elif stream.device != device:
         _refuse(f"stream on {stream.device}, tensors on {device}")
-    return torch.cuda.stream(stream), c_vp(stream.cuda_stream)
+    return torch.cuda.stream(stream)
 
 
 def _room(workspace, nbytes, device):
-    """A workspace of at least nbytes: the caller's, or a new one."""
+    """Address and size of the caller's workspace, or of a new one."""
     if workspace is None:
-        workspace = _workspace(nbytes, device)
+        if nbytes == 0:
+            return None, None, 0
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
     elif workspace.device != device or not workspace.is_contiguous():
-        _refuse(f"workspace on {workspace.device}")
-    return workspace, workspace.numel() * workspace.element_size()
+        _refuse(f"workspace on {workspace.device}{'' if workspace.is_contiguous() else ', not contiguous'}")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 # ------------------------------------------------------------------ window attention
@@ -422,23 +429,25 @@ def _window_shapes(win):
 
 
 def _starts(win, starts, device):
-    return None if starts is None else _arg(starts, "starts", (win.batch + 1,), torch.int32, device)
+    return None if starts is None else _arg(starts, "starts", (win.batch + 1,), _I32, device)
 
 
 def window_fwd(win: Window, q, k, v, starts=None, out=None, lse=None, stream=None):
     """msparse_window_fwd: returns (out bf16 like q, lse fp32 [B, Hq, N]).  Packed sequences (win.tokens > 0): tensors
     [1, heads, tokens, d], lse [1, Hq, tokens], starts int32 [batch + 1]; rows of no sequence keep their contents."""
     dev = q.device
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return window_fwd(win, q, k, v, starts, out, lse)
     qs, ks = _window_shapes(win)
-    ctx, s = _on(dev, stream)
-    with ctx:
-        if out is None:
-            out = torch.empty(qs, dtype=torch.bfloat16, device=dev)
-        if lse is None:
-            lse = torch.empty(qs[:3], dtype=torch.float32, device=dev)
-        _check(lib().msparse_window_fwd(win, _starts(win, starts, dev), _rows(q, "q", qs, dev), _rows(k, "k", ks, dev),
-                                        _rows(v, "v", ks, dev), _rows(out, "out", qs, dev),
-                                        _arg(lse, "lse", qs[:3], torch.float32, dev), s))
+    tq = _rows(q, "q", qs, dev)
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty(qs[:3], dtype=_F32, device=dev)
+    _check(lib().msparse_window_fwd(win, _starts(win, starts, dev), tq, _rows(k, "k", ks, dev), _rows(v, "v", ks, dev),
+                                    _rows(out, "out", qs, dev), _arg(lse, "lse", qs[:3], _F32, dev),
+                                    torch.cuda.current_stream(dev).cuda_stream))
     return out, lse
 
 
@@ -448,21 +457,21 @@ def window_bwd_workspace_bytes(win: Window) -> int:
 
 def window_bwd(win: Window, q, k, v, out, dout, lse, starts=None, dq=None, dk=None, dv=None, workspace=None,
                stream=None):
-    """msparse_window_bwd: returns (dq, dk, dv) bf16, from window_fwd's out and lse."""
+    """msparse_window_bwd: returns (dq, dk, dv) bf16 like q, k, v, from window_fwd's out and lse."""
     dev = q.device
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return window_bwd(win, q, k, v, out, dout, lse, starts, dq, dk, dv, workspace)
     qs, ks = _window_shapes(win)
-    bf = torch.bfloat16
-    ctx, s = _on(dev, stream)
-    with ctx:
-        dq = torch.empty(qs, dtype=bf, device=dev) if dq is None else dq
-        dk = torch.empty(ks, dtype=bf, device=dev) if dk is None else dk
-        dv = torch.empty(ks, dtype=bf, device=dev) if dv is None else dv
-        workspace, room = _room(workspace, window_bwd_workspace_bytes(win), dev)
-        _check(lib().msparse_window_bwd(win, _starts(win, starts, dev), _rows(q, "q", qs, dev), _rows(k, "k", ks, dev),
-                                        _rows(v, "v", ks, dev), _rows(out, "out", qs, dev),
-                                        _rows(dout, "dout", qs, dev), _arg(lse, "lse", qs[:3], torch.float32, dev),
-                                        _rows(dq, "dq", qs, dev), _rows(dk, "dk", ks, dev), _rows(dv, "dv", ks, dev),
-                                        _p(workspace), room, s))
+    tq, tk, tv = _rows(q, "q", qs, dev), _rows(k, "k", ks, dev), _rows(v, "v", ks, dev)
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(v) if dv is None else dv
+    workspace, at, room = _room(workspace, window_bwd_workspace_bytes(win), dev)
+    _check(lib().msparse_window_bwd(win, _starts(win, starts, dev), tq, tk, tv, _rows(out, "out", qs, dev),
+                                    _rows(dout, "dout", qs, dev), _arg(lse, "lse", qs[:3], _F32, dev),
+                                    _rows(dq, "dq", qs, dev), _rows(dk, "dk", ks, dev), _rows(dv, "dv", ks, dev),
+                                    at, room, torch.cuda.current_stream(dev).cuda_stream))
     return dq, dk, dv
 
 
@@ -478,11 +487,11 @@ class Cache:
 
 
 def make_cache(pages, heads_kv, head_dim, device) -> Cache:
-    f8 = torch.float8_e4m3fn
-    return Cache(torch.empty((pages, heads_kv, 64, head_dim), dtype=f8, device=device),
-                 torch.empty((pages, heads_kv, head_dim, 64), dtype=f8, device=device),
-                 torch.empty((pages, heads_kv), dtype=torch.float32, device=device),
-                 torch.empty((pages, heads_kv), dtype=torch.float32, device=device))
+    """An empty pool (its memory as it comes: no token is in it)."""
+    return Cache(torch.empty((pages, heads_kv, 64, head_dim), dtype=_F8, device=device),
+                 torch.empty((pages, heads_kv, head_dim, 64), dtype=_F8, device=device),
+                 torch.empty((pages, heads_kv), dtype=_F32, device=device),
+                 torch.empty((pages, heads_kv), dtype=_F32, device=device))
 
 
 def _cache(cache, page_table, lens, device):
@@ -490,42 +499,45 @@ def _cache(cache, page_table, lens, device):
         _refuse(f"cache.k is {tuple(cache.k.shape)}, page_table {tuple(page_table.shape)}")
     pages, heads, page, d = cache.k.shape
     B, width = page_table.shape
-    if page != 64:
-        _refuse(f"pages of {page} tokens (64)")
-    f8, f32, i32 = torch.float8_e4m3fn, torch.float32, torch.int32
-    return CacheStruct(_arg(cache.k, "cache.k", (pages, heads, 64, d), f8, device),
-                       _arg(cache.v, "cache.v", (pages, heads, d, 64), f8, device),
-                       _arg(cache.k_scale, "cache.k_scale", (pages, heads), f32, device),
-                       _arg(cache.v_scale, "cache.v_scale", (pages, heads), f32, device),
-                       _arg(page_table, "page_table", (B, width), i32, device), _arg(lens, "lens", (B,), i32, device),
+    return CacheStruct(_arg(cache.k, "cache.k", (pages, heads, 64, d), _F8, device),
+                       _arg(cache.v, "cache.v", (pages, heads, d, 64), _F8, device),
+                       _arg(cache.k_scale, "cache.k_scale", (pages, heads), _F32, device),
+                       _arg(cache.v_scale, "cache.v_scale", (pages, heads), _F32, device),
+                       _arg(page_table, "page_table", (B, width), _I32, device), _arg(lens, "lens", (B,), _I32, device),
                        pages, width, B, heads, d)
 
 
 def cache_append(cache: Cache, page_table, lens, k, v, q=None, inv_freq=None, counts=None, q_out=None, stream=None):
     """msparse_cache_append: k, v bf16 [B, Hkv, T, d] after the lens [B] tokens that the sequences hold (counts [B] of
-    the T tokens; None: all); returns the rotated q (bf16 [B, Hq, T, d]), None without one.  lens is not changed."""
+    the T tokens; None: all); returns the rotated q (bf16 [B, Hq, T, d], all T rows), None without one.  lens is not
+    changed."""
     dev = k.device
-    ctx, s = _on(dev, stream)
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return cache_append(cache, page_table, lens, k, v, q, inv_freq, counts, q_out)
     c = _cache(cache, page_table, lens, dev)
     if k.dim() != 4:
         _refuse(f"k is {tuple(k.shape)}")
     T = k.shape[2]
     ks = (c.batch, c.heads_kv, T, c.head_dim)
-    with ctx:
-        tq = tqo = None
-        heads_q = c.heads_kv
-        if q is not None:
-            heads_q = q.shape[1]
-            qs = (c.batch, heads_q, T, c.head_dim)
-            if q_out is None:
-                q_out = torch.empty(qs, dtype=torch.bfloat16, device=dev)
-            tq, tqo = _rows(q, "q", qs, dev), _rows(q_out, "q_out", qs, dev)
-        elif q_out is not None:
-            _refuse("q_out without q")
-        freq = None if inv_freq is None else _arg(inv_freq, "inv_freq", (c.head_dim // 2,), torch.float32, dev)
-        cnt = None if counts is None else _arg(counts, "counts", (c.batch,), torch.int32, dev)
-        _check(lib().msparse_cache_append(c, heads_q, T, tq, _rows(k, "k", ks, dev), _rows(v, "v", ks, dev), tqo, freq,
-                                          cnt, s))
+    tk, tv = _rows(k, "k", ks, dev), _rows(v, "v", ks, dev)
+    tq = tqo = None
+    heads_q = c.heads_kv
+    if q is not None:
+        if q.dim() != 4:
+            _refuse(f"q is {tuple(q.shape)}")
+        heads_q = q.shape[1]
+        qs = (c.batch, heads_q, T, c.head_dim)
+        tq = _rows(q, "q", qs, dev)
+        if q_out is None:
+            q_out = torch.empty_like(q)
+        tqo = _rows(q_out, "q_out", qs, dev)
+    elif q_out is not None:
+        _refuse("q_out without q")
+    freq = None if inv_freq is None else _arg(inv_freq, "inv_freq", (c.head_dim // 2,), _F32, dev)
+    cnt = None if counts is None else _arg(counts, "counts", (c.batch,), _I32, dev)
+    _check(lib().msparse_cache_append(c, heads_q, T, tq, tk, tv, tqo, freq, cnt,
+                                      torch.cuda.current_stream(dev).cuda_stream))
     return q_out
 
 
@@ -539,23 +551,25 @@ def cache_attn_workspace_bytes(cache: Cache, page_table, heads_q, tokens=1) -> i
 def cache_attn(cache: Cache, page_table, lens, q, window=0, sinks=0, scale=0.0, out=None, lse=None, workspace=None,
                stream=None):
     """msparse_cache_attn: the newest T tokens' queries (bf16 [B, Hq, T, d], rotated) over the first lens [B] tokens of
-    their sequences, themselves included; returns (out bf16, lse fp32 [B, Hq, T])."""
+    their sequences, themselves included; returns (out bf16 like q, lse fp32 [B, Hq, T])."""
     dev = q.device
-    ctx, s = _on(dev, stream)
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return cache_attn(cache, page_table, lens, q, window, sinks, scale, out, lse, workspace)
     c = _cache(cache, page_table, lens, dev)
     if q.dim() != 4:
         _refuse(f"q is {tuple(q.shape)}")
     heads_q, T = q.shape[1], q.shape[2]
     qs = (c.batch, heads_q, T, c.head_dim)
-    with ctx:
-        if out is None:
-            out = torch.empty(qs, dtype=torch.bfloat16, device=dev)
-        if lse is None:
-            lse = torch.empty(qs[:3], dtype=torch.float32, device=dev)
-        workspace, room = _room(workspace, lib().msparse_cache_attn_workspace(c, heads_q, T), dev)
-        _check(lib().msparse_cache_attn(c, heads_q, T, window, sinks, scale, _rows(q, "q", qs, dev),
-                                        _rows(out, "out", qs, dev), _arg(lse, "lse", qs[:3], torch.float32, dev),
-                                        _p(workspace), room, s))
+    tq = _rows(q, "q", qs, dev)
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty(qs[:3], dtype=_F32, device=dev)
+    workspace, at, room = _room(workspace, lib().msparse_cache_attn_workspace(c, heads_q, T), dev)
+    _check(lib().msparse_cache_attn(c, heads_q, T, window, sinks, scale, tq, _rows(out, "out", qs, dev),
+                                    _arg(lse, "lse", qs[:3], _F32, dev), at, room,
+                                    torch.cuda.current_stream(dev).cuda_stream))
     return out, lse
 
 

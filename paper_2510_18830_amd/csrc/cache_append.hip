@@ -120,12 +120,14 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
     const int64_t base = int64_t(lp) * kPage;
     const int s0 = int(max(int64_t(len) - base, int64_t(0)));                  // slots [s0, s1) are new
     const int s1 = int(min(int64_t(len) + cnt - base, int64_t(kPage)));
-    if (s1 <= s0) return;
     const int m = s1 - s0;
     const int t0 = int(base + s0 - len);           // their first token of the call
-    const int page = cache_page(a.c, b, lp);
+    // queries are rotated for all T tokens, the count's and those behind it alike
+    const int mq = a.q ? int(min(int64_t(len) + a.T - base, int64_t(kPage))) - s0 : 0;
+    if (max(m, mq) <= 0) return;
+    const int page = m > 0 ? cache_page(a.c, b, lp) : -1;
     if (a.freq) {
-        for (int x = tid; x < m * H2; x += kThreads) {
+        for (int x = tid; x < max(m, mq) * H2; x += kThreads) {
             const int t = x / H2, i = x % H2;
             float c, s;
             cos_sin(int(base + s0 + t), a.freq[i], c, s);
@@ -241,11 +243,11 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
             }
         }
     // ---- the queries of this share's heads
-    if (!a.q) return;
+    if (mq <= 0) return;
     constexpr int QC = D / 16;                     // chunks of 8 pairs of columns
     const int heads = (a.Hq - share + a.split - 1) / a.split;
-    for (int x = tid; x < heads * m * QC; x += kThreads) {
-        const int c = x % QC, t = x / QC % m, h = share + a.split * (x / (QC * m));
+    for (int x = tid; x < heads * mq * QC; x += kThreads) {
+        const int c = x % QC, t = x / QC % mq, h = share + a.split * (x / (QC * mq));
         const uint16_t* src = a.q + b * a.qs[0] + h * a.qs[1] + (t0 + t) * a.qs[2] + 8 * c;
         uint16_t* dst = a.qout + b * a.qos[0] + h * a.qos[1] + (t0 + t) * a.qos[2] + 8 * c;
         u32x4 lo = *reinterpret_cast<const u32x4*>(src), hi = *reinterpret_cast<const u32x4*>(src + H2);
