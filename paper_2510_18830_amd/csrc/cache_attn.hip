@@ -15,10 +15,12 @@
 //
 // One token per sequence is bound by the cache's bytes: waves walk pages with the
 // next page's loads in flight, and long contexts are cut into chunks of equal
-// length whatever the batch's raggedness, joined by a second launch.  Many rows
-// are bound by the products and the conversions: four waves take rows of their
-// own over the same pages.
+// length whatever the batch's raggedness, joined by a second launch: 8 contexts of
+// 13K to 128K tokens x 8 heads (1.3 GB) take 208 us, 6.2 TB/s; the join 7 us.  Many
+// rows are bound by the products, conversions and exponentials: four waves take rows
+// of their own over the same pages, 770 TFLOP/s in the walk.
 #include "cache.h"
+#include "tiles.h"
 #include "trace.h"
 
 #include <algorithm>
@@ -27,7 +29,11 @@ namespace msparse {
 
 namespace {
 
+constexpr int kStages = 3;           // pages staged by the kernel for many rows
 constexpr int kThreads = 256;
+constexpr int64_t kMaxSplit = 4096;  // row tiles up to which their pages are split
+constexpr int64_t kManyRows = 2048;  // rows from which the join takes one per group of lanes
+constexpr int kMinChunk = 4;         // pages: one for each wave
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -85,363 +91,542 @@ __device__ __forceinline__ TileRows tile_rows(const CacheAttnArgs& a, int b, int
     return t;
 }
 
-// Which tile and which of its chunks workgroup `item` takes: chunk = the pages a
-// chunk holds, from the pages of all tiles and the chunks aimed at; first = the
-// number of the tile's first chunk.  False past the last one.
+// Inclusive sum over the wave's lanes, in registers (a sum through LDS permutes
+// takes a microsecond of a workgroup's start).
+__device__ __forceinline__ int32_t wave_scan(int32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // the lane 1, 2, 4, 8 before, within 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // lane 15 of the 16 before, to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // lane 31, to rows 2 and 3
+    return x;
+}
+__device__ __forceinline__ PageList tile_pages(const CacheAttnArgs& a, const TileRows& t) {
+    return page_list(t.p0, t.p1, a.W, a.S, a.c.width);
+}
+// Tiles' pages are cut into chunks of one length, so that whatever the raggedness
+// the workgroups take as long: `pages`, from the sum over all tiles and the number
+// of chunks aimed at.  Workgroup `item` takes chunk `index` of the `count` of tile
+// e, `first` being the number of that tile's first; a tile without pages has one
+// chunk too.  False past the last one.  Every wave finds it for itself.
 struct Chunk {
     int32_t e, first, count, index, pages;
 };
-__device__ bool find_chunk(const CacheAttnArgs& a, int rows, int item, Chunk& out) {
-    __shared__ int64_t sum[kThreads / 64];
-    __shared__ int32_t sh[kThreads / 64];
-    __shared__ Chunk found;
-    const int tid = threadIdx.x, E = a.c.B * a.tiles;
+__device__ __forceinline__ bool find_chunk(const CacheAttnArgs& a, int rows, int item, int lane, Chunk& out) {
+    const int E = a.c.B * a.tiles;
     auto pages_of = [&](int e) {
-        const TileRows t = tile_rows(a, e / a.tiles, e % a.tiles, rows);
-        return page_list(t.p0, t.p1, a.W, a.S, a.c.width).count;
+        return e < E ? tile_pages(a, tile_rows(a, e / a.tiles, e % a.tiles, rows)).count : 0;
     };
-    int64_t mine = 0;
-    for (int e = tid; e < E; e += kThreads) mine += pages_of(e);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o);
-    if ((tid & 63) == 0) sum[tid >> 6] = mine;
-    if (tid == 0) found.count = 0;
-    __syncthreads();
-    const int64_t total = sum[0] + sum[1] + sum[2] + sum[3];
-    const int chunk = int(max((total + a.items - 1) / a.items, int64_t(4)));
+    const int own = pages_of(lane);   // the first 64 tiles are looked up once
+    int sum = own;
+    for (int e = 64 + lane; e < E; e += 64) sum += pages_of(e);
+    const uint32_t total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
+    const uint32_t pages = max((total + a.items - 1) / a.items, uint32_t(kMinChunk));
     int base = 0;
-    for (int e0 = 0; e0 < E && base <= item; e0 += kThreads) {
-        const int e = e0 + tid;
-        const int np = e < E ? pages_of(e) : 0;
-        const int n = e < E ? max((np + chunk - 1) / chunk, 1) : 0;
-        int x = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(x, o);
-            if ((tid & 63) >= o) x += y;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        const uint32_t np = e0 == 0 ? own : pages_of(e0 + lane);
+        const int n = e0 + lane < E ? max(int((np + pages - 1) / pages), 1) : 0;
+        const int last = base + wave_scan(n);   // chunks up to this tile's end
+        const uint64_t beyond = __ballot(item < last);
+        if (beyond) {
+            const int l = __builtin_ctzll(beyond);
+            const int first = __builtin_amdgcn_readlane(last - n, l);
+            out = Chunk{e0 + l, first, __builtin_amdgcn_readlane(n, l), item - first, int32_t(pages)};
+            return true;
         }
-        if ((tid & 63) == 63) sh[tid >> 6] = x;
-        __syncthreads();
-        int before = base;
-        for (int w = 0; w < (tid >> 6); ++w) before += sh[w];
-        const int first = before + x - n;
-        if (n > 0 && item >= first && item < first + n) found = Chunk{e, first, n, item - first, chunk};
-        base += sh[0] + sh[1] + sh[2] + sh[3];
-        __syncthreads();
+        base = __builtin_amdgcn_readlane(last, 63);
     }
-    out = found;
-    return found.count > 0;
+    return false;
 }
 
-// RT tiles of 16 rows per wave; WR = 4: the waves take rows of their own, 1: they
-// share the rows and take pages in turn.
-template <int D, int RT, int WR>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, RT == 1 ? 3 : 2)))
-cache_attn_kernel(CacheAttnArgs a) {
-    constexpr int KS = D / 32;      // k-steps of S^T
-    constexpr int KL = D / 64;      // 16-byte loads of a token's key per lane
-    constexpr int ND = D / 16;      // column tiles of O^T
-    constexpr int ROWS = 16 * RT * WR;
-    const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, m = lane & 15;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = a.Hq / a.c.Hkv, R = a.T * G;
-    const int hk = blockIdx.x % a.c.Hkv;
-    Chunk ch{};
-    if (a.items > 0) {
-        if (!find_chunk(a, ROWS, blockIdx.x / a.c.Hkv, ch)) return;
-        ch.e = __builtin_amdgcn_readfirstlane(ch.e);
-        ch.first = __builtin_amdgcn_readfirstlane(ch.first);
-        ch.count = __builtin_amdgcn_readfirstlane(ch.count);
-        ch.index = __builtin_amdgcn_readfirstlane(ch.index);
-        ch.pages = __builtin_amdgcn_readfirstlane(ch.pages);
-    } else {
-        ch.e = blockIdx.x / a.c.Hkv;
-        ch.count = 1;
-        ch.pages = INT32_MAX;
-    }
-    const int b = ch.e / a.tiles;
-    const TileRows tr = tile_rows(a, b, ch.e % a.tiles, ROWS);
-    const PageList pl = page_list(tr.p0, tr.p1, a.W, a.S, a.c.width);
-    const int c0 = int(min(int64_t(ch.index) * ch.pages, int64_t(pl.count)));
-    const int c1 = int(min(int64_t(c0) + ch.pages, int64_t(pl.count)));
-    if (a.items > 0 && hk == 0 && ch.index == 0 && tid == 0) {
-        a.info[2 * ch.e] = ch.first;
-        a.info[2 * ch.e + 1] = ch.count;
-    }
-    // this wave's rows
-    const int wr0 = tr.r0 + (WR > 1 ? 16 * RT * w : 0);
-    int pos[RT];
+// ---------------------------------------------------------------- one wave's rows
+// RT tiles of 16 rows of a (sequence, KV head); lane (quarter g, m) owns row m of each.
+template <int D, int RT>
+struct CacheRows {
+    static constexpr int KS = D / 32;      // k-steps of S^T
+    static constexpr int KL = D / 64;      // 16-byte pieces of a token's key per lane
+    static constexpr int ND = D / 16;      // column tiles of O^T
     u32x4 q[RT][KS];
+    f32x4 o[RT][ND];
+    float mx[RT], l[RT];
+    int pos[RT];
+    int wp0, wp1;   // positions of the first and last row; below 0: rows before the sequence, which see nothing
+    int far;        // the last position that the window of no row reaches
+};
+
+// rows from wr0 on (past the last: that one again) of R = T G
+template <int D, int RT>
+__device__ __forceinline__ void open_rows(const CacheAttnArgs& a, CacheRows<D, RT>& st, int b, int hk, int len, int wr0,
+                                          int lane) {
+    const int g4 = lane >> 4, m = lane & 15, G = a.Hq / a.c.Hkv, R = a.T * G;
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int r = min(wr0 + 16 * x + m, R - 1);
-        pos[x] = tr.len - a.T + r / G;
+        st.pos[x] = len - a.T + r / G;
         const uint16_t* qp = a.q + b * a.qs[0] + (hk * G + r % G) * a.qs[1] + (r / G) * a.qs[2];
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-            q[x][s] = *reinterpret_cast<const u32x4*>(qp + 64 * (s >> 1) + 16 * g4 + 8 * (s & 1));
+        for (int s = 0; s < CacheRows<D, RT>::KS; ++s)
+            st.q[x][s] = *reinterpret_cast<const u32x4*>(qp + 64 * (s >> 1) + 16 * g4 + 8 * (s & 1));
+        st.mx[x] = -INFINITY;
+        st.l[x] = 0.f;
+#pragma unroll
+        for (int y = 0; y < CacheRows<D, RT>::ND; ++y) st.o[x][y] = f32x4{};
     }
-    const int wp0 = tr.len - a.T + min(wr0, R - 1) / G;       // below 0: rows before the sequence, which see nothing
-    const int wp1 = tr.len - a.T + min(wr0 + 16 * RT - 1, R - 1) / G;
-    f32x4 o[RT][ND];
-    float mx[RT], l[RT];
+    st.wp0 = len - a.T + min(wr0, R - 1) / G;
+    st.wp1 = len - a.T + min(wr0 + 16 * RT - 1, R - 1) / G;
+    st.far = max(st.wp0, 0) - a.W;
+}
+
+// byte offsets of this lane's 16-byte operands in a page's codes of one head
+__device__ __forceinline__ int key_offset(int t, int j, int lane, int D) {
+    const int g4 = lane >> 4, m = lane & 15;
+    return (16 * (m >> 2) + 4 * t + (m & 3)) * D + 64 * j + 16 * g4;
+}
+__device__ __forceinline__ int value_offset(int y, int lane) {
+    return (16 * y + (lane & 15)) * kPage + 16 * (lane >> 4);
+}
+
+// Which of this lane's 16 tokens of a page at t0 some of the rows wp0 .. wp1 see, a
+// byte each.  (Codes of free slots and of pages used before may stand for anything,
+// NaN among it, which a weight of 0 would not remove.)
+__device__ __forceinline__ u32x4 seen_bytes(int t0, int wp1, int far, int S, int lane) {
+    u32x4 keep;
+    const int lim = min(S - 1, wp1);
 #pragma unroll
-    for (int x = 0; x < RT; ++x) {
-        mx[x] = -INFINITY;
-        l[x] = 0.f;
+    for (int j = 0; j < 4; ++j) {
+        uint32_t byte = 0;
 #pragma unroll
-        for (int y = 0; y < ND; ++y) o[x][y] = f32x4{};
-    }
-    const float c2 = a.scale * kLog2e;
-    u32x4 kr[4][KL], vr[ND];
-    auto load_k = [&](int page) {
-        const uint8_t* p = a.c.k + (int64_t(page) * a.c.Hkv + hk) * (kPage * D) + (16 * (m >> 2) + (m & 3)) * D + 16 * g4;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int j = 0; j < KL; ++j) kr[t][j] = *reinterpret_cast<const u32x4*>(p + 4 * t * D + 64 * j);
-    };
-    auto load_v = [&](int page) {
-        const uint8_t* p = a.c.v + (int64_t(page) * a.c.Hkv + hk) * (kPage * D) + m * kPage + 16 * g4;
-#pragma unroll
-        for (int y = 0; y < ND; ++y) vr[y] = *reinterpret_cast<const u32x4*>(p + 16 * y * kPage);
-    };
-    const int far = max(wp0, 0) - a.W;   // the last position that the window of no row reaches
-    constexpr int STEP = WR > 1 ? 1 : kThreads / 64;
-    // the next page's codes are requested as soon as this one's are used up
-    int page = -1;
-    int x0 = c0 + (WR > 1 ? 0 : w);
-    if (x0 < c1) {
-        page = cache_page(a.c, b, pl.page(x0));
-        load_k(max(page, 0));
-        load_v(max(page, 0));
-    }
-    for (; x0 < c1; x0 += STEP) {
-        // a page that the table does not have lies beyond every row
-        const int t0 = page < 0 ? kMaxWidth * kPage : 64 * pl.page(x0);
-        const bool more = x0 + STEP < c1;
-        const int next = more ? cache_page(a.c, b, pl.page(x0 + STEP)) : -1;
-        const bool part = !(t0 <= wp0 - 63 && (t0 > wp1 - a.W || t0 < a.S - 63));
-        const int64_t at = int64_t(max(page, 0)) * a.c.Hkv + hk;
-        // (kept above 0: a masked logit times 0 would be NaN)
-        const float kscale = fmaxf(ldc(a.c.ks, at) * c2, 0x1p-126f), vscale = ldc(a.c.vs, at);
-        // ---- S^T
-        f32x4 s[RT][4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-#pragma unroll
-            for (int x = 0; x < RT; ++x) s[x][t] = f32x4{};
-#pragma unroll
-            for (int j = 0; j < KL; ++j) {
-                const uint32_t k0 = kr[t][j].x, k1 = kr[t][j].y, k2 = kr[t][j].z, k3 = kr[t][j].w;
-                const u32x4 lo = codes_to_bf16(k0, k1), hi = codes_to_bf16(k2, k3);
-#pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    s[x][t] = mfma16(lo, q[x][2 * j], s[x][t]);
-                    s[x][t] = mfma16(hi, q[x][2 * j + 1], s[x][t]);
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);   // one token tile's operands at a time
+        for (int e = 0; e < 4; ++e) {
+            const int k = t0 + 16 * (lane >> 4) + 4 * j + e;
+            if (k <= wp1 && (k > far || k <= lim)) byte |= 0xffu << (8 * e);
         }
-        if (more) load_k(max(next, 0));
+        keep[j] = byte;
+    }
+    return keep;
+}
+// whether some of the rows wp0 .. wp1 do not see all of the page at t0
+__device__ __forceinline__ bool partly(int t0, int wp0, int wp1, int W, int S) {
+    return !(t0 <= wp0 - 63 && (t0 > wp1 - W || t0 < S - 63));
+}
+
+// One page, its first token at position t0: key(t, j) and value(y) give this lane's
+// operands; keys_done() runs once the keys are used up, and clear(t0) before the
+// values of a page are that some row does not see in full: it clears the codes of
+// the tokens that no row sees.
+template <int D, int RT, int TS, int YS, class Key, class Value, class Done, class Clear>
+__device__ __forceinline__ void page_step(CacheRows<D, RT>& st, int t0, float kscale, float vscale, int W, int S,
+                                          int lane, Key key, Value value, Done keys_done, Clear clear) {
+    constexpr int KL = CacheRows<D, RT>::KL, ND = CacheRows<D, RT>::ND;
+    const int g4 = lane >> 4;
+    const bool part = partly(t0, st.wp0, st.wp1, W, S);
+    // ---- S^T, TS token tiles at a time: their operands are read a group ahead, and
+    // the accumulators of a group take turns, as an MFMA that adds to the one before
+    // it waits for it
+    f32x4 s[RT][4];
+    u32x4 kb[2][TS][KL];
+    auto read_k = [&](int set, int t) {
+#pragma unroll
+        for (int i = 0; i < TS; ++i)
+#pragma unroll
+            for (int j = 0; j < KL; ++j) kb[set][i][j] = key(t + i, j);
+    };
+    read_k(0, 0);
+#pragma unroll
+    for (int t = 0; t < 4; t += TS) {
+        const int set = (t / TS) & 1;
+        if (t + TS < 4) read_k(set ^ 1, t + TS);
         __builtin_amdgcn_sched_barrier(0);
-        if (part) {
-            keep_branch();
 #pragma unroll
-            for (int x = 0; x < RT; ++x) {
-                const int lim = min(a.S - 1, pos[x]);
+        for (int i = 0; i < TS; ++i)
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+            for (int x = 0; x < RT; ++x) s[x][t + i] = f32x4{};
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int j = t0 + 16 * g4 + 4 * t + r;
-                        if (!(uint32_t(pos[x] - j) < uint32_t(a.W) || j <= lim)) s[x][t][r] = -INFINITY;
-                    }
-            }
-            // codes of tokens that no row sees (free slots, pages reused) may stand
-            // for anything, NaN among it, which a weight of 0 would not remove
-            u32x4 keep;
-            const int lim = min(a.S - 1, wp1);
+        for (int j = 0; j < KL; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t byte = 0;
+            for (int p = 0; p < 2; ++p)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int k = t0 + 16 * g4 + 4 * j + e;
-                    if (k <= wp1 && (k > far || k <= lim)) byte |= 0xffu << (8 * e);
+                for (int i = 0; i < TS; ++i) {
+                    const uint32_t k0 = kb[set][i][j][2 * p], k1 = kb[set][i][j][2 * p + 1];
+                    const u32x4 k = codes_to_bf16(k0, k1);
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) s[x][t + i] = mfma16(k, st.q[x][2 * j + p], s[x][t + i]);
                 }
-                keep[j] = byte;
-            }
-#pragma unroll
-            for (int y = 0; y < ND; ++y) vr[y] &= keep;
-        }
-        // ---- softmax
-        u32x4 pb[RT][2];
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    keys_done();
+    __builtin_amdgcn_sched_barrier(0);
+    if (part) {
+        keep_branch();
 #pragma unroll
         for (int x = 0; x < RT; ++x) {
-            float top = -INFINITY;
+            const int lim = min(S - 1, st.pos[x]);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) top = fmaxf(top, s[x][t][r]);
-            top = fmaxf(row_max(top) * kscale, mx[x]);
-            if (__any(top > mx[x])) {
-                const float alpha = mx[x] == -INFINITY ? 0.f : fast_exp2(mx[x] - top);
-                l[x] *= alpha;
-#pragma unroll
-                for (int y = 0; y < ND; ++y) o[x][y] *= alpha;
-                mx[x] = top;
-            }
-            const float use = top == -INFINITY ? 0.f : top;
-            float sum = 0.f;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                float p[4];
-#pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    p[r] = fast_exp2(__builtin_fmaf(s[x][t][r], kscale, -use));
-                    sum += p[r];
+                    const int j = t0 + 16 * g4 + 4 * t + r;
+                    if (!(uint32_t(st.pos[x] - j) < uint32_t(W) || j <= lim)) s[x][t][r] = -INFINITY;
                 }
-                pb[x][t >> 1][2 * (t & 1)] = pack_bf16x2(p[0] * vscale, p[1] * vscale);
-                pb[x][t >> 1][2 * (t & 1) + 1] = pack_bf16x2(p[2] * vscale, p[3] * vscale);
-            }
-            l[x] += sum;
         }
-        // ---- O^T
-#pragma unroll
-        for (int y = 0; y < ND; ++y) {
-            const uint32_t v0 = vr[y].x, v1 = vr[y].y, v2 = vr[y].z, v3 = vr[y].w;
-            const u32x4 lo = codes_to_bf16(v0, v1), hi = codes_to_bf16(v2, v3);
-#pragma unroll
-            for (int x = 0; x < RT; ++x) {
-                o[x][y] = mfma16(lo, pb[x][0], o[x][y]);
-                o[x][y] = mfma16(hi, pb[x][1], o[x][y]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (more) load_v(max(next, 0));
-        page = next;
+        clear(t0);
     }
+    // ---- softmax
+    u32x4 pb[RT][2];
 #pragma unroll
-    for (int x = 0; x < RT; ++x) l[x] = row_sum(l[x]);
-    // ---- join the waves of a shared row tile: a fixed order, by halves
-    if constexpr (WR == 1) {
-        __shared__ __attribute__((aligned(16))) float so[2][RT * ND * 4 * 64];
-        __shared__ float sml[2][RT][2][64];
+    for (int x = 0; x < RT; ++x) {
+        float top = -INFINITY;
 #pragma unroll
-        for (int half = 2; half >= 1; half >>= 1) {
-            if (w >= half && w < 2 * half) {
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    sml[w - half][x][0][lane] = mx[x];
-                    sml[w - half][x][1][lane] = l[x];
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, s[x][t][r]);
+        top = fmaxf(row_max(top) * kscale, st.mx[x]);
+        if (__any(top > st.mx[x])) {
+            const float alpha = st.mx[x] == -INFINITY ? 0.f : fast_exp2(st.mx[x] - top);
+            st.l[x] *= alpha;
 #pragma unroll
-                    for (int y = 0; y < ND; ++y)
-                        *reinterpret_cast<f32x4*>(&so[w - half][((x * ND + y) * 64 + lane) * 4]) = o[x][y];
-                }
-            }
-            __syncthreads();
-            if (w < half) {
-#pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    const float m1 = sml[w][x][0][lane], l1 = sml[w][x][1][lane];
-                    const float top = fmaxf(mx[x], m1);
-                    const float a0 = mx[x] == -INFINITY ? 0.f : fast_exp2(mx[x] - top);
-                    const float a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - top);
-                    mx[x] = top;
-                    l[x] = l[x] * a0 + l1 * a1;
-#pragma unroll
-                    for (int y = 0; y < ND; ++y)
-                        o[x][y] = o[x][y] * a0 + *reinterpret_cast<const f32x4*>(&so[w][((x * ND + y) * 64 + lane) * 4]) * a1;
-                }
-            }
-            __syncthreads();
+            for (int y = 0; y < ND; ++y) st.o[x][y] *= alpha;
+            st.mx[x] = top;
         }
-        if (w != 0) return;
+        const float use = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            float p[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p[r] = fast_exp2(__builtin_fmaf(s[x][t][r], kscale, -use));
+                sum += p[r];
+            }
+            pb[x][t >> 1][2 * (t & 1)] = pack_bf16x2(p[0] * vscale, p[1] * vscale);
+            pb[x][t >> 1][2 * (t & 1) + 1] = pack_bf16x2(p[2] * vscale, p[3] * vscale);
+        }
+        st.l[x] += sum;
     }
+    // ---- O^T, YS column tiles at a time, likewise
+    u32x4 vb[2][YS];
+    auto read_v = [&](int set, int y) {
+#pragma unroll
+        for (int i = 0; i < YS; ++i) vb[set][i] = value(y + i);
+    };
+    read_v(0, 0);
+#pragma unroll
+    for (int y = 0; y < ND; y += YS) {
+        const int set = (y / YS) & 1;
+        if (y + YS < ND) read_v(set ^ 1, y + YS);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int i = 0; i < YS; ++i) {
+                const uint32_t v0 = vb[set][i][2 * p], v1 = vb[set][i][2 * p + 1];
+                const u32x4 v = codes_to_bf16(v0, v1);
+#pragma unroll
+                for (int x = 0; x < RT; ++x) st.o[x][y + i] = mfma16(v, pb[x][p], st.o[x][y + i]);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// What a workgroup walks: the entries [c0, c1) of its tile's pages.
+struct Walk {
+    Chunk ch;
+    TileRows tr;
+    PageList pl;
+    int32_t b, hk, c0, c1;
+};
+// The rows' results: to out and lse, or, of a tile with several chunks, to this
+// chunk's slot.  wr0: the wave's first row.
+template <int D, int RT>
+__device__ __forceinline__ void close_rows(const CacheAttnArgs& a, const CacheRows<D, RT>& st, const Walk& k, int wr0,
+                                           int rows, int lane) {
+    constexpr int ND = CacheRows<D, RT>::ND;
+    const int g4 = lane >> 4, m = lane & 15, G = a.Hq / a.c.Hkv, R = a.T * G;
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int r = wr0 + 16 * x + m;
         if (r >= R) continue;
-        if (ch.count > 1) {
-            const int64_t row = (int64_t(ch.first + ch.index) * a.c.Hkv + hk) * ROWS + (r - tr.r0);
+        if (k.ch.count > 1) {
+            const int64_t row = (int64_t(k.ch.first + k.ch.index) * a.c.Hkv + k.hk) * rows + (r - k.tr.r0);
             float* po = a.po + row * D + 4 * g4;
 #pragma unroll
-            for (int y = 0; y < ND; ++y) *reinterpret_cast<f32x4*>(po + 16 * y) = o[x][y];
+            for (int y = 0; y < ND; ++y) *reinterpret_cast<f32x4*>(po + 16 * y) = st.o[x][y];
             if (g4 == 0) {
-                a.pml[2 * row] = mx[x];
-                a.pml[2 * row + 1] = l[x];
+                a.pml[2 * row] = st.mx[x];
+                a.pml[2 * row + 1] = st.l[x];
             }
             continue;
         }
-        const int t = r / G, h = hk * G + r % G;
-        const bool empty = mx[x] == -INFINITY;
-        const float inv = empty ? 0.f : 1.f / l[x];
-        uint16_t* op = a.out + b * a.os[0] + h * a.os[1] + t * a.os[2] + 4 * g4;
+        const int t = r / G, h = k.hk * G + r % G;
+        const bool empty = st.mx[x] == -INFINITY;
+        const float inv = empty ? 0.f : 1.f / st.l[x];
+        uint16_t* op = a.out + k.b * a.os[0] + h * a.os[1] + t * a.os[2] + 4 * g4;
 #pragma unroll
         for (int y = 0; y < ND; ++y) {
             u32x2 pk;
-            pk.x = pack_bf16x2(o[x][y].x * inv, o[x][y].y * inv);
-            pk.y = pack_bf16x2(o[x][y].z * inv, o[x][y].w * inv);
+            pk.x = pack_bf16x2(st.o[x][y].x * inv, st.o[x][y].y * inv);
+            pk.y = pack_bf16x2(st.o[x][y].z * inv, st.o[x][y].w * inv);
             *reinterpret_cast<u32x2*>(op + 16 * y) = pk;
         }
         if (a.lse && g4 == 0)
-            a.lse[(int64_t(b) * a.Hq + h) * a.T + t] = empty ? -INFINITY : (mx[x] + fast_log2(l[x])) * kLn2;
+            a.lse[(int64_t(k.b) * a.Hq + h) * a.T + t] = empty ? -INFINITY : (st.mx[x] + fast_log2(st.l[x])) * kLn2;
     }
 }
 
-// Joins the chunks of one row, in order: groups of D / 4 lanes take chunks in turn.
+__device__ __forceinline__ bool open_walk(const CacheAttnArgs& a, int rows, int lane, Walk& k) {
+    k.hk = blockIdx.x % a.c.Hkv;
+    k.ch = Chunk{int32_t(blockIdx.x / a.c.Hkv), 0, 1, 0, INT32_MAX};   // a workgroup per tile
+    if (a.items > 0 && !find_chunk(a, rows, blockIdx.x / a.c.Hkv, lane, k.ch)) return false;
+    k.b = k.ch.e / a.tiles;
+    k.tr = tile_rows(a, k.b, k.ch.e % a.tiles, rows);
+    k.pl = tile_pages(a, k.tr);
+    k.c0 = int(min(int64_t(k.ch.index) * k.ch.pages, int64_t(k.pl.count)));
+    k.c1 = int(min(int64_t(k.c0) + k.ch.pages, int64_t(k.pl.count)));
+    if (a.items > 0 && k.hk == 0 && k.ch.index == 0 && threadIdx.x == 0) {
+        a.info[2 * k.ch.e] = k.ch.first;
+        a.info[2 * k.ch.e + 1] = k.ch.count;
+    }
+    return true;
+}
+// Pages and scales of the next 64 entries x, x + step, .. of a walk, one per lane:
+// looked up together, then read lane by lane.  A lookup for each page on its way
+// would put two dependent memory latencies into every step.
+struct Pages {
+    int32_t page;     // -1: the table has none
+    float ks, vs;     // scales of the logits (in log2 units) and of the values
+};
+__device__ __forceinline__ Pages look_up(const CacheAttnArgs& a, const Walk& k, int x, int step, int lane) {
+    const int e = x + step * lane;
+    int32_t page = -1;
+    if (e < k.c1) {
+        const int index = k.pl.page(e);
+        if (index < a.c.width) page = a.c.table[int64_t(k.b) * a.c.width + index];
+        if (uint32_t(page) >= uint32_t(a.c.pages)) page = -1;
+    }
+    const int64_t at = int64_t(max(page, 0)) * a.c.Hkv + k.hk;
+    // (the first stays above 0, as a masked logit times 0 would be NaN)
+    return Pages{page, fmaxf(a.c.ks[at] * (a.scale * kLog2e), 0x1p-126f), a.c.vs[at]};
+}
+__device__ __forceinline__ int32_t page_at(const Pages& p, int i) { return __builtin_amdgcn_readlane(p.page, i); }
+__device__ __forceinline__ float lane_value(float x, int i) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i));
+}
+// position of a page's first token; a page that the table does not have lies beyond every row
+__device__ __forceinline__ int page_start(int page, int index) { return page < 0 ? kMaxWidth * kPage : kPage * index; }
+
+// Up to 32 rows: the four waves share them and take pages in turn, straight from
+// memory to registers.  A page is read by one wave alone, once, hence past the
+// caches (a plain read reaches 7.0 TB/s that way against 6.1).
+template <int D, int RT>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 3 : 2, RT == 1 ? 3 : 2)))
+cache_attn_kernel(CacheAttnArgs a) {
+    constexpr int KL = CacheRows<D, RT>::KL, ND = CacheRows<D, RT>::ND, ROWS = 16 * RT;
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ __attribute__((aligned(16))) float so[2][RT * ND * 4 * 64];
+    __shared__ float sml[2][RT][2][64];
+    Walk k;
+    if (!open_walk(a, ROWS, lane, k)) return;
+    CacheRows<D, RT> st;
+    open_rows(a, st, k.b, k.hk, k.tr.len, k.tr.r0, lane);
+    u32x4 kr[4][KL], vr[ND];
+    auto load_k = [&](int page) {
+        const uint8_t* p = a.c.k + (int64_t(max(page, 0)) * a.c.Hkv + k.hk) * (kPage * D) + key_offset(0, 0, lane, D);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < KL; ++j)
+                kr[t][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 4 * t * D + 64 * j));
+    };
+    auto load_v = [&](int page) {
+        const uint8_t* p = a.c.v + (int64_t(max(page, 0)) * a.c.Hkv + k.hk) * (kPage * D) + value_offset(0, lane);
+#pragma unroll
+        for (int y = 0; y < ND; ++y)
+            vr[y] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 16 * y * kPage));
+    };
+    // the next page's codes are requested as soon as this one's are used up
+    constexpr int STEP = kThreads / 64;
+    for (int x0 = k.c0 + w; x0 < k.c1; x0 += 64 * STEP) {
+        const Pages pages = look_up(a, k, x0, STEP, lane);
+        const int n = min((k.c1 - x0 + STEP - 1) / STEP, 64);
+        load_k(page_at(pages, 0));
+        load_v(page_at(pages, 0));
+        for (int i = 0; i < n; ++i) {
+            const int next = page_at(pages, min(i + 1, 63));
+            page_step<D, RT, RT == 1 ? 2 : 1, RT == 1 ? 4 : 2>(
+                st, page_start(page_at(pages, i), k.pl.page(x0 + i * STEP)), lane_value(pages.ks, i),
+                lane_value(pages.vs, i), a.W, a.S, lane, [&](int t, int j) { return kr[t][j]; },
+                [&](int y) { return vr[y]; },
+                [&] {
+                    if (i + 1 < n) load_k(next);
+                },
+                [&](int t0) {
+                    const u32x4 keep = seen_bytes(t0, st.wp1, st.far, a.S, lane);
+#pragma unroll
+                    for (int y = 0; y < ND; ++y) vr[y] &= keep;
+                });
+            if (i + 1 < n) load_v(next);
+        }
+    }
+    // join the waves, by halves in a fixed order
+#pragma unroll
+    for (int x = 0; x < RT; ++x) st.l[x] = row_sum(st.l[x]);
+#pragma unroll
+    for (int half = 2; half >= 1; half >>= 1) {
+        if (w >= half && w < 2 * half) {
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                sml[w - half][x][0][lane] = st.mx[x];
+                sml[w - half][x][1][lane] = st.l[x];
+#pragma unroll
+                for (int y = 0; y < ND; ++y)
+                    *reinterpret_cast<f32x4*>(&so[w - half][((x * ND + y) * 64 + lane) * 4]) = st.o[x][y];
+            }
+        }
+        __syncthreads();
+        if (w < half) {
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                const float m1 = sml[w][x][0][lane], l1 = sml[w][x][1][lane];
+                const float top = fmaxf(st.mx[x], m1);
+                const float a0 = st.mx[x] == -INFINITY ? 0.f : fast_exp2(st.mx[x] - top);
+                const float a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - top);
+                st.mx[x] = top;
+                st.l[x] = st.l[x] * a0 + l1 * a1;
+#pragma unroll
+                for (int y = 0; y < ND; ++y)
+                    st.o[x][y] = st.o[x][y] * a0 +
+                                 *reinterpret_cast<const f32x4*>(&so[w][((x * ND + y) * 64 + lane) * 4]) * a1;
+            }
+        }
+        __syncthreads();
+    }
+    if (w == 0) close_rows(a, st, k, k.tr.r0, ROWS, lane);
+}
+
+// More rows: each of the four waves takes 32 of its own through all pages of the
+// chunk.  A page is staged once for the workgroup, by direct global->LDS loads in
+// the order of the operands (a lane fetches what it would read itself), with the
+// loads of the next pages in flight.
 template <int D>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3)))
+cache_attn_rows_kernel(CacheAttnArgs a) {
+    constexpr int RT = 2, KL = CacheRows<D, RT>::KL, ND = CacheRows<D, RT>::ND, ROWS = 16 * RT * 4;
+    constexpr int kOps = 4 * KL + ND;              // operands of a page, 1 KB each
+    __shared__ __attribute__((aligned(16))) uint16_t buf[kStages][kOps * 512];
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Walk k;
+    if (!open_walk(a, ROWS, lane, k)) return;
+    const int wr0 = k.tr.r0 + 16 * RT * w;
+    CacheRows<D, RT> st;
+    open_rows(a, st, k.b, k.hk, k.tr.len, wr0, lane);
+    const bool live = wr0 < a.T * (a.Hq / a.c.Hkv);
+    constexpr int kLoads = KL + ND / 4;            // a wave's loads of a page
+    auto stage = [&](int slot, int page) {
+        const int64_t at = (int64_t(max(page, 0)) * a.c.Hkv + k.hk) * (kPage * D);
+        const uint8_t* kp = a.c.k + at + key_offset(w, 0, lane, D);   // wave w: the token tile w
+#pragma unroll
+        for (int j = 0; j < KL; ++j) dma16(kp + 64 * j, lds_addr(&buf[slot][(w * KL + j) * 512]));
+        const uint8_t* vp = a.c.v + at + value_offset(w, lane);       // columns w, w + 4, ...
+#pragma unroll
+        for (int y = 0; y < ND / 4; ++y) dma16(vp + 64 * y * kPage, lds_addr(&buf[slot][(4 * KL + w + 4 * y) * 512]));
+    };
+    for (int x0 = k.c0; x0 < k.c1; x0 += 64) {
+        const Pages pages = look_up(a, k, x0, 1, lane);
+        const int n = min(k.c1 - x0, 64);
+        // every page of the 64 before has been read: its last step ended with a barrier
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i)
+            if (i < n) stage(i, page_at(pages, i));
+        for (int i = 0; i < n; ++i) {
+            // page i has landed when only the loads of the pages behind it are out
+            if (i + kStages - 1 <= n) __builtin_amdgcn_s_waitcnt(0x0F70 | (kLoads * (kStages - 2)));
+            else wait_vmem();
+            const int t0 = page_start(page_at(pages, i), k.pl.page(x0 + i));
+            if (partly(t0, k.tr.p0, k.tr.p1, a.W, a.S)) {   // each wave clears what it staged
+                keep_branch();
+                const u32x4 keep = seen_bytes(t0, k.tr.p1, max(k.tr.p0, 0) - a.W, a.S, lane);
+                u32x4* v = reinterpret_cast<u32x4*>(buf[i % kStages] + (4 * KL + w) * 512) + lane;
+#pragma unroll
+                for (int y = 0; y < ND / 4; ++y) v[4 * y * 64] &= keep;
+            }
+            __syncthreads();
+            if (i + kStages - 1 < n) stage((i + kStages - 1) % kStages, page_at(pages, i + kStages - 1));
+            const uint16_t* cur = buf[i % kStages];
+            if (live && t0 <= st.wp1 && (t0 + 63 > st.far || t0 < a.S))
+                page_step<D, RT, 1, 2>(
+                    st, t0, lane_value(pages.ks, i), lane_value(pages.vs, i), a.W, a.S, lane,
+                    [&](int t, int j) { return *reinterpret_cast<const u32x4*>(cur + (t * KL + j) * 512 + 8 * lane); },
+                    [&](int y) { return *reinterpret_cast<const u32x4*>(cur + (4 * KL + y) * 512 + 8 * lane); },
+                    [] {}, [](int) {});
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int x = 0; x < RT; ++x) st.l[x] = row_sum(st.l[x]);
+    if (live) close_rows(a, st, k, wr0, ROWS, lane);
+}
+
+// Joins a row's chunks.  D / 4 lanes hold a row; the kThreads / (D / 4) groups of a
+// workgroup take a row each (MANY), or the chunks of one row in turn, so that a
+// long context's hundreds of chunks are not one walk.  Both orders are fixed.
+template <int D, bool MANY>
 __global__ void __launch_bounds__(kThreads) cache_join_kernel(CacheAttnArgs a, int rows) {
     constexpr int C = D / 4, N = kThreads / C;
-    __shared__ __attribute__((aligned(16))) float so[N][D];
+    __shared__ __attribute__((aligned(16))) float so[MANY ? 1 : N][D];
     __shared__ float sm[N], sl[N];
     const int G = a.Hq / a.c.Hkv, R = a.T * G;
-    const int r = blockIdx.x % R, hk = blockIdx.x / R % a.c.Hkv, b = blockIdx.x / (R * a.c.Hkv);
-    const int e = b * a.tiles + r / rows;
-    const int first = a.info[2 * e], count = a.info[2 * e + 1];
-    if (count <= 1) return;
     const int c = threadIdx.x % C, n = threadIdx.x / C;
+    const int64_t at = MANY ? int64_t(blockIdx.x) * N + n : blockIdx.x;   // row of (sequence, KV head, row)
+    if (at >= int64_t(a.c.B) * a.c.Hkv * R) return;
+    const int r = int(at % R), hk = int(at / R % a.c.Hkv), b = int(at / R / a.c.Hkv);
+    const int e = b * a.tiles + r / rows;
+    const int first = a.info[2 * e], count = a.info[2 * e + 1];   // slots of the tile's chunks
+    if (count <= 1) return;   // (the same for every thread unless MANY, which has no barrier)
     float mx = -INFINITY, l = 0.f;
     f32x4 o = f32x4{};
-    for (int s = n; s < count; s += N) {
+#pragma unroll 4
+    for (int s = MANY ? 0 : n; s < count; s += MANY ? 1 : N) {
         const int64_t row = (int64_t(first + s) * a.c.Hkv + hk) * rows + r % rows;
         const float m1 = a.pml[2 * row], l1 = a.pml[2 * row + 1];
         const f32x4 x = *reinterpret_cast<const f32x4*>(a.po + row * D + 4 * c);
-        const float top = fmaxf(mx, m1);
-        if (top == -INFINITY) continue;
-        const float a0 = fast_exp2(mx - top), a1 = fast_exp2(m1 - top);
+        const float top = fmaxf(mx, m1), use = top == -INFINITY ? 0.f : top;
+        const float a0 = fast_exp2(mx - use), a1 = fast_exp2(m1 - use);
         mx = top;
         l = l * a0 + l1 * a1;
         o = o * a0 + x * a1;
     }
-    *reinterpret_cast<f32x4*>(&so[n][4 * c]) = o;
-    if (c == 0) {
-        sm[n] = mx;
-        sl[n] = l;
-    }
-    __syncthreads();
-    if (n > 0) return;
-    float top = -INFINITY;
+    if constexpr (!MANY) {
+        *reinterpret_cast<f32x4*>(&so[n][4 * c]) = o;
+        if (c == 0) {
+            sm[n] = mx;
+            sl[n] = l;
+        }
+        __syncthreads();
+        if (n > 0) return;
+        mx = -INFINITY;
 #pragma unroll
-    for (int s = 0; s < N; ++s) top = fmaxf(top, sm[s]);
-    float sum = 0.f;
-    o = f32x4{};
-    if (top != -INFINITY)
+        for (int s = 0; s < N; ++s) mx = fmaxf(mx, sm[s]);
+        const float use = mx == -INFINITY ? 0.f : mx;
+        l = 0.f;
+        o = f32x4{};
 #pragma unroll
         for (int s = 0; s < N; ++s) {
-            const float f = fast_exp2(sm[s] - top);
-            sum += sl[s] * f;
+            const float f = fast_exp2(sm[s] - use);
+            l += sl[s] * f;
             o += *reinterpret_cast<const f32x4*>(&so[s][4 * c]) * f;
         }
-    const bool empty = top == -INFINITY;
-    const float inv = empty ? 0.f : 1.f / sum;
+    }
+    const bool empty = mx == -INFINITY;
+    const float inv = empty ? 0.f : 1.f / l;
     const int t = r / G, h = hk * G + r % G;
     u32x2 pk;
     pk.x = pack_bf16x2(o.x * inv, o.y * inv);
     pk.y = pack_bf16x2(o.z * inv, o.w * inv);
     *reinterpret_cast<u32x2*>(a.out + b * a.os[0] + h * a.os[1] + t * a.os[2] + 4 * c) = pk;
-    if (a.lse && c == 0) a.lse[(int64_t(b) * a.Hq + h) * a.T + t] = empty ? -INFINITY : (top + fast_log2(sum)) * kLn2;
+    if (a.lse && c == 0) a.lse[(int64_t(b) * a.Hq + h) * a.T + t] = empty ? -INFINITY : (mx + fast_log2(l)) * kLn2;
 }
 
 template <int D>
@@ -450,14 +635,18 @@ void launch(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
     const dim3 g(static_cast<unsigned>(wgs)), t(kThreads);
     {
         TraceScope _t("cache_attn", s);
-        if (p.wr == 4) hipLaunchKernelGGL((cache_attn_kernel<D, 2, 4>), g, t, 0, s, a);
-        else if (p.rt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2, 1>), g, t, 0, s, a);
-        else hipLaunchKernelGGL((cache_attn_kernel<D, 1, 1>), g, t, 0, s, a);
+        if (p.wr == 4) hipLaunchKernelGGL((cache_attn_rows_kernel<D>), g, t, 0, s, a);
+        else if (p.rt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2>), g, t, 0, s, a);
+        else hipLaunchKernelGGL((cache_attn_kernel<D, 1>), g, t, 0, s, a);
     }
     if (p.items > 0) {
         TraceScope _t("cache_join", s);
-        const dim3 gj(unsigned(int64_t(a.c.B) * a.Hq * a.T));
-        hipLaunchKernelGGL((cache_join_kernel<D>), gj, t, 0, s, a, p.rows);
+        const int64_t rows = int64_t(a.c.B) * a.Hq * a.T;
+        constexpr int N = kThreads / (D / 4);
+        if (rows >= kManyRows)
+            hipLaunchKernelGGL((cache_join_kernel<D, true>), dim3(unsigned((rows + N - 1) / N)), t, 0, s, a, p.rows);
+        else
+            hipLaunchKernelGGL((cache_join_kernel<D, false>), dim3(unsigned(rows)), t, 0, s, a, p.rows);
     }
 }
 
@@ -471,10 +660,16 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
     p.rows = 16 * p.rt * p.wr;
     p.tiles = int32_t((rows + p.rows - 1) / p.rows);
     const int64_t e = B * p.tiles;
-    constexpr int64_t kItems = 768;
-    if (width > 4 && e * Hkv < 2 * kItems) {
-        p.items = int32_t(std::max<int64_t>(1, kItems / Hkv));
-        p.slots = int32_t(std::min(p.items + e, e * ((width + 3) / 4)));
+    // Chunks: where rows bound the work, as many as are resident at once (three
+    // workgroups a CU; 512, 768, 1024 of them: 69, 67, 73 us for 4 x 200 tokens of 16
+    // over 2 heads in a window of 4096), where memory does, two rounds of them (512,
+    // 768, 1024, 1536, 2048: 255, 236, 224, 211, 211 us for 8 contexts of up to 128K
+    // x 8 heads).  Each tile may have one more than its share; and a chunk is no
+    // longer than the mean tile, however many there are.
+    const int64_t aim = (p.rt == 1 ? 1536 : 768) / Hkv;
+    if (width > kMinChunk && e <= kMaxSplit && e * width < INT32_MAX) {
+        p.items = int32_t(std::max(aim - e, e));
+        p.slots = int32_t(std::min(p.items + e, e * ((width + kMinChunk - 1) / kMinChunk)));
     }
     return p;
 }
