@@ -840,14 +840,15 @@ static WindowArgs window_args(const msparse_window* w, const int32_t* starts) {
 
 // lse log2(e) and Delta of every row, the sink keys' partial gradients.
 static size_t carve_window_bwd(WindowArgs* a, char* base) {
-    const SinkPlan p = sink_plan(a->B, a->Hkv, a->Hq / a->Hkv, a->seq, a->W, a->S);
-    a->sink_pairs = p.pairs;
+    const int keys = window_key_group(a->d);
+    const SinkPlan p = sink_plan(a->B, a->Hkv, a->Hq / a->Hkv, a->seq, a->W, a->S, keys);
+    a->sink_groups = p.groups;
     a->slots = p.slots;
     a->chunk = p.chunk;
     a->rows_pad = a->tokens > 0 ? padded_rows(a->tokens) + 64 * (int64_t(a->B) + 1) : a->B * padded_rows(a->seq);
     Carve c{base};
     a->rows = c.take<float>(size_t(2) * a->Hq * a->rows_pad);
-    a->part = c.take<float>(size_t(a->B) * a->Hkv * p.pairs * p.slots * 2 * 128 * a->d);
+    a->part = c.take<float>(size_t(a->B) * a->Hkv * p.groups * p.slots * 2 * keys * a->d);
     return c.off;
 }
 

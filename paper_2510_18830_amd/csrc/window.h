@@ -38,9 +38,9 @@ struct WindowArgs {
     // backward workspace
     float* rows;           // [Hq][2][rows_pad]: lse log2(e) and Delta of every row, sequences from a multiple of 64 on
     int64_t rows_pad;
-    float* part;           // sink keys' partial gradients: [B Hkv sink_pairs][slots][2][128][d]
-    int32_t sink_pairs;    // pairs of key blocks that hold sinks
-    int32_t slots;         // partials of such a pair: its window's, then `slots - 1` chunks of the rows beyond
+    float* part;           // sink keys' partial gradients: [B Hkv sink_groups][slots][2][keys of a group][d]
+    int32_t sink_groups;   // groups of key blocks that hold sinks
+    int32_t slots;         // partials of such a group: its window's, then `slots - 1` chunks of the rows beyond
     int32_t chunk;         // query tiles of a chunk
 };
 
@@ -141,18 +141,20 @@ __device__ __forceinline__ void window_tile_of(const WindowArgs& a, int64_t t, i
 hipError_t launch_window_fwd(const WindowArgs& a, hipStream_t s);
 hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s);
 
-// Sizes of the backward's partial gradients of the sink keys (0 sink_pairs: none).
+// Keys that a workgroup of the key-major backward takes.
+int window_key_group(int d);
+// Sizes of the backward's partial gradients of the sink keys (0 groups: none).
 struct SinkPlan {
-    int32_t pairs, slots, chunk;
+    int32_t groups, slots, chunk;
 };
-inline SinkPlan sink_plan(int64_t B, int64_t Hkv, int64_t G, int64_t seq, int64_t W, int64_t S) {
+inline SinkPlan sink_plan(int64_t B, int64_t Hkv, int64_t G, int64_t seq, int64_t W, int64_t S, int64_t keys) {
     SinkPlan p{0, 0, 0};
     const int64_t tiles = (seq + 63) / 64;
     const int64_t first = W / 64;             // the rows of tiles before are inside the window of key 0
     if (S <= 0 || W >= seq || first >= tiles) return p;
-    p.pairs = int32_t((std::min(S, seq) + 127) / 128);
-    const int64_t beyond = G * (tiles - first);      // query tiles beyond a pair's window, at most
-    const int64_t items = std::max<int64_t>(1, std::min<int64_t>(256, 1024 / (B * Hkv * p.pairs)));
+    p.groups = int32_t((std::min(S, seq) + keys - 1) / keys);
+    const int64_t beyond = G * (tiles - first);      // query tiles beyond a group's window, at most
+    const int64_t items = std::max<int64_t>(1, std::min<int64_t>(256, 1024 / (B * Hkv * p.groups)));
     p.chunk = int32_t(std::max<int64_t>(16, (beyond + items - 1) / items));
     p.slots = int32_t(1 + (beyond + p.chunk - 1) / p.chunk);
     return p;

@@ -4,13 +4,13 @@
 // dK and dV summed over the query heads of each KV head.
 //
 // Launches on the caller's stream, all deterministic (no atomics):
-//   rows    lse log2(e) and Delta of every row, in blocks of 64 from each
-//           sequence's start (rows past its end: P = 0)
-//   dq      query-major, as the forward: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dZ^T
-//   dkdv    key-major over pairs of 64-key blocks: S = Q K^T, dP = dO V^T,
+//   dq      query-major, as the forward: S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dZ^T;
+//           it leaves lse log2(e) and Delta of its rows for the next pass, in blocks of
+//           64 from each sequence's start (rows past its end: P = 0)
+//   dkdv    key-major over groups of 64-key blocks: S = Q K^T, dP = dO V^T,
 //           dV^T += dO^T P, dK^T += Q^T dZ over the heads of the KV group and the
-//           query tiles of the pair's window.  Sink keys are seen by every later
-//           row too: a walk over the whole sequence for a single pair, so those
+//           query tiles of the keys' window.  Sink keys are seen by every later
+//           row too: a walk over the whole sequence for a single group, so those
 //           rows are cut into chunks, a workgroup each, and the chunks' sums go
 //           to the workspace (fp32)
 //   sinks   adds them up, chunks in order.
@@ -19,44 +19,13 @@
 #include "window.h"
 #include "trace.h"
 
+#ifndef MS_KB64
+#define MS_KB64 1
+#define MS_KW64 3
+#endif
 namespace msparse {
 
 namespace {
-
-// ------------------------------------------------------------------ row values
-constexpr int kRowThreads = 256;
-
-// 16 lanes per row; a workgroup takes 64 rows.
-template <int D>
-__global__ void __launch_bounds__(kRowThreads) window_rows_kernel(WindowArgs a) {
-    constexpr int PER = D / 16;
-    const int blocks = (a.seq + 63) >> 6, bh = blockIdx.x / blocks, i0 = 64 * (blockIdx.x % blocks);
-    const int h = bh % a.Hq;
-    const Sequence sq = sequence(a, bh / a.Hq);
-    if (i0 >= sq.n) return;
-    const int64_t v0 = value_row(a, sq);
-    float* lse2 = a.rows + int64_t(2 * h) * a.rows_pad + v0;
-    float* delta = lse2 + a.rows_pad;
-    const uint16_t* gp = head_rows(a, a.dout, sq, h);
-    const uint16_t* op = head_rows(a, a.out, sq, h);
-    const float* lse = a.lse + lse_row(a, sq, h);
-    const int sub = threadIdx.x & 15;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int i = i0 + 16 * u + (threadIdx.x >> 4), r = min(i, sq.n - 1);
-        const uint32_t* g = reinterpret_cast<const uint32_t*>(gp + r * a.dout.token + sub * PER);
-        const uint32_t* o = reinterpret_cast<const uint32_t*>(op + r * a.out.token + sub * PER);
-        float acc = 0.f;
-#pragma unroll
-        for (int j = 0; j < PER / 2; ++j) acc += bf16_lo(g[j]) * bf16_lo(o[j]) + bf16_hi(g[j]) * bf16_hi(o[j]);
-#pragma unroll
-        for (int off = 8; off >= 1; off >>= 1) acc += __shfl_xor(acc, off);
-        if (sub == 0) {
-            lse2[i] = i < sq.n ? lse[i] * kLog2e : INFINITY;
-            delta[i] = i < sq.n ? acc : 0.f;
-        }
-    }
-}
 
 // ------------------------------------------------------------------ dQ
 constexpr int kDqThreads = 256, kDqRows = 128;
@@ -145,14 +114,29 @@ __global__ void __launch_bounds__(kDqThreads)
     {
         const uint16_t* qp = head_rows(a, a.q, sq, hq) + ic * a.q.token;
         const uint16_t* gp = head_rows(a, a.dout, sq, hq) + ic * a.dout.token;
+        const uint16_t* op = head_rows(a, a.out, sq, hq) + ic * a.out.token;
+        u32x4 o[KD];
 #pragma unroll
         for (int s = 0; s < KD; ++s) {
             st.q[s] = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * h);
             st.g[s] = *reinterpret_cast<const u32x4*>(gp + 16 * s + 8 * h);
+            o[s] = *reinterpret_cast<const u32x4*>(op + 16 * s + 8 * h);
         }
-        const float* rv = a.rows + int64_t(2 * hq) * a.rows_pad + value_row(a, sq) + ic;
-        st.lse2 = rv[0];
-        st.dlt = rv[a.rows_pad];
+        // this row's lse log2(e) and Delta, for the key-major pass too
+        const bool real = i <= last;
+        st.lse2 = a.lse[lse_row(a, sq, hq) + ic] * kLog2e;
+        float acc = 0.f;
+#pragma unroll
+        for (int s = 0; s < KD; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                acc += bf16_lo(st.g[s][e]) * bf16_lo(o[s][e]) + bf16_hi(st.g[s][e]) * bf16_hi(o[s][e]);
+        st.dlt = half_swap_sum(acc);
+        if (h == 0 && i < padded_rows(sq.n)) {
+            float* rv = a.rows + int64_t(2 * hq) * a.rows_pad + value_row(a, sq) + i;
+            rv[0] = real ? st.lse2 : INFINITY;   // a row past the end: P = 0
+            rv[a.rows_pad] = real ? st.dlt : 0.f;
+        }
     }
 #pragma unroll
     for (int x = 0; x < ND; ++x) st.acc[x] = f32x16{};
@@ -193,10 +177,13 @@ __global__ void __launch_bounds__(kDqThreads)
 }
 
 // ------------------------------------------------------------------ dK / dV
-// Eight waves per pair of key blocks: wave (block, key half, row half) holds 32
-// keys' K in registers and takes 32 of each query tile's 64 rows; V of the pair
-// lies in LDS.  The row halves' sums are added at the end, in a fixed order.
-constexpr int kKvThreads = 512;
+// Four waves per block of 64 keys: wave (key half, row half) holds 32 keys' K in
+// registers and takes 32 of each query tile's 64 rows; V of the block lies in LDS.
+// The row halves' sums are added at the end, in a fixed order.  At head dim 128 a
+// workgroup has two blocks, which share the staged query tiles (two waves per SIMD,
+// one workgroup a CU); at 64 one, three workgroups a CU.
+template <int D>
+constexpr int kKeyBlocks = D == 128 ? 2 : MS_KB64;
 
 template <int D>
 struct WinTile {   // a staged query tile: Q rows, dO rows, 64 lse2, 64 Delta
@@ -290,52 +277,52 @@ __device__ __forceinline__ void kv_tile(const uint16_t* t, const u32x4* kreg, co
     }
 }
 
-// The query tiles of a key pair: its window's, tiles lo .. hi of every head of
-// the group, and those beyond it up to the sequence's end (sink pairs).
+// The query tiles of the keys j0 .. j1: their window's, tiles lo .. hi of every head
+// of the group, and those beyond it up to the sequence's end (sink keys).
 struct QueryRange {
     int lo, hi, end;
 };
-__device__ __forceinline__ QueryRange query_range(const Sequence& sq, int pair, int W) {
+__device__ __forceinline__ QueryRange query_range(const Sequence& sq, int j0, int j1, int W) {
     QueryRange r;
     r.end = (sq.n + 63) >> 6;
-    r.lo = 2 * pair;
-    const int64_t far = (int64_t(128) * pair + 126 + W) >> 6;   // the last tile with a row that sees the last key
+    r.lo = j0 >> 6;
+    const int64_t far = (int64_t(j1) - 1 + W) >> 6;   // the last tile with a row that sees the last key
     r.hi = int(min(far, int64_t(r.end - 1)));
     return r;
 }
 
-// Workgroups 0 .. B Hkv sink_pairs (slots - 1) - 1: the chunks of the sink keys'
-// rows beyond the window (the longest walks first); the rest: pairs of key blocks.
+// Workgroups 0 .. B Hkv sink_groups (slots - 1) - 1: the chunks of the sink keys'
+// rows beyond the window; the rest: groups of kKeyBlocks key blocks.
 template <int D>
-__global__ void __launch_bounds__(kKvThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-window_dkdv_kernel(WindowArgs a) {
-    constexpr int KD = D / 16, ND = D / 32;
+__global__ void __launch_bounds__(256 * kKeyBlocks<D>)
+    __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : MS_KW64, D == 128 ? 2 : MS_KW64))) window_dkdv_kernel(WindowArgs a) {
+    constexpr int KD = D / 16, ND = D / 32, KB = kKeyBlocks<D>, KEYS = 64 * KB, NW = 4 * KB;
     constexpr int TE = WinTile<D>::kElems, VE = DmaTile<D, kRowPad>::kElems;
     __shared__ __attribute__((aligned(16))) uint16_t tb[2 * TE];
-    __shared__ __attribute__((aligned(16))) uint16_t vsm[2 * VE];
+    __shared__ __attribute__((aligned(16))) uint16_t vsm[KB * VE];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = w >> 2, kh = (w >> 1) & 1, rh = w & 1;
     const int BK = a.B * a.Hkv, G = a.Hq / a.Hkv;
-    const int pairs = (a.seq + 127) >> 7;
-    const int64_t extra = int64_t(BK) * a.sink_pairs * (a.slots - 1);
-    int bk, pair, slot;      // slot: 0 the window, 1 .. a chunk beyond
+    const int groups = (a.seq + KEYS - 1) / KEYS;
+    const int64_t extra = int64_t(BK) * a.sink_groups * (a.slots - 1);
+    int bk, group, slot;      // slot: 0 the window, 1 .. a chunk beyond
     if (int64_t(blockIdx.x) < extra) {
-        bk = int(blockIdx.x / (a.sink_pairs * (a.slots - 1)));
-        const int r = int(blockIdx.x % (a.sink_pairs * (a.slots - 1)));
-        pair = r / (a.slots - 1);
+        bk = int(blockIdx.x / (a.sink_groups * (a.slots - 1)));
+        const int r = int(blockIdx.x % (a.sink_groups * (a.slots - 1)));
+        group = r / (a.slots - 1);
         slot = 1 + r % (a.slots - 1);
     } else {
-        const int64_t u = xcd_chunk(blockIdx.x - extra, int64_t(BK) * pairs);
-        bk = int(u / pairs);
-        pair = int(u % pairs);
+        const int64_t u = xcd_chunk(blockIdx.x - extra, int64_t(BK) * groups);
+        bk = int(u / groups);
+        group = int(u % groups);
         slot = 0;
     }
     const int b = bk / a.Hkv, hk = bk % a.Hkv;
     const Sequence sq = sequence(a, b);
-    if (128 * pair >= sq.n) return;
+    if (KEYS * group >= sq.n) return;
     const int last = sq.n - 1;
-    const QueryRange range = query_range(sq, pair, a.W);
+    const QueryRange range = query_range(sq, KEYS * group, KEYS * group + KEYS - 1, a.W);
     // entries [e0, e1) of the walk: head g = e / width, tile base + e % width
     int base = range.lo, width = range.hi - range.lo + 1, e0 = 0, e1 = G * width;
     if (slot > 0) {
@@ -346,7 +333,7 @@ window_dkdv_kernel(WindowArgs a) {
         if (e0 >= e1) return;
     }
     const int key = 32 * kh + l32;
-    const int j0 = 128 * pair + 64 * half, j = j0 + key;
+    const int j0 = KEYS * group + 64 * half, j = j0 + key;
     const bool live = j0 <= last && (slot == 0 || j0 < a.S);
     const uint16_t* kp = head_rows(a, a.k, sq, hk);
     u32x4 kreg[KD];
@@ -354,8 +341,9 @@ window_dkdv_kernel(WindowArgs a) {
     for (int s = 0; s < KD; ++s)
         kreg[s] = *reinterpret_cast<const u32x4*>(kp + min(j, last) * a.k.token + 16 * s + 8 * h);
     const uint16_t* vp = head_rows(a, a.v, sq, hk);
-    dma_sequence<D, kRowPad, 8>(vsm, vp, a.v.token, 128 * pair, last, w, lane);
-    dma_sequence<D, kRowPad, 8>(vsm + VE, vp, a.v.token, 128 * pair + 64, last, w, lane);
+#pragma unroll
+    for (int x = 0; x < KB; ++x)
+        dma_sequence<D, kRowPad, NW>(vsm + x * VE, vp, a.v.token, KEYS * group + 64 * x, last, w, lane);
     const uint16_t* vt = vsm + half * VE;
     f32x16 dv[ND], dk[ND];
 #pragma unroll
@@ -365,25 +353,34 @@ window_dkdv_kernel(WindowArgs a) {
     }
     const float c2 = a.scale * kLog2e;
     const int64_t v0 = value_row(a, sq);
-    auto load = [&](uint16_t* t, int e) {
-        const int hq = hk * G + e / width, row0 = 64 * (base + e % width);
-        dma_sequence<D, kDualPad, 8>(t + WinTile<D>::kQ, head_rows(a, a.q, sq, hq), a.q.token, row0, last, w, lane);
-        dma_sequence<D, kDualPad, 8>(t + WinTile<D>::kG, head_rows(a, a.dout, sq, hq), a.dout.token, row0, last, w,
-                                     lane);
+    // the walk's next entry to load
+    int lg = e0 / width, lt = e0 % width;
+    auto load = [&](uint16_t* t) {
+        const int hq = hk * G + lg, row0 = 64 * (base + lt);
+        dma_sequence<D, kDualPad, NW>(t + WinTile<D>::kQ, head_rows(a, a.q, sq, hq), a.q.token, row0, last, w, lane);
+        dma_sequence<D, kDualPad, NW>(t + WinTile<D>::kG, head_rows(a, a.dout, sq, hq), a.dout.token, row0, last, w,
+                                      lane);
         if (w == 0 && lane < 32) {   // lse2 -> floats 0..63, Delta -> floats 64..127
             const float* rv = a.rows + int64_t(2 * hq) * a.rows_pad + v0 + row0;
             dma16(lane < 16 ? rv + 4 * lane : rv + a.rows_pad + 4 * (lane - 16), lds_addr(t + WinTile<D>::kRw));
         }
+        if (++lt == width) {
+            lt = 0;
+            ++lg;
+        }
     };
-    load(tb, e0);
+    int ct = lt;   // the tile of the entry computed
+    load(tb);
     wait_vmem();
     __syncthreads();
-    auto step = [&](int e, const uint16_t* ct, uint16_t* nt) {
-        if (e + 1 < e1) load(nt, e + 1);
-        const int i0 = 64 * (base + e % width), r0 = i0 + 32 * rh, k0 = j0 + 32 * kh;
+    auto step = [&](int e, const uint16_t* cur, uint16_t* nxt) {
+        const int next = lt;
+        if (e + 1 < e1) load(nxt);
+        const int i0 = 64 * (base + ct), r0 = i0 + 32 * rh, k0 = j0 + 32 * kh;
         const Sight seen = sight(r0, r0 + 31, k0, k0 + 31, a.W, a.S);
-        if (live && seen != kNone) kv_tile<D>(ct, kreg, vt, seen == kPart, i0, j, a.W, a.S, key, rh, c2, lane, dv, dk);
+        if (live && seen != kNone) kv_tile<D>(cur, kreg, vt, seen == kPart, i0, j, a.W, a.S, key, rh, c2, lane, dv, dk);
         __builtin_amdgcn_sched_barrier(0);
+        ct = next;
         wait_vmem();
         __syncthreads();
     };
@@ -394,7 +391,7 @@ window_dkdv_kernel(WindowArgs a) {
     // add the row halves (through LDS, every tile has been read)
     float* red = reinterpret_cast<float*>(tb);
     constexpr int kSlot = ND * 16 * 64;
-    static_assert(sizeof(tb) >= 4 * kSlot * 4, "reduction space");
+    static_assert(sizeof(tb) >= 2 * KB * kSlot * 4, "reduction space");
     float* mine = red + (2 * half + kh) * kSlot;
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
@@ -413,8 +410,8 @@ window_dkdv_kernel(WindowArgs a) {
         __syncthreads();
     }
     if (rh != 0 || j > last || !live) return;
-    if (pair < a.sink_pairs) {
-        float* p = a.part + ((int64_t(bk) * a.sink_pairs + pair) * a.slots + slot) * (2 * 128 * D) +
+    if (group < a.sink_groups) {
+        float* p = a.part + ((int64_t(bk) * a.sink_groups + group) * a.slots + slot) * (2 * KEYS * D) +
                    (64 * half + key) * D + 4 * h;
 #pragma unroll
         for (int x = 0; x < ND; ++x)
@@ -427,7 +424,7 @@ window_dkdv_kernel(WindowArgs a) {
                     z[e] = dv[x][4 * g + e];
                 }
                 *reinterpret_cast<f32x4*>(p + 32 * x + 8 * g) = y;
-                *reinterpret_cast<f32x4*>(p + 128 * D + 32 * x + 8 * g) = z;
+                *reinterpret_cast<f32x4*>(p + KEYS * D + 32 * x + 8 * g) = z;
             }
         return;
     }
@@ -447,36 +444,35 @@ window_dkdv_kernel(WindowArgs a) {
         }
 }
 
-// dK and dV of the sink pairs' keys: the window's sum, then the chunks in order.
-// Keys of such a pair that are no sinks have no chunks.  One thread per 4 columns.
+// dK and dV of the keys in groups with sinks: the window's sum, then the chunks in
+// order.  Blocks of 64 keys without a sink have no chunks.  A thread per 4 columns.
 constexpr int kSumThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kSumThreads) window_sinks_kernel(WindowArgs a) {
-    constexpr int C = D / 4;
-    const int per = 2 * 128 * C / kSumThreads;   // workgroups per pair
+    constexpr int C = D / 4, KEYS = 64 * kKeyBlocks<D>;
+    const int per = 2 * KEYS * C / kSumThreads;   // workgroups per group
     const int item = blockIdx.x / per;
-    const int bk = item / a.sink_pairs, pair = item % a.sink_pairs;
+    const int bk = item / a.sink_groups, group = item % a.sink_groups;
     const int t = (blockIdx.x % per) * kSumThreads + threadIdx.x;
-    const int which = t / (128 * C), key = t / C % 128, c = 4 * (t % C);
+    const int which = t / (KEYS * C), key = t / C % KEYS, c = 4 * (t % C);
     const int b = bk / a.Hkv, hk = bk % a.Hkv;
     const Sequence sq = sequence(a, b);
-    const int j = 128 * pair + key;
+    const int j = KEYS * group + key;
     if (j >= sq.n) return;
-    const QueryRange range = query_range(sq, pair, a.W);
+    const QueryRange range = query_range(sq, KEYS * group, KEYS * group + KEYS - 1, a.W);
     const int beyond = (a.Hq / a.Hkv) * (range.end - 1 - range.hi);
-    // a block of 64 keys without a sink has no chunks
     const int used = (j & ~63) < a.S ? 1 + (beyond + a.chunk - 1) / a.chunk : 1;
-    const float* p = a.part + int64_t(item) * a.slots * (2 * 128 * D) + which * (128 * D) + key * D + c;
+    const float* p = a.part + int64_t(item) * a.slots * (2 * KEYS * D) + which * (KEYS * D) + key * D + c;
     f32x4 sum = *reinterpret_cast<const f32x4*>(p);
     int s = 1;
     for (; s + 8 <= used; s += 8) {
         f32x4 x[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const f32x4*>(p + int64_t(s + u) * (2 * 128 * D));
+        for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const f32x4*>(p + int64_t(s + u) * (2 * KEYS * D));
 #pragma unroll
         for (int u = 0; u < 8; ++u) sum += x[u];
     }
-    for (; s < used; ++s) sum += *reinterpret_cast<const f32x4*>(p + int64_t(s) * (2 * 128 * D));
+    for (; s < used; ++s) sum += *reinterpret_cast<const f32x4*>(p + int64_t(s) * (2 * KEYS * D));
     const RowView& v = which == 0 ? a.dk : a.dv;
     const float f = which == 0 ? a.scale : 1.f;
     u32x2 pk;
@@ -487,35 +483,31 @@ __global__ void __launch_bounds__(kSumThreads) window_sinks_kernel(WindowArgs a)
 
 }  // namespace
 
+int window_key_group(int d) { return 64 * (d == 128 ? kKeyBlocks<128> : kKeyBlocks<64>); }
+
 hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s) {
     const bool wide = a.d == 128;
-    {
-        TraceScope _t("window_rows", s);
-        const dim3 g(unsigned(int64_t(a.B) * a.Hq * ((a.seq + 63) / 64))), t(kRowThreads);
-        if (wide) hipLaunchKernelGGL(window_rows_kernel<128>, g, t, 0, s, a);
-        else hipLaunchKernelGGL(window_rows_kernel<64>, g, t, 0, s, a);
-    }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
     {
         TraceScope _t("window_dq", s);
         const dim3 g(unsigned(int64_t(a.B) * a.Hq * ((a.seq + kDqRows - 1) / kDqRows))), t(kDqThreads);
         if (wide) hipLaunchKernelGGL(window_dq_kernel<128>, g, t, 0, s, a);
         else hipLaunchKernelGGL(window_dq_kernel<64>, g, t, 0, s, a);
     }
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t bk = int64_t(a.B) * a.Hkv;
     {
         TraceScope _t("window_dkdv", s);
-        const int64_t bk = int64_t(a.B) * a.Hkv;
-        const int64_t extra = bk * a.sink_pairs * std::max(0, a.slots - 1);
-        const dim3 g(unsigned(extra + bk * ((a.seq + 127) / 128))), t(kKvThreads);
-        if (wide) hipLaunchKernelGGL(window_dkdv_kernel<128>, g, t, 0, s, a);
-        else hipLaunchKernelGGL(window_dkdv_kernel<64>, g, t, 0, s, a);
+        const int keys = window_key_group(a.d);
+        const int64_t extra = bk * a.sink_groups * std::max(0, a.slots - 1);
+        const dim3 g(unsigned(extra + bk * ((a.seq + keys - 1) / keys)));
+        if (wide) hipLaunchKernelGGL(window_dkdv_kernel<128>, g, dim3(256 * kKeyBlocks<128>), 0, s, a);
+        else hipLaunchKernelGGL(window_dkdv_kernel<64>, g, dim3(256 * kKeyBlocks<64>), 0, s, a);
     }
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.sink_pairs > 0) {
+    if (a.sink_groups > 0) {
         TraceScope _t("window_sinks", s);
-        const dim3 g(unsigned(int64_t(a.B) * a.Hkv * a.sink_pairs * (2 * 128 * a.d / 4 / kSumThreads))), t(kSumThreads);
+        const dim3 g(unsigned(bk * a.sink_groups * (2 * window_key_group(a.d) * a.d / 4 / kSumThreads))), t(kSumThreads);
         if (wide) hipLaunchKernelGGL(window_sinks_kernel<128>, g, t, 0, s, a);
         else hipLaunchKernelGGL(window_sinks_kernel<64>, g, t, 0, s, a);
     }
