@@ -988,9 +988,10 @@ msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q,
     a.Hq = heads_q;
     a.T = tokens;
     const int64_t P = (int64_t(tokens) + 2 * kPage - 2) / kPage;   // the most pages that tokens in a row touch
-    if (B * P > kMaxGroups) return fail(MSPARSE_ERR_UNSUPPORTED, "%lld pages in one call", (long long)(B * P));
+    if (B * P > kMaxGroups / 2) return fail(MSPARSE_ERR_UNSUPPORTED, "%lld pages in one call", (long long)(B * P));
     a.P = int32_t(P);
-    a.split = append_split(B * P, q ? heads_q : cache->heads_kv);
+    a.kv_shares = append_shares(B * P, cache->heads_kv);
+    a.q_shares = q && B * P <= kAppendApart ? append_shares(B * P, heads_q) : 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return check_hip(launch_cache_append(a, s), s, "cache append");
 }

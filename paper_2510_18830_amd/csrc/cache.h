@@ -44,13 +44,19 @@ struct AppendArgs {
     const int32_t* counts;                    // [B] or NULL: T
     int32_t Hq, T;
     int32_t P;                                // pages that T tokens can touch
-    int32_t split;                            // workgroups that share a page's heads
+    // workgroups that share a page's KV heads, and its query heads (0: the same ones)
+    int32_t kv_shares, q_shares;
 };
-// Workgroups that share a page's heads: as many as bring the grid to about four
-// a CU, each head in one of them.
-inline int32_t append_split(int64_t pages, int64_t heads) {
-    return int32_t(std::max<int64_t>(1, std::min<int64_t>(heads, 1024 / pages)));
+// Workgroups that share a page's `heads`: as many as bring their grid to about one
+// a CU, a head in one of them.
+inline int32_t append_shares(int64_t pages, int64_t heads) {
+    return int32_t(std::max<int64_t>(1, std::min<int64_t>(heads, 256 / pages)));
 }
+// Pages up to which the queries have workgroups of their own: few pages wait for
+// latencies (6 ragged chunks of 501 tokens, 54 pages: 7.6 us, 9.6 with the queries
+// behind the keys; 64 pages of one token each: 8.3, 7.9), many for memory, where the
+// two kinds of work mix better in one (128K tokens, 2049 pages: 457, 431).
+constexpr int64_t kAppendApart = 512;
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 
 struct CacheAttnArgs {
