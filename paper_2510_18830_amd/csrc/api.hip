@@ -838,17 +838,16 @@ static WindowArgs window_args(const msparse_window* w, const int32_t* starts) {
     return a;
 }
 
-// lse log2(e) and Delta of every row, the sink keys' partial gradients.
+// lse log2(e) and Delta of every row, the keys' partial gradients.
 static size_t carve_window_bwd(WindowArgs* a, char* base) {
     const int keys = window_key_group(a->d);
-    const SinkPlan p = sink_plan(a->B, a->Hkv, a->Hq / a->Hkv, a->seq, a->W, a->S, keys);
-    a->sink_groups = p.groups;
-    a->slots = p.slots;
-    a->chunk = p.chunk;
+    const KeyPlan& p = a->plan = key_plan(a->B, a->Hkv, a->Hq / a->Hkv, a->seq, a->W, a->S, keys,
+                                          window_key_resident(a->d));
+    const int64_t slots = int64_t(p.part_groups) * p.near_slots + int64_t(p.sink_groups) * p.far_slots;
     a->rows_pad = a->tokens > 0 ? padded_rows(a->tokens) + 64 * (int64_t(a->B) + 1) : a->B * padded_rows(a->seq);
     Carve c{base};
     a->rows = c.take<float>(size_t(2) * a->Hq * a->rows_pad);
-    a->part = c.take<float>(size_t(a->B) * a->Hkv * p.groups * p.slots * 2 * keys * a->d);
+    a->part = c.take<float>(size_t(a->B) * a->Hkv * slots * 2 * keys * a->d);
     return c.off;
 }
 

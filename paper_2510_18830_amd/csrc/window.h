@@ -27,6 +27,43 @@ struct RowView {
     int64_t batch, head, token;
 };
 
+// The key-major backward's workgroups for a group of keys: near_slots for the query
+// tiles of its window (every head of the KV group: near_chunk of them each), and for
+// one with sinks far_slots for the tiles beyond (far_chunk each, no more than a
+// window's: 8 heads x 2048, window 256, sinks 4, head dim 128: dK / dV 34 us with 16
+// tiles each, 24 with 6).  A group with more than one leaves partial sums: those with
+// sinks, or, where windows are cut too, all of them.  Windows are cut, into 8 tiles at
+// least, while all workgroups are resident at once (`resident`), which pays for the
+// sums: dK / dV and sums 36 -> 30 us for 8 x 1024 causal (64 groups), 58 -> 48 for 8 x
+// 2048 (128); beyond that it costs: 16 x 2048 (256 groups, cut in two) 61 -> 85.
+struct KeyPlan {
+    int32_t near_slots, near_chunk, sink_groups, far_slots, far_chunk, part_groups;
+};
+inline KeyPlan key_plan(int64_t B, int64_t Hkv, int64_t G, int64_t seq, int64_t W, int64_t S, int64_t keys,
+                        int64_t resident) {
+    KeyPlan p{1, 1, 0, 0, 1, 0};
+    if (seq <= 0) return p;
+    const int64_t tiles = (seq + 63) / 64, groups = (seq + keys - 1) / keys, bk = B * Hkv;
+    const int64_t walk = G * std::min(tiles, (keys + W - 2) / 64 + 1);   // query tiles of a group's window
+    const int64_t first = W / 64;             // the rows of tiles before are inside the window of key 0
+    if (S > 0 && W < seq && first < tiles) {
+        p.sink_groups = p.part_groups = int32_t((std::min(S, seq) + keys - 1) / keys);
+        const int64_t beyond = G * (tiles - first);      // query tiles beyond a group's window, at most
+        const int64_t items = std::max<int64_t>(1, std::min<int64_t>(256, 1024 / (bk * p.sink_groups)));
+        p.far_chunk = int32_t(std::max(std::min<int64_t>(16, walk), (beyond + items - 1) / items));
+        p.far_slots = int32_t((beyond + p.far_chunk - 1) / p.far_chunk);
+    }
+    const int64_t room = resident - bk * p.sink_groups * p.far_slots;
+    const int64_t cuts = std::min(room / (bk * groups), walk / 8);
+    p.near_chunk = int32_t(walk);
+    if (cuts > 1) {
+        p.near_chunk = int32_t((walk + cuts - 1) / cuts);
+        p.near_slots = int32_t((walk + p.near_chunk - 1) / p.near_chunk);
+        p.part_groups = int32_t(groups);
+    }
+    return p;
+}
+
 struct WindowArgs {
     RowView q, k, v, out, dout, dq, dk, dv;
     float* lse;            // [batch, Hq, seq], packed: [Hq, tokens]
@@ -38,10 +75,8 @@ struct WindowArgs {
     // backward workspace
     float* rows;           // [Hq][2][rows_pad]: lse log2(e) and Delta of every row, sequences from a multiple of 64 on
     int64_t rows_pad;
-    float* part;           // sink keys' partial gradients: [B Hkv sink_groups][slots][2][keys of a group][d]
-    int32_t sink_groups;   // groups of key blocks that hold sinks
-    int32_t slots;         // partials of such a group: its window's, then `slots - 1` chunks of the rows beyond
-    int32_t chunk;         // query tiles of a chunk
+    float* part;           // partial dK, dV: [B Hkv part_groups][near_slots], then [B Hkv sink_groups][far_slots],
+    KeyPlan plan;         //   each [2][keys of a group][d]
 };
 
 // Where sequence b lies: `row` its first row (packed), n its length.  Starts out
@@ -140,24 +175,8 @@ __device__ __forceinline__ void window_tile_of(const WindowArgs& a, int64_t t, i
 
 hipError_t launch_window_fwd(const WindowArgs& a, hipStream_t s);
 hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s);
-
-// Keys that a workgroup of the key-major backward takes.
+// Keys that a workgroup of the key-major backward takes, and how many of them run at once.
 int window_key_group(int d);
-// Sizes of the backward's partial gradients of the sink keys (0 groups: none).
-struct SinkPlan {
-    int32_t groups, slots, chunk;
-};
-inline SinkPlan sink_plan(int64_t B, int64_t Hkv, int64_t G, int64_t seq, int64_t W, int64_t S, int64_t keys) {
-    SinkPlan p{0, 0, 0};
-    const int64_t tiles = (seq + 63) / 64;
-    const int64_t first = W / 64;             // the rows of tiles before are inside the window of key 0
-    if (S <= 0 || W >= seq || first >= tiles) return p;
-    p.groups = int32_t((std::min(S, seq) + keys - 1) / keys);
-    const int64_t beyond = G * (tiles - first);      // query tiles beyond a group's window, at most
-    const int64_t items = std::max<int64_t>(1, std::min<int64_t>(256, 1024 / (B * Hkv * p.groups)));
-    p.chunk = int32_t(std::max<int64_t>(16, (beyond + items - 1) / items));
-    p.slots = int32_t(1 + (beyond + p.chunk - 1) / p.chunk);
-    return p;
-}
+int window_key_resident(int d);
 
 }  // namespace msparse

@@ -12,8 +12,8 @@
 //           query tiles of the keys' window.  Sink keys are seen by every later
 //           row too: a walk over the whole sequence for a single group, so those
 //           rows are cut into chunks, a workgroup each, and the chunks' sums go
-//           to the workspace (fp32)
-//   sinks   adds them up, chunks in order.
+//           to the workspace (fp32); on small grids the windows' walks are too
+//   sums    adds them up, chunks in order.
 // All products take bf16 operands with fp32 accumulation: P and dZ are rounded to
 // the inputs' type (8 significant bits), each term of the sums independently.
 #include "window.h"
@@ -25,6 +25,14 @@ namespace {
 
 // ------------------------------------------------------------------ dQ
 constexpr int kDqThreads = 256, kDqRows = 128;
+// Grids of 128-row workgroups up to which the split kernel runs (both in us, 128
+// rows -> split; heads x tokens, window):
+//   d 128   28 (4 x 777, 256): 29 -> 17.5; 128: 41 -> 36 (4 x 4096, 1024), 57 -> 45 (8 x
+//           2048, all); 192: 31 -> 42 (12 x 2048, 512); 256: 33 -> 42
+//   d 64    28: 18 -> 13; 128: 30 -> 23.5, 40 -> 27; 256: 24 -> 21 (16 x 2048, 512), 41 -> 36
+//           (16 x 2048, all); 384: 29.8 -> 29.4; 512: 33 -> 35, 70.5 -> 75 (8 x 8192, 2048)
+template <int D>
+constexpr int64_t kSplitGrid = D == 128 ? 128 : 256;
 
 template <int D>
 struct WinDq {
@@ -88,10 +96,58 @@ __device__ __forceinline__ void dq_tile(const uint16_t* kt, const uint16_t* vt, 
     }
 }
 
+// Row i's operands, lse log2(e) and Delta; `first` waves leave the latter two for the
+// key-major pass.
+template <int D>
+__device__ __forceinline__ void open_rows(const WindowArgs& a, const Sequence& sq, int hq, int i, int h, bool first,
+                                          WinDq<D>& st) {
+    constexpr int KD = WinDq<D>::KD;
+    const bool real = i < sq.n;
+    const int ic = min(i, sq.n - 1);
+    const uint16_t* qp = head_rows(a, a.q, sq, hq) + ic * a.q.token;
+    const uint16_t* gp = head_rows(a, a.dout, sq, hq) + ic * a.dout.token;
+    const uint16_t* op = head_rows(a, a.out, sq, hq) + ic * a.out.token;
+    u32x4 o[KD];
+#pragma unroll
+    for (int s = 0; s < KD; ++s) {
+        st.q[s] = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * h);
+        st.g[s] = *reinterpret_cast<const u32x4*>(gp + 16 * s + 8 * h);
+        o[s] = *reinterpret_cast<const u32x4*>(op + 16 * s + 8 * h);
+    }
+    st.lse2 = a.lse[lse_row(a, sq, hq) + ic] * kLog2e;
+    float acc = 0.f;
+#pragma unroll
+    for (int s = 0; s < KD; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            acc += bf16_lo(st.g[s][e]) * bf16_lo(o[s][e]) + bf16_hi(st.g[s][e]) * bf16_hi(o[s][e]);
+    st.dlt = half_swap_sum(acc);
+    if (first && h == 0 && i < padded_rows(sq.n)) {
+        float* rv = a.rows + int64_t(2 * hq) * a.rows_pad + value_row(a, sq) + i;
+        rv[0] = real ? st.lse2 : INFINITY;   // a row past the end: P = 0
+        rv[a.rows_pad] = real ? st.dlt : 0.f;
+    }
+#pragma unroll
+    for (int x = 0; x < WinDq<D>::ND; ++x) st.acc[x] = f32x16{};
+}
+template <int D>
+__device__ __forceinline__ void store_dq(const WindowArgs& a, const Sequence& sq, int hq, int i, int h,
+                                         const WinDq<D>& st) {
+    uint16_t* dq = head_rows(a, a.dq, sq, hq) + i * a.dq.token;
+#pragma unroll
+    for (int x = 0; x < WinDq<D>::ND; ++x)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            u32x2 pk;
+            pk.x = pack_bf16x2(st.acc[x][4 * g + 0] * a.scale, st.acc[x][4 * g + 1] * a.scale);
+            pk.y = pack_bf16x2(st.acc[x][4 * g + 2] * a.scale, st.acc[x][4 * g + 3] * a.scale);
+            *reinterpret_cast<u32x2*>(dq + 32 * x + 8 * g + 4 * h) = pk;
+        }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kDqThreads)
     __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) window_dq_kernel(WindowArgs a) {
-    constexpr int KD = WinDq<D>::KD, ND = WinDq<D>::ND;
     constexpr int TE = DmaTile<D, kDualPad>::kElems;
     __shared__ uint16_t k0s[TE], v0s[TE], k1s[TE], v1s[TE];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
@@ -105,37 +161,9 @@ __global__ void __launch_bounds__(kDqThreads)
     const int hk = hq / (a.Hq / a.Hkv);
     const uint16_t* kp = head_rows(a, a.k, sq, hk);
     const uint16_t* vp = head_rows(a, a.v, sq, hk);
-    const int w0 = i0 + 32 * w, i = w0 + l32, ic = min(i, last);
+    const int w0 = i0 + 32 * w, i = w0 + l32;
     WinDq<D> st;
-    {
-        const uint16_t* qp = head_rows(a, a.q, sq, hq) + ic * a.q.token;
-        const uint16_t* gp = head_rows(a, a.dout, sq, hq) + ic * a.dout.token;
-        const uint16_t* op = head_rows(a, a.out, sq, hq) + ic * a.out.token;
-        u32x4 o[KD];
-#pragma unroll
-        for (int s = 0; s < KD; ++s) {
-            st.q[s] = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * h);
-            st.g[s] = *reinterpret_cast<const u32x4*>(gp + 16 * s + 8 * h);
-            o[s] = *reinterpret_cast<const u32x4*>(op + 16 * s + 8 * h);
-        }
-        // this row's lse log2(e) and Delta, for the key-major pass too
-        const bool real = i <= last;
-        st.lse2 = a.lse[lse_row(a, sq, hq) + ic] * kLog2e;
-        float acc = 0.f;
-#pragma unroll
-        for (int s = 0; s < KD; ++s)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                acc += bf16_lo(st.g[s][e]) * bf16_lo(o[s][e]) + bf16_hi(st.g[s][e]) * bf16_hi(o[s][e]);
-        st.dlt = half_swap_sum(acc);
-        if (h == 0 && i < padded_rows(sq.n)) {
-            float* rv = a.rows + int64_t(2 * hq) * a.rows_pad + value_row(a, sq) + i;
-            rv[0] = real ? st.lse2 : INFINITY;   // a row past the end: P = 0
-            rv[a.rows_pad] = real ? st.dlt : 0.f;
-        }
-    }
-#pragma unroll
-    for (int x = 0; x < ND; ++x) st.acc[x] = f32x16{};
+    open_rows(a, sq, hq, i, h, true, st);
     const float c2 = a.scale * kLog2e;
     const KeyWalk walk = key_walk(i0, min(i0 + kDqRows - 1, last), a.W, a.S);
     auto load = [&](uint16_t* kt, uint16_t* vt, int t) {
@@ -159,17 +187,67 @@ __global__ void __launch_bounds__(kDqThreads)
         step(t, k0s, v0s, k1s, v1s);
         if (t + 1 < walk.tiles) step(t + 1, k1s, v1s, k0s, v0s);
     }
-    if (i > last) return;
-    uint16_t* dq = head_rows(a, a.dq, sq, hq) + i * a.dq.token;
+    if (i <= last) store_dq(a, sq, hq, i, h, st);
+}
+
+// Small grids: 64 rows per workgroup, two halves on alternate tiles (as the
+// forward's); the second half's sum is added to the first's.
+template <int D>
+__global__ void __launch_bounds__(kDqThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+window_dq_split_kernel(WindowArgs a) {
+    constexpr int ND = WinDq<D>::ND;
+    constexpr int TE = DmaTile<D, kDualPad>::kElems;
+    __shared__ __attribute__((aligned(16))) uint16_t kb[2][2][TE], vb[2][2][TE];   // [half][parity]
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), half = w >> 1, rh = w & 1;
+    int b, hq, tile;
+    window_tile_of(a, blockIdx.x, (a.seq + 63) >> 6, b, hq, tile);
+    const Sequence sq = sequence(a, b);
+    const int i0 = 64 * tile;
+    if (i0 >= sq.n) return;
+    const int last = sq.n - 1;
+    const int hk = hq / (a.Hq / a.Hkv);
+    const uint16_t* kp = head_rows(a, a.k, sq, hk);
+    const uint16_t* vp = head_rows(a, a.v, sq, hk);
+    const int w0 = i0 + 32 * rh, i = w0 + l32;
+    const float c2 = a.scale * kLog2e;
+    const KeyWalk walk = key_walk(i0, min(i0 + 63, last), a.W, a.S);
+    const int steps = (walk.tiles + 1) >> 1;
+    auto load = [&](int t) {   // tile 2 t + half
+        const int row0 = 64 * walk.tile(2 * t + half);
+        dma_sequence<D, kDualPad, 2>(kb[half][t & 1], kp, a.k.token, row0, last, rh, lane);
+        dma_sequence<D, kDualPad, 2>(vb[half][t & 1], vp, a.v.token, row0, last, rh, lane);
+    };
+    if (half < walk.tiles) load(0);
+    WinDq<D> st;
+    open_rows(a, sq, hq, i, h, half == 0, st);
+    for (int t = 0; t < steps; ++t) {
+        wait_vmem();
+        __syncthreads();   // tile t has landed, and the buffers of tile t - 1 are read
+        if (2 * (t + 1) + half < walk.tiles) load(t + 1);
+        if (2 * t + half < walk.tiles) {
+            const int j0 = 64 * walk.tile(2 * t + half);
+            const Sight seen = sight(w0, w0 + 31, j0, j0 + 63, a.W, a.S);
+            if (seen != kNone && w0 <= last)
+                dq_tile<D>(kb[half][t & 1], vb[half][t & 1], seen == kPart, i, j0, a.W, a.S, st, lane, c2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();   // every tile has been read
+    float* x1 = reinterpret_cast<float*>(&kb[0][0][0]) + rh * (ND * 16 * 64);
+    static_assert(sizeof(kb) >= 2 * ND * 16 * 64 * 4, "exchange space");
+    if (half == 1)
+#pragma unroll
+        for (int x = 0; x < ND; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x1[(x * 16 + r) * 64 + lane] = st.acc[x][r];
+    __syncthreads();
+    if (half == 1 || i > last) return;
 #pragma unroll
     for (int x = 0; x < ND; ++x)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            u32x2 pk;
-            pk.x = pack_bf16x2(st.acc[x][4 * g + 0] * a.scale, st.acc[x][4 * g + 1] * a.scale);
-            pk.y = pack_bf16x2(st.acc[x][4 * g + 2] * a.scale, st.acc[x][4 * g + 3] * a.scale);
-            *reinterpret_cast<u32x2*>(dq + 32 * x + 8 * g + 4 * h) = pk;
-        }
+        for (int r = 0; r < 16; ++r) st.acc[x][r] += x1[(x * 16 + r) * 64 + lane];
+    store_dq(a, sq, hq, i, h, st);
 }
 
 // ------------------------------------------------------------------ dK / dV
@@ -288,8 +366,8 @@ __device__ __forceinline__ QueryRange query_range(const Sequence& sq, int j0, in
     return r;
 }
 
-// Workgroups 0 .. B Hkv sink_groups (slots - 1) - 1: the chunks of the sink keys'
-// rows beyond the window; the rest: groups of kKeyBlocks key blocks.
+// Workgroups 0 .. B Hkv sink_groups far_slots - 1: the chunks of the sink keys' rows
+// beyond the window; the rest: groups of kKeyBlocks key blocks, near_slots for each.
 template <int D>
 __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
     __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3))) window_dkdv_kernel(WindowArgs a) {
@@ -302,36 +380,27 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
     const int half = w >> 2, kh = (w >> 1) & 1, rh = w & 1;
     const int BK = a.B * a.Hkv, G = a.Hq / a.Hkv;
     const int groups = (a.seq + KEYS - 1) / KEYS;
-    const int64_t extra = int64_t(BK) * a.sink_groups * (a.slots - 1);
-    int bk, group, slot;      // slot: 0 the window, 1 .. a chunk beyond
-    if (int64_t(blockIdx.x) < extra) {
-        bk = int(blockIdx.x / (a.sink_groups * (a.slots - 1)));
-        const int r = int(blockIdx.x % (a.sink_groups * (a.slots - 1)));
-        group = r / (a.slots - 1);
-        slot = 1 + r % (a.slots - 1);
-    } else {
-        const int64_t u = xcd_chunk(blockIdx.x - extra, int64_t(BK) * groups);
-        bk = int(u / groups);
-        group = int(u % groups);
-        slot = 0;
-    }
+    const KeyPlan& p = a.plan;
+    const int64_t extra = int64_t(BK) * p.sink_groups * p.far_slots;
+    const bool far = int64_t(blockIdx.x) < extra;
+    const int64_t u = far ? blockIdx.x : xcd_chunk(blockIdx.x - extra, int64_t(BK) * groups * p.near_slots);
+    const int slot = int(u % (far ? p.far_slots : p.near_slots));
+    const int item = int(u / (far ? p.far_slots : p.near_slots));
+    const int group = item % (far ? p.sink_groups : groups), bk = item / (far ? p.sink_groups : groups);
     const int b = bk / a.Hkv, hk = bk % a.Hkv;
     const Sequence sq = sequence(a, b);
     if (KEYS * group >= sq.n) return;
     const int last = sq.n - 1;
     const QueryRange range = query_range(sq, KEYS * group, KEYS * group + KEYS - 1, a.W);
     // entries [e0, e1) of the walk: head g = e / width, tile base + e % width
-    int base = range.lo, width = range.hi - range.lo + 1, e0 = 0, e1 = G * width;
-    if (slot > 0) {
-        base = range.hi + 1;
-        width = range.end - base;
-        e0 = (slot - 1) * a.chunk;
-        e1 = min(e0 + a.chunk, G * width);
-        if (e0 >= e1) return;
-    }
+    const int base = far ? range.hi + 1 : range.lo;
+    const int width = far ? range.end - base : range.hi - range.lo + 1;
+    const int chunk = far ? p.far_chunk : p.near_chunk;
+    const int e0 = slot * chunk, e1 = min(e0 + chunk, G * width);
+    if (e0 >= e1) return;
     const int key = 32 * kh + l32;
     const int j0 = KEYS * group + 64 * half, j = j0 + key;
-    const bool live = j0 <= last && (slot == 0 || j0 < a.S);
+    const bool live = j0 <= last && (!far || j0 < a.S);
     const uint16_t* kp = head_rows(a, a.k, sq, hk);
     u32x4 kreg[KD];
 #pragma unroll
@@ -407,9 +476,10 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
         __syncthreads();
     }
     if (rh != 0 || j > last || !live) return;
-    if (group < a.sink_groups) {
-        float* p = a.part + ((int64_t(bk) * a.sink_groups + group) * a.slots + slot) * (2 * KEYS * D) +
-                   (64 * half + key) * D + 4 * h;
+    if (far || group < p.part_groups) {
+        const int64_t at = far ? int64_t(BK) * p.part_groups * p.near_slots + u
+                               : (int64_t(bk) * p.part_groups + group) * p.near_slots + slot;
+        float* o = a.part + at * (2 * KEYS * D) + (64 * half + key) * D + 4 * h;
 #pragma unroll
         for (int x = 0; x < ND; ++x)
 #pragma unroll
@@ -420,8 +490,8 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
                     y[e] = dk[x][4 * g + e];
                     z[e] = dv[x][4 * g + e];
                 }
-                *reinterpret_cast<f32x4*>(p + 32 * x + 8 * g) = y;
-                *reinterpret_cast<f32x4*>(p + KEYS * D + 32 * x + 8 * g) = z;
+                *reinterpret_cast<f32x4*>(o + 32 * x + 8 * g) = y;
+                *reinterpret_cast<f32x4*>(o + KEYS * D + 32 * x + 8 * g) = z;
             }
         return;
     }
@@ -441,35 +511,46 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
         }
 }
 
-// dK and dV of the keys in groups with sinks: the window's sum, then the chunks in
-// order.  Blocks of 64 keys without a sink have no chunks.  A thread per 4 columns.
+// dK and dV of the keys of part_groups: the sums of their window's chunks, then, for
+// blocks of 64 keys with a sink, those of the rows beyond, in order.  A thread per 4
+// columns.
 constexpr int kSumThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(kSumThreads) window_sinks_kernel(WindowArgs a) {
+__device__ __forceinline__ void add_slots(f32x4& sum, const float* p, int n) {
+    constexpr int64_t kStep = 2 * 64 * kKeyBlocks<D> * D;
+    int s = 0;
+    for (; s + 8 <= n; s += 8) {
+        f32x4 x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const f32x4*>(p + (s + u) * kStep);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum += x[u];
+    }
+    for (; s < n; ++s) sum += *reinterpret_cast<const f32x4*>(p + s * kStep);
+}
+template <int D>
+__global__ void __launch_bounds__(kSumThreads) window_sums_kernel(WindowArgs a) {
     constexpr int C = D / 4, KEYS = 64 * kKeyBlocks<D>;
+    const KeyPlan& p = a.plan;
     const int per = 2 * KEYS * C / kSumThreads;   // workgroups per group
     const int item = blockIdx.x / per;
-    const int bk = item / a.sink_groups, group = item % a.sink_groups;
+    const int bk = item / p.part_groups, group = item % p.part_groups;
     const int t = (blockIdx.x % per) * kSumThreads + threadIdx.x;
     const int which = t / (KEYS * C), key = t / C % KEYS, c = 4 * (t % C);
-    const int b = bk / a.Hkv, hk = bk % a.Hkv;
+    const int b = bk / a.Hkv, hk = bk % a.Hkv, G = a.Hq / a.Hkv;
     const Sequence sq = sequence(a, b);
     const int j = KEYS * group + key;
     if (j >= sq.n) return;
     const QueryRange range = query_range(sq, KEYS * group, KEYS * group + KEYS - 1, a.W);
-    const int beyond = (a.Hq / a.Hkv) * (range.end - 1 - range.hi);
-    const int used = (j & ~63) < a.S ? 1 + (beyond + a.chunk - 1) / a.chunk : 1;
-    const float* p = a.part + int64_t(item) * a.slots * (2 * KEYS * D) + which * (KEYS * D) + key * D + c;
-    f32x4 sum = *reinterpret_cast<const f32x4*>(p);
-    int s = 1;
-    for (; s + 8 <= used; s += 8) {
-        f32x4 x[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const f32x4*>(p + int64_t(s + u) * (2 * KEYS * D));
-#pragma unroll
-        for (int u = 0; u < 8; ++u) sum += x[u];
-    }
-    for (; s < used; ++s) sum += *reinterpret_cast<const f32x4*>(p + int64_t(s) * (2 * KEYS * D));
+    const float* part = a.part + which * (KEYS * D) + key * D + c;
+    f32x4 sum = f32x4{};
+    add_slots<D>(sum, part + int64_t(item) * p.near_slots * (2 * KEYS * D),
+                 (G * (range.hi - range.lo + 1) + p.near_chunk - 1) / p.near_chunk);
+    if ((j & ~63) < a.S && group < p.sink_groups)
+        add_slots<D>(sum,
+                     part + (int64_t(a.B) * a.Hkv * p.part_groups * p.near_slots +
+                             (int64_t(bk) * p.sink_groups + group) * p.far_slots) * (2 * KEYS * D),
+                     (G * (range.end - 1 - range.hi) + p.far_chunk - 1) / p.far_chunk);
     const RowView& v = which == 0 ? a.dk : a.dv;
     const float f = which == 0 ? a.scale : 1.f;
     u32x2 pk;
@@ -480,14 +561,19 @@ __global__ void __launch_bounds__(kSumThreads) window_sinks_kernel(WindowArgs a)
 
 }  // namespace
 
+int window_key_resident(int d) { return d == 128 ? 256 : 768; }   // one or three a CU
 int window_key_group(int d) { return 64 * (d == 128 ? kKeyBlocks<128> : kKeyBlocks<64>); }
 
 hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s) {
     const bool wide = a.d == 128;
     {
         TraceScope _t("window_dq", s);
-        const dim3 g(unsigned(int64_t(a.B) * a.Hq * ((a.seq + kDqRows - 1) / kDqRows))), t(kDqThreads);
-        if (wide) hipLaunchKernelGGL(window_dq_kernel<128>, g, t, 0, s, a);
+        const int64_t heads = int64_t(a.B) * a.Hq, grid = heads * ((a.seq + kDqRows - 1) / kDqRows);
+        const bool split = grid <= (wide ? kSplitGrid<128> : kSplitGrid<64>);
+        const dim3 g(unsigned(split ? heads * ((a.seq + 63) / 64) : grid)), t(kDqThreads);
+        if (split && wide) hipLaunchKernelGGL(window_dq_split_kernel<128>, g, t, 0, s, a);
+        else if (split) hipLaunchKernelGGL(window_dq_split_kernel<64>, g, t, 0, s, a);
+        else if (wide) hipLaunchKernelGGL(window_dq_kernel<128>, g, t, 0, s, a);
         else hipLaunchKernelGGL(window_dq_kernel<64>, g, t, 0, s, a);
     }
     hipError_t e = hipGetLastError();
@@ -496,17 +582,17 @@ hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s) {
     {
         TraceScope _t("window_dkdv", s);
         const int keys = window_key_group(a.d);
-        const int64_t extra = bk * a.sink_groups * std::max(0, a.slots - 1);
-        const dim3 g(unsigned(extra + bk * ((a.seq + keys - 1) / keys)));
+        const int64_t groups = (a.seq + keys - 1) / keys;
+        const dim3 g(unsigned(bk * (a.plan.sink_groups * int64_t(a.plan.far_slots) + groups * a.plan.near_slots)));
         if (wide) hipLaunchKernelGGL(window_dkdv_kernel<128>, g, dim3(256 * kKeyBlocks<128>), 0, s, a);
         else hipLaunchKernelGGL(window_dkdv_kernel<64>, g, dim3(256 * kKeyBlocks<64>), 0, s, a);
     }
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.sink_groups > 0) {
-        TraceScope _t("window_sinks", s);
-        const dim3 g(unsigned(bk * a.sink_groups * (2 * window_key_group(a.d) * a.d / 4 / kSumThreads))), t(kSumThreads);
-        if (wide) hipLaunchKernelGGL(window_sinks_kernel<128>, g, t, 0, s, a);
-        else hipLaunchKernelGGL(window_sinks_kernel<64>, g, t, 0, s, a);
+    if (a.plan.part_groups > 0) {
+        TraceScope _t("window_sums", s);
+        const dim3 g(unsigned(bk * a.plan.part_groups * (2 * window_key_group(a.d) * a.d / 4 / kSumThreads))), t(kSumThreads);
+        if (wide) hipLaunchKernelGGL(window_sums_kernel<128>, g, t, 0, s, a);
+        else hipLaunchKernelGGL(window_sums_kernel<64>, g, t, 0, s, a);
     }
     return hipGetLastError();
 }

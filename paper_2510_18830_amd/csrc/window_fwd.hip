@@ -1,4 +1,7 @@
-// Forward of the attention with a sliding window and sinks.
+// Forward of the attention with a sliding window and sinks.  Bound by the matrix
+// cores and the softmax terms beside them, at long lengths by the power they take:
+// 16 over 2 heads x 32K, window 4096, 64 sinks, head dim 128: 1.09 ms, 960 TFLOP/s on
+// the visible pairs.
 //
 // One workgroup of four wavefronts per (sequence, query head, 128 rows), 32 rows
 // a wave.  Key tiles of 64 are staged by direct global->LDS loads, the next one
@@ -20,6 +23,14 @@ namespace {
 constexpr float kSlack = 8.f;        // log2 units
 constexpr int kFwdRows = 128;        // query rows per workgroup
 constexpr int kFwdThreads = 256;
+// Grids of 128-row workgroups up to which the split kernel runs instead (both in us,
+// 128 rows -> split; heads x tokens, window):
+//   d 128   28 (4 x 777, 256): 16.7 -> 11.8; 128: 33.2 -> 25.9 (4 x 4096, 1024), 46.6 ->
+//           35.9 (8 x 2048, all); 192: 23.9 -> 31.8 (12 x 2048, 512); 256: 25.2 -> 32.8
+//   d 64    28: 12.7 -> 8.0; 128: 24.3 -> 15.5, 34.8 -> 22.2; 256: 18.2 -> 14.3 (16 x
+//           2048, 512); 384: 24.0 -> 22.8; 512: 24.1 -> 25.9, 57.8 -> 62.6 (8 x 8192, 2048)
+template <int D>
+constexpr int64_t kSplitGrid = D == 128 ? 128 : 384;
 
 template <int D>
 struct WinRows {
@@ -136,6 +147,25 @@ __device__ __forceinline__ void win_tile(const uint16_t* kt, const uint16_t* vt,
     }
 }
 
+// out and lse of this lane's row i
+template <int D>
+__device__ __forceinline__ void store_rows(const WindowArgs& a, const WinRows<D>& st, const Sequence& sq, int hq, int i,
+                                           int h) {
+    constexpr int ND = WinRows<D>::ND;
+    const float inv = 1.f / st.lr;
+    uint16_t* op = head_rows(a, a.out, sq, hq) + i * a.out.token;
+#pragma unroll
+    for (int x = 0; x < ND; ++x)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            u32x2 pk;
+            pk.x = pack_bf16x2(st.o[x][4 * g + 0] * inv, st.o[x][4 * g + 1] * inv);
+            pk.y = pack_bf16x2(st.o[x][4 * g + 2] * inv, st.o[x][4 * g + 3] * inv);
+            *reinterpret_cast<u32x2*>(op + 32 * x + 8 * g + 4 * h) = pk;
+        }
+    if (h == 0) a.lse[lse_row(a, sq, hq) + i] = (st.m + fast_log2(st.l)) * kLn2;
+}
+
 // Two waves per SIMD at head dim 128 (256 registers), three at 64.
 template <int D>
 __global__ void __launch_bounds__(kFwdThreads) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 3 : 2)))
@@ -186,28 +216,97 @@ window_fwd_kernel(WindowArgs a) {
         step(t, k0s, v0s, k1s, v1s);
         if (t + 1 < walk.tiles) step(t + 1, k1s, v1s, k0s, v0s);
     }
-    if (i > last) return;
-    const float inv = 1.f / st.lr;
-    uint16_t* op = head_rows(a, a.out, sq, hq) + i * a.out.token;
+    if (i <= last) store_rows(a, st, sq, hq, i, h);
+}
+
+// Small grids: 64 rows per workgroup, waves (row half, key half); the key halves walk
+// alternate tiles with tile buffers of their own and are joined at the end, the
+// second's (m, sums, O) into the first's.  A row tile's walk is bound by latency:
+// half of it by half the rows each is faster while twice the workgroups, of which one
+// fits a CU where two do otherwise (two where three do, at head dim 64), are resident
+// at once.
+template <int D>
+__global__ void __launch_bounds__(kFwdThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+window_fwd_split_kernel(WindowArgs a) {
+    constexpr int KD = WinRows<D>::KD, ND = WinRows<D>::ND;
+    constexpr int KE = DmaTile<D, kRowPad>::kElems, VE = DmaTile<D, kTrPad>::kElems;
+    __shared__ __attribute__((aligned(16))) uint16_t kb[2][2][KE], vb[2][2][VE];   // [half][parity]
+    __shared__ float part[2][3][64];
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), half = w >> 1, rh = w & 1;
+    int b, hq, tile;
+    window_tile_of(a, blockIdx.x, (a.seq + 63) >> 6, b, hq, tile);
+    const Sequence sq = sequence(a, b);
+    const int i0 = 64 * tile;
+    if (i0 >= sq.n) return;
+    const int last = sq.n - 1;
+    const int hk = hq / (a.Hq / a.Hkv);
+    const uint16_t* kp = head_rows(a, a.k, sq, hk);
+    const uint16_t* vp = head_rows(a, a.v, sq, hk);
+    const int w0 = i0 + 32 * rh, i = w0 + l32;
+    const float c2 = a.scale * kLog2e;
+    const KeyWalk walk = key_walk(i0, min(i0 + 63, last), a.W, a.S);
+    const int steps = (walk.tiles + 1) >> 1;
+    auto load = [&](int t) {   // tile 2 t + half
+        const int row0 = 64 * walk.tile(2 * t + half);
+        dma_sequence<D, kRowPad, 2>(kb[half][t & 1], kp, a.k.token, row0, last, rh, lane);
+        dma_sequence<D, kTrPad, 2>(vb[half][t & 1], vp, a.v.token, row0, last, rh, lane);
+    };
+    if (half < walk.tiles) load(0);
+    WinRows<D> st;
+    const uint16_t* qp = head_rows(a, a.q, sq, hq) + min(i, last) * a.q.token;
+#pragma unroll
+    for (int s = 0; s < KD; ++s) st.q[s] = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * h);
+#pragma unroll
+    for (int x = 0; x < ND; ++x) st.o[x] = f32x16{};
+    for (int t = 0; t < steps; ++t) {
+        wait_vmem();
+        __syncthreads();   // tile t has landed, and the buffers of tile t - 1 are read
+        if (2 * (t + 1) + half < walk.tiles) load(t + 1);
+        if (2 * t + half < walk.tiles) {
+            const int j0 = 64 * walk.tile(2 * t + half);
+            const Sight seen = sight(w0, w0 + 31, j0, j0 + 63, a.W, a.S);
+            if (seen != kNone && w0 <= last)
+                win_tile<D>(kb[half][t & 1], vb[half][t & 1], seen == kPart, i, j0, a.W, a.S, st, lane, c2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();   // every tile has been read
+    float* ox = reinterpret_cast<float*>(&kb[0][0][0]) + rh * (ND * 16 * 64);
+    static_assert(sizeof(kb) >= 2 * ND * 16 * 64 * 4, "exchange space");
+    if (half == 1) {
+#pragma unroll
+        for (int x = 0; x < ND; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) ox[(x * 16 + r) * 64 + lane] = st.o[x][r];
+        part[rh][0][lane] = st.m;
+        part[rh][1][lane] = st.l;
+        part[rh][2][lane] = st.lr;
+    }
+    __syncthreads();
+    if (half == 1 || i > last) return;
+    const float m1 = part[rh][0][lane], m = fmaxf(st.m, m1);
+    const float a0 = st.m == -INFINITY ? 0.f : fast_exp2(st.m - m), a1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - m);
+    st.m = m;
+    st.l = st.l * a0 + part[rh][1][lane] * a1;
+    st.lr = st.lr * a0 + part[rh][2][lane] * a1;
 #pragma unroll
     for (int x = 0; x < ND; ++x)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            u32x2 pk;
-            pk.x = pack_bf16x2(st.o[x][4 * g + 0] * inv, st.o[x][4 * g + 1] * inv);
-            pk.y = pack_bf16x2(st.o[x][4 * g + 2] * inv, st.o[x][4 * g + 3] * inv);
-            *reinterpret_cast<u32x2*>(op + 32 * x + 8 * g + 4 * h) = pk;
-        }
-    if (h == 0) a.lse[lse_row(a, sq, hq) + i] = (st.m + fast_log2(st.l)) * kLn2;
+        for (int r = 0; r < 16; ++r) st.o[x][r] = st.o[x][r] * a0 + ox[(x * 16 + r) * 64 + lane] * a1;
+    store_rows(a, st, sq, hq, i, h);
 }
 
 }  // namespace
 
 hipError_t launch_window_fwd(const WindowArgs& a, hipStream_t s) {
-    const int64_t tiles = (a.seq + kFwdRows - 1) / kFwdRows;
+    const int64_t heads = int64_t(a.B) * a.Hq, grid = heads * ((a.seq + kFwdRows - 1) / kFwdRows);
+    const bool split = grid <= (a.d == 128 ? kSplitGrid<128> : kSplitGrid<64>);
     TraceScope _t("window_fwd", s);
-    const dim3 g(unsigned(tiles * a.B * a.Hq)), t(kFwdThreads);
-    if (a.d == 128) hipLaunchKernelGGL(window_fwd_kernel<128>, g, t, 0, s, a);
+    const dim3 g(unsigned(split ? heads * ((a.seq + 63) / 64) : grid)), t(kFwdThreads);
+    if (split && a.d == 128) hipLaunchKernelGGL(window_fwd_split_kernel<128>, g, t, 0, s, a);
+    else if (split) hipLaunchKernelGGL(window_fwd_split_kernel<64>, g, t, 0, s, a);
+    else if (a.d == 128) hipLaunchKernelGGL(window_fwd_kernel<128>, g, t, 0, s, a);
     else hipLaunchKernelGGL(window_fwd_kernel<64>, g, t, 0, s, a);
     return hipGetLastError();
 }
