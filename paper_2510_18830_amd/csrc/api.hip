@@ -996,7 +996,7 @@ msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q,
 }
 
 static size_t carve_cache_attn(const msparse_cache* c, const CacheAttnPlan& p, char* base, CacheAttnArgs* a) {
-    if (p.items == 0) return 0;
+    if (p.slots == 0) return 0;
     Carve w{base};
     a->info = w.take<int32_t>(size_t(2) * c->batch * p.tiles);
     a->pml = w.take<float>(size_t(p.slots) * c->heads_kv * p.rows * 2);
@@ -1025,8 +1025,8 @@ msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, i
     if ((st = check_tensor(out, "out", B, heads_q, tokens, d, true))) return st;
     if (misaligned({lse, ws})) return fail(MSPARSE_ERR_INVALID, "lse or workspace is not 16-byte aligned");
     const CacheAttnPlan p = cache_attn_plan(B, heads_q, cache->heads_kv, tokens, cache->width);
-    if (p.items == 0 && B * p.tiles > kMaxGroups / cache->heads_kv)
-        return fail(MSPARSE_ERR_UNSUPPORTED, "%lld row tiles", (long long)(B * p.tiles * cache->heads_kv));
+    if (cache_attn_groups(p, B) > kMaxGroups / cache->heads_kv)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%lld row tiles of %d heads", (long long)(B * p.tiles), cache->heads_kv);
     CacheAttnArgs a{};
     const size_t need = carve_cache_attn(cache, p, static_cast<char*>(ws), &a);
     if (need && (!ws || ws_bytes < need))
@@ -1044,6 +1044,8 @@ msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, i
     a.scale = scale > 0.f ? scale : 1.0f / std::sqrt(float(d));
     a.tiles = p.tiles;
     a.items = p.items;
+    a.chunk = p.chunk;
+    a.per_tile = p.per_tile;
     a.slots = p.slots;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return check_hip(launch_cache_attn(a, p, s), s, "cache attn");

@@ -68,19 +68,22 @@ struct CacheAttnArgs {
     int32_t Hq, T, W, S;    // W = INT32_MAX: no window
     float scale;
     int32_t tiles;          // row tiles of a (sequence, KV head): its G T rows
-    int32_t items;          // chunks aimed at per KV head (0: one workgroup per row tile)
-    // workspace (items > 0)
+    int32_t items;          // chunks aimed at per KV head; 0: chunks of `chunk` pages, up to per_tile of a row tile
+    int32_t chunk, per_tile;
+    // workspace (slots > 0)
     int32_t* info;          // [B tiles][2]: first chunk, chunks
     float* po;              // [slots, Hkv, rows, d]: sums of the weighted values
     float* pml;             // [slots, Hkv, rows, 2]: running maximum (log2 units), sum of the weights
-    int32_t slots;
+    int32_t slots;          // 0: one chunk per row tile, nothing to join
 };
 // Row tiles and chunks of a call.  rows = G T rows of a (sequence, KV head).
 struct CacheAttnPlan {
     int32_t rt, wr;         // 16-row tiles per wave; waves of a workgroup over rows (1: over pages)
     int32_t rows;           // rows of a workgroup
-    int32_t tiles, items, slots;
+    int32_t tiles, items, chunk, per_tile, slots;
 };
+// workgroups per KV head
+inline int64_t cache_attn_groups(const CacheAttnPlan& p, int64_t B) { return p.slots > 0 ? p.slots : B * p.tiles; }
 CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 

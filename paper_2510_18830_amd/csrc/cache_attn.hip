@@ -31,9 +31,9 @@ namespace {
 
 constexpr int kStages = 3;           // pages staged by the kernel for many rows
 constexpr int kThreads = 256;
-constexpr int64_t kMaxSplit = 4096;  // row tiles up to which their pages are split
 constexpr int64_t kManyRows = 2048;  // rows from which the join takes one per group of lanes
 constexpr int kMinChunk = 4;         // pages: one for each wave
+constexpr int64_t kLongTile = 128;   // pages that many workgroups take without a cut
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -105,14 +105,14 @@ __device__ __forceinline__ int32_t wave_scan(int32_t x) {
 __device__ __forceinline__ PageList tile_pages(const CacheAttnArgs& a, const TileRows& t) {
     return page_list(t.p0, t.p1, a.W, a.S, a.c.width);
 }
-// Tiles' pages are cut into chunks of one length, so that whatever the raggedness
-// the workgroups take as long: `pages`, from the sum over all tiles and the number
-// of chunks aimed at.  Workgroup `item` takes chunk `index` of the `count` of tile
-// e, `first` being the number of that tile's first; a tile without pages has one
-// chunk too.  False past the last one.  Every wave finds it for itself.
+// A workgroup's chunk: `index` of the `count` of tile e, `pages` each, `first` being the
+// slot of that tile's first; a tile without pages has one chunk too.
 struct Chunk {
     int32_t e, first, count, index, pages;
 };
+// With few tiles their pages are cut into chunks of one length, from the sum over all
+// tiles and the number of chunks aimed at, so that whatever the raggedness the
+// workgroups take as long.  False past the last chunk.  Every wave finds its own.
 __device__ __forceinline__ bool find_chunk(const CacheAttnArgs& a, int rows, int item, int lane, Chunk& out) {
     const int E = a.c.B * a.tiles;
     auto pages_of = [&](int e) {
@@ -375,14 +375,22 @@ __device__ __forceinline__ void close_rows(const CacheAttnArgs& a, const CacheRo
 
 __device__ __forceinline__ bool open_walk(const CacheAttnArgs& a, int rows, int lane, Walk& k) {
     k.hk = blockIdx.x % a.c.Hkv;
-    k.ch = Chunk{int32_t(blockIdx.x / a.c.Hkv), 0, 1, 0, INT32_MAX};   // a workgroup per tile
-    if (a.items > 0 && !find_chunk(a, rows, blockIdx.x / a.c.Hkv, lane, k.ch)) return false;
+    const int item = blockIdx.x / a.c.Hkv, E = a.c.B * a.tiles;
+    if (a.items > 0) {
+        if (!find_chunk(a, rows, item, lane, k.ch)) return false;
+    } else {   // the tiles' first chunks, then their second ones, ..
+        k.ch = Chunk{item % E, item % E * a.per_tile, 1, item / E, a.chunk};
+    }
     k.b = k.ch.e / a.tiles;
     k.tr = tile_rows(a, k.b, k.ch.e % a.tiles, rows);
     k.pl = tile_pages(a, k.tr);
+    if (a.items == 0) {
+        k.ch.count = max(int((int64_t(k.pl.count) + a.chunk - 1) / a.chunk), 1);
+        if (k.ch.index >= k.ch.count) return false;
+    }
     k.c0 = int(min(int64_t(k.ch.index) * k.ch.pages, int64_t(k.pl.count)));
     k.c1 = int(min(int64_t(k.c0) + k.ch.pages, int64_t(k.pl.count)));
-    if (a.items > 0 && k.hk == 0 && k.ch.index == 0 && threadIdx.x == 0) {
+    if (a.slots > 0 && k.hk == 0 && k.ch.index == 0 && threadIdx.x == 0) {
         a.info[2 * k.ch.e] = k.ch.first;
         a.info[2 * k.ch.e + 1] = k.ch.count;
     }
@@ -404,8 +412,11 @@ __device__ __forceinline__ Pages look_up(const CacheAttnArgs& a, const Walk& k, 
         if (uint32_t(page) >= uint32_t(a.c.pages)) page = -1;
     }
     const int64_t at = int64_t(max(page, 0)) * a.c.Hkv + k.hk;
-    // (the first stays above 0, as a masked logit times 0 would be NaN)
-    return Pages{page, fmaxf(a.c.ks[at] * (a.scale * kLog2e), 0x1p-126f), a.c.vs[at]};
+    // (The first stays above 0, as a masked logit times 0 would be NaN.  A missing page's
+    // values weigh 0, whatever scale stands where it reads one; masked by its sign, as a
+    // selection becomes a branch around the load: 8 x 128K 225 us, 209 so.)
+    const float vs = __uint_as_float(__float_as_uint(a.c.vs[at]) & ~uint32_t(page >> 31));
+    return Pages{page, fmaxf(a.c.ks[at] * (a.scale * kLog2e), 0x1p-126f), vs};
 }
 __device__ __forceinline__ int32_t page_at(const Pages& p, int i) { return __builtin_amdgcn_readlane(p.page, i); }
 __device__ __forceinline__ float lane_value(float x, int i) {
@@ -631,7 +642,7 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(CacheAttnArgs a, i
 
 template <int D>
 void launch(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
-    const int64_t wgs = (p.items > 0 ? int64_t(p.slots) : int64_t(a.c.B) * p.tiles) * a.c.Hkv;
+    const int64_t wgs = cache_attn_groups(p, a.c.B) * a.c.Hkv;
     const dim3 g(static_cast<unsigned>(wgs)), t(kThreads);
     {
         TraceScope _t("cache_attn", s);
@@ -639,7 +650,7 @@ void launch(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
         else if (p.rt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2>), g, t, 0, s, a);
         else hipLaunchKernelGGL((cache_attn_kernel<D, 1>), g, t, 0, s, a);
     }
-    if (p.items > 0) {
+    if (p.slots > 0) {
         TraceScope _t("cache_join", s);
         const int64_t rows = int64_t(a.c.B) * a.Hq * a.T;
         constexpr int N = kThreads / (D / 4);
@@ -659,17 +670,39 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
     p.wr = rows <= 32 ? 1 : 4;
     p.rows = 16 * p.rt * p.wr;
     p.tiles = int32_t((rows + p.rows - 1) / p.rows);
-    const int64_t e = B * p.tiles;
-    // Chunks: where rows bound the work, as many as are resident at once (three
-    // workgroups a CU; 512, 768, 1024 of them: 69, 67, 73 us for 4 x 200 tokens of 16
-    // over 2 heads in a window of 4096), where memory does, two rounds of them (512,
-    // 768, 1024, 1536, 2048: 255, 236, 224, 211, 211 us for 8 contexts of up to 128K
-    // x 8 heads).  Each tile may have one more than its share; and a chunk is no
-    // longer than the mean tile, however many there are.
-    const int64_t aim = (p.rt == 1 ? 1536 : 768) / Hkv;
-    if (width > kMinChunk && e <= kMaxSplit && e * width < INT32_MAX) {
+    const int64_t e = B * p.tiles, groups = e * Hkv;
+    // One chunk per row tile, where a cut would cost a short context more than it saves
+    // (a join and half the walk: 64 contexts of 512 tokens, one KV head: 10.7 -> 8.7 us)
+    p.per_tile = 1;
+    p.chunk = INT32_MAX;
+    if (width <= (p.wr == 4 ? kMinChunk : 2 * kMinChunk)) return p;
+    if (groups < (p.wr == 4 ? 512 : width <= kLongTile ? 192 : 560)) {
+        // Few tiles: equal chunks whatever the raggedness (find_chunk).  Where rows bound
+        // the work, as many as are resident at once (three workgroups a CU; 512, 768,
+        // 1024 of them: 69, 67, 73 us for 4 x 200 tokens of 16 over 2 heads in a window
+        // of 4096), where memory does, two rounds of them (512, 768, 1024, 1536, 2048:
+        // 255, 236, 224, 211, 211 us for 8 contexts of up to 128K x 8 heads).  Each tile
+        // may have one more than its share; a chunk is no longer than the mean tile.
+        const int64_t aim = (p.rt == 1 ? 1536 : 768) / Hkv;
         p.items = int32_t(std::max(aim - e, e));
         p.slots = int32_t(std::min(p.items + e, e * ((width + kMinChunk - 1) / kMinChunk)));
+        return p;
+    }
+    // Many tiles fill the card by themselves; every wave's search for its chunk among
+    // them, and the join, would cost more than even shares give (both in us, equal chunks
+    // -> these): one token, 8 KV heads: 256 ragged contexts of up to 512 tokens 60 -> 37,
+    // 1024 of 4096 952 -> 788, 4096 of 512 4207 -> 535, 64 of 4096 63 -> 69 (all of one
+    // length 100 -> 90); of 16K: 52: 180 -> 213 (302 -> 325), 72: 245 -> 259 (466 -> 417),
+    // 90: 330 -> 335 (736 -> 506).  128 rows: 4 x 1024 new tokens, 8 heads of 4 each, at
+    // 5120: 518 -> 403; 4096 at 8192, one head: 512 tiles 368 -> 343, 128 tiles 102 -> 244.
+    // Contexts longer than kLongTile pages are still cut, at even lengths from the
+    // table's width, so that one long context among short ones is not a walk of one
+    // workgroup's; the slots of their chunks take about 1/2 GB at most.
+    const int64_t most = std::min<int64_t>(8, (p.wr == 4 ? 8192 : 32768) / groups);
+    if (width > kLongTile && most > 1) {
+        p.chunk = int32_t(std::max<int64_t>(kLongTile, (width + most - 1) / most));
+        p.per_tile = int32_t((width + p.chunk - 1) / p.chunk);
+        p.slots = int32_t(e * p.per_tile);
     }
     return p;
 }

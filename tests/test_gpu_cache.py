@@ -339,3 +339,138 @@ def test_decode_loop_together(gpu):
     want, _ = ms.window_fwd(win, rot(q).to(BF).to(gpu), rot(k).to(BF).to(gpu), v)
     err = (out.double() - want.double()).abs()
     assert float(err.max()) < 0.5 and float((err.square().sum() / want.double().square().sum()).sqrt()) < 0.1
+
+
+# ---------------------------------------------------------------- many sequences, long tables
+def _some_lens(seed, B, top):
+    lens = np.random.default_rng(seed).integers(0, top + 1, B)
+    lens[::9] = 0
+    lens[1] = top
+    return [int(x) for x in lens]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,d,T,top,wide", [
+    (150, 2, 1, 64, 1, 700, 0),      # equal chunks over more than 64 tiles
+    (100, 4, 2, 128, 1, 600, 0),     # a workgroup per tile
+    (800, 1, 1, 64, 1, 300, 150),    # chunks from the table's width, most tables half empty
+    (30, 12, 4, 128, 2, 400, 130), (4200, 1, 1, 64, 1, 150, 0), (2, 20, 1, 128, 1, 9000, 0),
+    (40, 4, 4, 64, 40, 500, 0), (70, 8, 2, 128, 70, 300, 140),
+])
+def test_attn_many_sequences(gpu, B, Hq, Hkv, d, T, top, wide):
+    print(f"attn B{B} Hq{Hq} Hkv{Hkv} d{d} T{T} top{top} width{wide}", flush=True)
+    lens = _some_lens(B, B, top)
+    cache, table, L = _filled(B, lens, Hkv, d, gpu)
+    if wide > table.shape[1]:
+        more = torch.full((B, wide), -1, dtype=torch.int32, device=gpu)
+        more[:, :table.shape[1]] = table
+        table = more
+    q = _randn(1, (B, Hq, T, d), gpu)
+    out, lse = ms.cache_attn(cache, table, L, q)
+    again = ms.cache_attn(cache, table, L, q)
+    torch.cuda.synchronize()
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    _attn_check(q, out, lse, cache, table, lens, 0, 0)
+
+
+def test_attn_one_long_among_many_short(gpu):
+    """Chunks of a fixed length: one context of many, the others of one."""
+    B, Hkv = 800, 1
+    lens = [20] * B
+    lens[5], lens[799] = 30000, 12345
+    cache, table, L = _filled(21, [20] * B, Hkv, 64, gpu, extra=700)
+    wide = torch.full((B, 470), -1, dtype=torch.int32, device=gpu)
+    wide[:, :1] = table
+    free = torch.tensor(sorted(set(range(cache.k.shape[0])) - set(table[:, 0].tolist())), dtype=torch.int32)
+    assert len(free) >= 469 + 192
+    wide[5, 1:469], wide[799, 1:193] = free[:468].to(gpu), free[468:660].to(gpu)
+    for i, b in enumerate((5, 799)):
+        n = lens[b] - 20
+        part = torch.tensor([20], dtype=torch.int32, device=gpu)
+        k, v = _randn(30 + i, (1, Hkv, n, 64), gpu), _randn(40 + i, (1, Hkv, n, 64), gpu)
+        ms.cache_append(cache, wide[b:b + 1].contiguous(), part, k, v, inv_freq=_freq(64, gpu))
+    L = torch.tensor(lens, dtype=torch.int32, device=gpu)
+    q = _randn(1, (B, 4, 1, 64), gpu, 2.0)
+    for W, S in ((0, 0), (9000, 100)):
+        out, lse = ms.cache_attn(cache, wide, L, q, window=W, sinks=S)
+        torch.cuda.synchronize()
+        _attn_check(q, out, lse, cache, wide, lens, W, S)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,T,L", [(4, 1, 64, 600, 1500), (2, 1, 128, 1100, 1700)])
+def test_attn_many_rows_in_chunks(gpu, Hq, Hkv, d, T, L):
+    """Row tiles whose chunks are joined a row per group of lanes."""
+    cache, table, lens = _filled(T, [L], Hkv, d, gpu)
+    q = _randn(1, (1, Hq, T, d), gpu)
+    out, lse = ms.cache_attn(cache, table, lens, q)
+    torch.cuda.synchronize()
+    _attn_check(q, out, lse, cache, table, [L], 0, 0)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,d,T,ragged", [(300, 3, 1, 64, 3, True), (1, 2, 1, 128, 36000, False),
+                                                 (260, 2, 2, 128, 1, False)])
+def test_append_of_many_pages(gpu, B, Hq, Hkv, d, T, ragged):
+    """Queries behind the keys in the same workgroups."""
+    rng = np.random.default_rng(T)
+    lens = [int(x) for x in rng.integers(0, 130, B)]
+    counts = [int(x) for x in rng.integers(0, T + 1, B)] if ragged else None
+    needs = [(n + T + 63) // 64 for n in lens]
+    cache = _pool(T, sum(needs) + 2, Hkv, d, gpu)
+    table = _table(T, needs, sum(needs) + 2)
+    _append_and_check(gpu, cache, table, [0] * B, max(lens), lens, Hq, d, None, 500)
+    _append_and_check(gpu, cache, table, lens, T, counts, Hq, d, _freq(d, gpu), 600)
+
+
+def test_attn_missing_page_beside_a_soiled_scale(gpu):
+    """A token without a page is not seen, whatever the scales of the pool's first page hold."""
+    for T, lens in ((1, [300, 90]), (1, [40 * 64, 200]), (40, [300, 90])):
+        cache, table, L = _filled(17, lens, 2, 64, gpu, extra=3)
+        held = set(table.flatten().tolist())
+        if 0 in held:   # page 0 to be nobody's
+            spare = next(p for p in range(1, cache.k.shape[0]) if p not in held)
+            for t in (cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scale, cache.v_scale):
+                t[spare] = t[0]
+            table[table == 0] = spare
+        table[0, 2] = -1
+        q = _randn(1, (2, 4, T, 64), gpu)
+        want = ms.cache_attn(cache, table, L, q)
+        for bad in (float("nan"), float("inf")):
+            cache.k_scale[0] = cache.v_scale[0] = bad
+            got = ms.cache_attn(cache, table, L, q)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        cache.k_scale[0] = cache.v_scale[0] = 1.0
+        _attn_check(q, got[0], got[1], cache, table, lens, 0, 0)
+
+
+def test_cache_beyond_4_gb(gpu):
+    """Pages whose codes lie past 2^32 bytes: the same codes and results as in a small pool."""
+    B, Hq, Hkv, d, pages = 2, 8, 8, 128, 70000
+    big, small = ms.make_cache(pages, Hkv, d, gpu), ms.make_cache(8, Hkv, d, gpu)
+    near = torch.arange(6, dtype=torch.int32, device=gpu).view(B, 3)
+    far = near + (pages - 6)
+    freq, lens = _freq(d, gpu), torch.tensor([0, 0], dtype=torch.int32, device=gpu)
+    q, k, v = (_randn(i, (B, h, 150, d), gpu) for i, h in ((1, Hq), (2, Hkv), (3, Hkv)))
+    got = []
+    for c, table in ((big, far), (small, near)):
+        r = ms.cache_append(c, table, lens, k, v, q=q, inv_freq=freq)
+        got.append((r,) + ms.cache_attn(c, table, lens + 150, r) + ms.cache_attn(c, table, lens + 150, r[:, :, :1]))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    for p in range(6):
+        m = 22 if p % 3 == 2 else 64   # the third page of a sequence holds 22 tokens, and anything behind them
+        assert torch.equal(big.k[pages - 6 + p, :, :m].view(torch.uint8), small.k[p, :, :m].view(torch.uint8))
+        assert torch.equal(big.v[pages - 6 + p, :, :, :m].view(torch.uint8), small.v[p, :, :, :m].view(torch.uint8))
+
+
+def test_cache_two_calls_at_once(gpu):
+    """Two streams read one cache, each with its own workspace and results."""
+    lens = [9000, 300, 77]
+    cache, table, L = _filled(23, lens, 2, 128, gpu)
+    qs = [_randn(i, (3, 8, 1, 128), gpu) for i in (1, 2)]
+    want = [ms.cache_attn(cache, table, L, q) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(5):
+        got = [ms.cache_attn(cache, table, L, q, stream=s) for q, s in zip(qs, streams)]
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
