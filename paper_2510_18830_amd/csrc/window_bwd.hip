@@ -96,13 +96,47 @@ __device__ __forceinline__ void dq_tile(const uint16_t* kt, const uint16_t* vt, 
     }
 }
 
-// Row i's operands, lse log2(e) and Delta; `first` waves leave the latter two for the
-// key-major pass.
+// This lane's share of Delta = sum P dP over one tile.
 template <int D>
-__device__ __forceinline__ void open_rows(const WindowArgs& a, const Sequence& sq, int hq, int i, int h, bool first,
+__device__ __forceinline__ float delta_tile(const uint16_t* kt, const uint16_t* vt, bool masked, int i, int j0, int W,
+                                            int S, const WinDq<D>& st, int lane, float c2) {
+    const int h = lane >> 5, l32 = lane & 31, lim = min(S - 1, i);
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        f32x16 sa = f32x16{}, pa = f32x16{};
+#pragma unroll
+        for (int k = 0; k < WinDq<D>::KD; ++k) {
+            sa = mfma32(dma_read16<D, kDualPad>(kt, 32 * c + l32, h + 2 * k), st.q[k], sa);
+            pa = mfma32(dma_read16<D, kDualPad>(vt, 32 * c + l32, h + 2 * k), st.g[k], pa);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float p = fast_exp2(__builtin_fmaf(sa[r], c2, -st.lse2)) * pa[r];
+            const bool seen = !masked || sees(i, j0 + 32 * c + 8 * (r >> 2) + 4 * h + (r & 3), W, lim);
+            sum += seen ? p : 0.f;
+        }
+    }
+    return sum;
+}
+
+// Rows that see few keys take Delta from the weights and products themselves, in a walk
+// of its own, instead of dO . O: O's rounding to bf16 is as large as the other roundings
+// of dQ and dK there, and falls with the number of keys that O averages over.  Error of
+// dQ and dK by their norm, and time of the backward pass of 64 heads x 1024 rows of 128:
+// window 4: 3.0e-3, 62 us with dO . O, 2.35e-3, 70 us with the walk; window 16 and 4
+// sinks: 2.5e-3, 90 and 2.35e-3, 99; window 64: 2.45e-3, 63 and 2.35e-3, 70; window 100
+// and 4 sinks: 2.4e-3, 90 and 2.35e-3, 102.
+constexpr int kFewKeys = 64;
+__device__ __forceinline__ bool few_keys(const WindowArgs& a, int i1) {
+    return min(int64_t(a.W) + a.S, int64_t(i1) + 1) <= kFewKeys;
+}
+
+// Row i's operands, lse log2(e) and dO . O
+template <int D>
+__device__ __forceinline__ void open_rows(const WindowArgs& a, const Sequence& sq, int hq, int i, int h,
                                           WinDq<D>& st) {
     constexpr int KD = WinDq<D>::KD;
-    const bool real = i < sq.n;
     const int ic = min(i, sq.n - 1);
     const uint16_t* qp = head_rows(a, a.q, sq, hq) + ic * a.q.token;
     const uint16_t* gp = head_rows(a, a.dout, sq, hq) + ic * a.dout.token;
@@ -122,13 +156,16 @@ __device__ __forceinline__ void open_rows(const WindowArgs& a, const Sequence& s
         for (int e = 0; e < 4; ++e)
             acc += bf16_lo(st.g[s][e]) * bf16_lo(o[s][e]) + bf16_hi(st.g[s][e]) * bf16_hi(o[s][e]);
     st.dlt = half_swap_sum(acc);
-    if (first && h == 0 && i < padded_rows(sq.n)) {
-        float* rv = a.rows + int64_t(2 * hq) * a.rows_pad + value_row(a, sq) + i;
-        rv[0] = real ? st.lse2 : INFINITY;   // a row past the end: P = 0
-        rv[a.rows_pad] = real ? st.dlt : 0.f;
-    }
 #pragma unroll
     for (int x = 0; x < WinDq<D>::ND; ++x) st.acc[x] = f32x16{};
+}
+// lse log2(e) and Delta of row i for the key-major pass
+template <int D>
+__device__ __forceinline__ void leave_rows(const WindowArgs& a, const Sequence& sq, int hq, int i, const WinDq<D>& st) {
+    if (i >= padded_rows(sq.n)) return;
+    float* rv = a.rows + int64_t(2 * hq) * a.rows_pad + value_row(a, sq) + i;
+    rv[0] = i < sq.n ? st.lse2 : INFINITY;   // a row past the end: P = 0
+    rv[a.rows_pad] = i < sq.n ? st.dlt : 0.f;
 }
 template <int D>
 __device__ __forceinline__ void store_dq(const WindowArgs& a, const Sequence& sq, int hq, int i, int h,
@@ -163,30 +200,45 @@ __global__ void __launch_bounds__(kDqThreads)
     const uint16_t* vp = head_rows(a, a.v, sq, hk);
     const int w0 = i0 + 32 * w, i = w0 + l32;
     WinDq<D> st;
-    open_rows(a, sq, hq, i, h, true, st);
+    open_rows(a, sq, hq, i, h, st);
     const float c2 = a.scale * kLog2e;
-    const KeyWalk walk = key_walk(i0, min(i0 + kDqRows - 1, last), a.W, a.S);
+    const int i1 = min(i0 + kDqRows - 1, last);
+    const KeyWalk walk = key_walk(i0, i1, a.W, a.S);
     auto load = [&](uint16_t* kt, uint16_t* vt, int t) {
         const int row0 = 64 * walk.tile(t);
         dma_sequence<D, kDualPad, 4>(kt, kp, a.k.token, row0, last, w, lane);
         dma_sequence<D, kDualPad, 4>(vt, vp, a.v.token, row0, last, w, lane);
     };
-    load(k0s, v0s, 0);
-    wait_vmem();
-    __syncthreads();
-    auto step = [&](int t, const uint16_t* ck, const uint16_t* cv, uint16_t* nk, uint16_t* nv) {
-        if (t + 1 < walk.tiles) load(nk, nv, t + 1);
-        const int j0 = 64 * walk.tile(t);
-        const Sight seen = sight(w0, w0 + 31, j0, j0 + 63, a.W, a.S);
-        if (seen != kNone && w0 <= last) dq_tile<D>(ck, cv, seen == kPart, i, j0, a.W, a.S, st, lane, c2);
-        __builtin_amdgcn_sched_barrier(0);
+    // tile(kt, vt, masked, j0) for every tile that the wave's rows see
+    auto walk_tiles = [&](auto tile) {
+        load(k0s, v0s, 0);
         wait_vmem();
         __syncthreads();
+        auto step = [&](int t, const uint16_t* ck, const uint16_t* cv, uint16_t* nk, uint16_t* nv) {
+            if (t + 1 < walk.tiles) load(nk, nv, t + 1);
+            const int j0 = 64 * walk.tile(t);
+            const Sight seen = sight(w0, w0 + 31, j0, j0 + 63, a.W, a.S);
+            if (seen != kNone && w0 <= last) tile(ck, cv, seen == kPart, j0);
+            __builtin_amdgcn_sched_barrier(0);
+            wait_vmem();
+            __syncthreads();
+        };
+        for (int t = 0; t < walk.tiles; t += 2) {
+            step(t, k0s, v0s, k1s, v1s);
+            if (t + 1 < walk.tiles) step(t + 1, k1s, v1s, k0s, v0s);
+        }
     };
-    for (int t = 0; t < walk.tiles; t += 2) {
-        step(t, k0s, v0s, k1s, v1s);
-        if (t + 1 < walk.tiles) step(t + 1, k1s, v1s, k0s, v0s);
+    if (few_keys(a, i1)) {
+        float sum = 0.f;
+        walk_tiles([&](const uint16_t* kt, const uint16_t* vt, bool masked, int j0) {
+            sum += delta_tile<D>(kt, vt, masked, i, j0, a.W, a.S, st, lane, c2);
+        });
+        st.dlt = half_swap_sum(sum);
     }
+    if (h == 0) leave_rows(a, sq, hq, i, st);
+    walk_tiles([&](const uint16_t* kt, const uint16_t* vt, bool masked, int j0) {
+        dq_tile<D>(kt, vt, masked, i, j0, a.W, a.S, st, lane, c2);
+    });
     if (i <= last) store_dq(a, sq, hq, i, h, st);
 }
 
@@ -198,6 +250,7 @@ window_dq_split_kernel(WindowArgs a) {
     constexpr int ND = WinDq<D>::ND;
     constexpr int TE = DmaTile<D, kDualPad>::kElems;
     __shared__ __attribute__((aligned(16))) uint16_t kb[2][2][TE], vb[2][2][TE];   // [half][parity]
+    __shared__ float share[2][2][64];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), half = w >> 1, rh = w & 1;
     int b, hq, tile;
@@ -211,7 +264,8 @@ window_dq_split_kernel(WindowArgs a) {
     const uint16_t* vp = head_rows(a, a.v, sq, hk);
     const int w0 = i0 + 32 * rh, i = w0 + l32;
     const float c2 = a.scale * kLog2e;
-    const KeyWalk walk = key_walk(i0, min(i0 + 63, last), a.W, a.S);
+    const int i1 = min(i0 + 63, last);
+    const KeyWalk walk = key_walk(i0, i1, a.W, a.S);
     const int steps = (walk.tiles + 1) >> 1;
     auto load = [&](int t) {   // tile 2 t + half
         const int row0 = 64 * walk.tile(2 * t + half);
@@ -220,19 +274,34 @@ window_dq_split_kernel(WindowArgs a) {
     };
     if (half < walk.tiles) load(0);
     WinDq<D> st;
-    open_rows(a, sq, hq, i, h, half == 0, st);
-    for (int t = 0; t < steps; ++t) {
-        wait_vmem();
-        __syncthreads();   // tile t has landed, and the buffers of tile t - 1 are read
-        if (2 * (t + 1) + half < walk.tiles) load(t + 1);
-        if (2 * t + half < walk.tiles) {
-            const int j0 = 64 * walk.tile(2 * t + half);
-            const Sight seen = sight(w0, w0 + 31, j0, j0 + 63, a.W, a.S);
-            if (seen != kNone && w0 <= last)
-                dq_tile<D>(kb[half][t & 1], vb[half][t & 1], seen == kPart, i, j0, a.W, a.S, st, lane, c2);
+    open_rows(a, sq, hq, i, h, st);
+    auto walk_tiles = [&](auto tile) {   // tile 0 is on its way
+        for (int t = 0; t < steps; ++t) {
+            wait_vmem();
+            __syncthreads();   // tile t has landed, and the buffers of tile t - 1 are read
+            if (2 * (t + 1) + half < walk.tiles) load(t + 1);
+            if (2 * t + half < walk.tiles) {
+                const int j0 = 64 * walk.tile(2 * t + half);
+                const Sight seen = sight(w0, w0 + 31, j0, j0 + 63, a.W, a.S);
+                if (seen != kNone && w0 <= last) tile(kb[half][t & 1], vb[half][t & 1], seen == kPart, j0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (few_keys(a, i1)) {
+        float sum = 0.f;
+        walk_tiles([&](const uint16_t* kt, const uint16_t* vt, bool masked, int j0) {
+            sum += delta_tile<D>(kt, vt, masked, i, j0, a.W, a.S, st, lane, c2);
+        });
+        share[half][rh][lane] = half_swap_sum(sum);
+        __syncthreads();       // every tile has been read
+        st.dlt = share[0][rh][lane] + share[1][rh][lane];
+        if (half < walk.tiles) load(0);
     }
+    if (half == 0 && h == 0) leave_rows(a, sq, hq, i, st);
+    walk_tiles([&](const uint16_t* kt, const uint16_t* vt, bool masked, int j0) {
+        dq_tile<D>(kt, vt, masked, i, j0, a.W, a.S, st, lane, c2);
+    });
     __syncthreads();   // every tile has been read
     float* x1 = reinterpret_cast<float*>(&kb[0][0][0]) + rh * (ND * 16 * 64);
     static_assert(sizeof(kb) >= 2 * ND * 16 * 64 * 4, "exchange space");

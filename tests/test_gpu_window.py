@@ -226,3 +226,124 @@ def test_window_on_another_stream(gpu):
     s.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n,d,W,S", [
+    (60, 8, 2, 129, 64, 50, 3), (40, 4, 4, 300, 128, 100, 7), (30, 8, 1, 260, 64, 0, 0), (24, 8, 4, 333, 128, 0, 0),
+    (50, 4, 1, 500, 64, 5, 0), (16, 16, 2, 257, 128, 20, 130), (70, 7, 1, 70, 128, 3, 1),
+])
+def test_window_on_large_grids(gpu, B, Hq, Hkv, n, d, W, S):
+    """More workgroups than the kernels for small grids take: the first, a middle and the last sequence."""
+    q, k, v, do = _inputs(n, B, Hq, Hkv, n, d, gpu)
+    win = ms.make_window(B, n, Hq, Hkv, d, W, S)
+    out, lse = ms.window_fwd(win, q, k, v)
+    grads = ms.window_bwd(win, q, k, v, out, do, lse)
+    torch.cuda.synchronize()
+    for b in (0, B // 2, B - 1):
+        at = slice(b, b + 1)
+        _check(q[at], k[at], v[at], do[at], out[at], lse[at], [g[at] for g in grads], W, S, d ** -0.5)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_window_packed_on_large_grids(gpu, d):
+    """Many documents, some empty, in tensors laid out as [tokens, heads, d]."""
+    Hq, Hkv, W, S = 6, 2, 90, 4
+    lens = (np.random.default_rng(d).integers(0, 420, 60) * (np.arange(60) % 7 != 3)).tolist()
+    starts = torch.tensor([0] + lens).cumsum(0).to(torch.int32)
+    total = int(starts[-1])
+    q, k, v, do = (_make(s, 1, total, h, d, gpu).transpose(1, 2) for s, h in ((1, Hq), (2, Hkv), (3, Hkv), (4, Hq)))
+    win = ms.make_window(len(lens), max(lens), Hq, Hkv, d, W, S, tokens=total)
+    st = starts.to(gpu)
+    out, lse = ms.window_fwd(win, q, k, v, starts=st)
+    grads = ms.window_bwd(win, q, k, v, out, do, lse, starts=st)
+    torch.cuda.synchronize()
+    for b in (0, 1, 3, 30, 58, 59):
+        if lens[b]:
+            _check(q, k, v, do, out, lse, grads, W, S, d ** -0.5, int(starts[b]), lens[b])
+
+
+@pytest.mark.parametrize("Hq,Hkv,n,d,W,S", [(2, 1, 2600, 64, 0, 0), (1, 1, 2100, 128, 600, 70), (8, 1, 1100, 128, 0, 0)])
+def test_window_keys_in_several_walks(gpu, Hq, Hkv, n, d, W, S):
+    """Few key groups with long walks over the rows, which are cut."""
+    q, k, v, do = _inputs(n, 1, Hq, Hkv, n, d, gpu)
+    win = ms.make_window(1, n, Hq, Hkv, d, W, S)
+    out, lse = ms.window_fwd(win, q, k, v)
+    grads = ms.window_bwd(win, q, k, v, out, do, lse)
+    torch.cuda.synchronize()
+    _check(q, k, v, do, out, lse, grads, W, S, d ** -0.5)
+
+
+@pytest.mark.parametrize("B,n", [(1, 200), (64, 200)])
+@pytest.mark.parametrize("W,S", [(1, 0), (4, 0), (20, 4), (60, 4)])
+def test_window_few_keys_gradient_error(gpu, B, n, W, S):
+    """Rows that see few keys: dQ and dK carry the roundings of dZ and of themselves to bf16, not that of O.  A rounding
+    moves m 2^e (1 <= m < 2) by a uniformly spread error of at most 2^-8 2^e: 2^-8 / (m sqrt(3)) rms of the value, 0.736
+    of 2^-8 / sqrt(3) over a binade of evenly spread logarithms, 1.66e-3; two of them are 2.35e-3 by the norms, and
+    2.7e-3 leaves 15 %.  (With O's rounding: 3.0e-3 for 4 keys.)
+    One key: P = 1 + t with |t| < 2^-20 (lse and its logit below 8 in log2 units, in fp32), dZ = -t dP with |dP| < 60,
+    times scale |K| < 0.7: below 4e-5."""
+    d, H = 64, 8
+    q, k, v, do = _inputs(77, B, H, H, n, d, gpu)
+    win = ms.make_window(B, n, H, H, d, W, S)
+    out, lse = ms.window_fwd(win, q, k, v)
+    dq, dk, _ = ms.window_bwd(win, q, k, v, out, do, lse)
+    f = [to_f64(t[0].cpu()) for t in (q, k, v, do)]
+    for got, (ref, _) in zip((dq, dk), OW.sequence_bwd(*f, W, S, d ** -0.5)):
+        err = to_f64(got[0].cpu()) - ref
+        if W == 1 and S == 0:
+            assert np.abs(err).max() <= 4e-5
+        else:
+            assert np.linalg.norm(err) <= 2.7e-3 * np.linalg.norm(ref)
+
+
+def test_window_far_strides(gpu):
+    """Heads 2^31 elements apart: the same bits as in contiguous tensors."""
+    n, d, gap = 150, 64, (1 << 31) + 64
+    q, k, v, do = _inputs(81, 1, 2, 2, n, d, gpu)
+    win = ms.make_window(1, n, 2, 2, d, 30, 2)
+    out, lse = ms.window_fwd(win, q, k, v)
+    want = (out, lse) + ms.window_bwd(win, q, k, v, out, do, lse)
+    pool = torch.zeros(gap + 8 * n * d, dtype=torch.bfloat16, device=gpu)
+    far = [pool.as_strided((1, 2, n, d), (0, gap, d, 1), i * n * d) for i in range(8)]
+    for a, b in zip(far, (q, k, v, do)):
+        a.copy_(b)
+    fo, fl = ms.window_fwd(win, *far[:3], out=far[4])
+    fg = ms.window_bwd(win, *far[:3], fo, far[3], fl, dq=far[5], dk=far[6], dv=far[7])
+    for a, b in zip((fo, fl) + tuple(fg), want):
+        assert torch.equal(a, b)
+
+
+def test_window_two_calls_at_once(gpu):
+    """Two streams, each with its own tensors and workspace; two graphs with one workspace, replayed in turn."""
+    win = ms.make_window(1, 600, 4, 2, 64, 128, 70)
+    data = [_inputs(90 + 10 * i, 1, 4, 2, 600, 64, gpu) for i in range(2)]
+
+    def step(x, ws):
+        out, lse = ms.window_fwd(win, *x[:3])
+        return (out, lse) + ms.window_bwd(win, *x[:3], out, x[3], lse, workspace=ws)
+
+    room = lambda: torch.empty(ms.window_bwd_workspace_bytes(win), dtype=torch.uint8, device=gpu)  # noqa: E731
+    want = [step(x, room()) for x in data]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in data], []
+    rooms = [room() for _ in data]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for s, x, ws in zip(streams, data, rooms):
+            with torch.cuda.stream(s):
+                got.append(step(x, ws))
+    torch.cuda.synchronize()
+    shared, graphs, outs = room(), [], []
+    for x in data:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(x, shared))
+        graphs.append(g)
+    for _ in range(3):
+        for g in graphs:   # one after the other on one stream
+            g.replay()
+        torch.cuda.synchronize()
+        for a, b, c in zip(got, want, outs):
+            for x, y, z in zip(a, b, c):
+                assert torch.equal(x, y) and torch.equal(z, y)
