@@ -479,8 +479,9 @@ typedef struct {
  * even.  Tokens that an earlier call wrote move to a larger scale when a later
  * one needs it (exact, but for values below 2^-6 of the new scale, which round
  * again).  A key or value that is not finite becomes NaN and does not count for
- * the scale.  Slots of other tokens keep their codes.  Two calls that append to
- * one page must not overlap. */
+ * the scale.  Slots of other tokens keep their codes.  A page that a call writes
+ * to stands in the tables once, else its codes are undefined; two calls that
+ * append to one page must not overlap. */
 MSPARSE_API msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q, int32_t tokens,
                                                 const msparse_tensor* q, const msparse_tensor* k,
                                                 const msparse_tensor* v, const msparse_tensor* q_out,

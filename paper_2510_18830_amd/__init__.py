@@ -388,6 +388,14 @@ def _rows(t, name, shape, device):
     return Tensor(t.data_ptr(), batch, head, token)
 
 
+def _like(t):
+    """A new tensor for an output like t (which _rows has passed: contiguous rows, and so are these), and it as an
+    msparse_tensor."""
+    new = torch.empty_like(t)
+    batch, head, token, _ = new.stride()
+    return new, Tensor(new.data_ptr(), batch, head, token)
+
+
 def _current(device):
     """The current stream of a device as a pointer (without the Stream object that torch.cuda.current_stream makes:
     2 us of a small call's 10)."""
@@ -398,7 +406,7 @@ def _elsewhere(device, stream):
     """Whether a call has to enter a stream (or a device) that is not the current one."""
     if device.type != "cuda":
         _refuse(f"tensors on {device}")
-    return stream is not None or device.index != torch.cuda.current_device()
+    return stream is not None or device.index != torch._C._cuda_getDevice()
 
 
 def _enter(device, stream):
@@ -416,7 +424,8 @@ def _room(workspace, nbytes, device):
         if nbytes == 0:
             return None, None, 0
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    elif workspace.device != device or not workspace.is_contiguous():
+        return workspace, workspace.data_ptr(), nbytes
+    if workspace.device != device or not workspace.is_contiguous():
         _refuse(f"workspace on {workspace.device}{'' if workspace.is_contiguous() else ', not contiguous'}")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
@@ -448,12 +457,16 @@ def window_fwd(win: Window, q, k, v, starts=None, out=None, lse=None, stream=Non
     qs, ks = _window_shapes(win)
     tq = _rows(q, "q", qs, dev)
     if out is None:
-        out = torch.empty_like(q)
+        out, to = _like(q)
+    else:
+        to = _rows(out, "out", qs, dev)
     if lse is None:
         lse = torch.empty(qs[:3], dtype=_F32, device=dev)
+        tl = lse.data_ptr()
+    else:
+        tl = _arg(lse, "lse", qs[:3], _F32, dev)
     _check(lib().msparse_window_fwd(win, _starts(win, starts, dev), tq, _rows(k, "k", ks, dev), _rows(v, "v", ks, dev),
-                                    _rows(out, "out", qs, dev), _arg(lse, "lse", qs[:3], _F32, dev),
-                                    _current(dev)))
+                                    to, tl, _current(dev)))
     return out, lse
 
 
@@ -470,13 +483,12 @@ def window_bwd(win: Window, q, k, v, out, dout, lse, starts=None, dq=None, dk=No
             return window_bwd(win, q, k, v, out, dout, lse, starts, dq, dk, dv, workspace)
     qs, ks = _window_shapes(win)
     tq, tk, tv = _rows(q, "q", qs, dev), _rows(k, "k", ks, dev), _rows(v, "v", ks, dev)
-    dq = torch.empty_like(q) if dq is None else dq
-    dk = torch.empty_like(k) if dk is None else dk
-    dv = torch.empty_like(v) if dv is None else dv
+    dq, tdq = _like(q) if dq is None else (dq, _rows(dq, "dq", qs, dev))
+    dk, tdk = _like(k) if dk is None else (dk, _rows(dk, "dk", ks, dev))
+    dv, tdv = _like(v) if dv is None else (dv, _rows(dv, "dv", ks, dev))
     workspace, at, room = _room(workspace, window_bwd_workspace_bytes(win), dev)
     _check(lib().msparse_window_bwd(win, _starts(win, starts, dev), tq, tk, tv, _rows(out, "out", qs, dev),
-                                    _rows(dout, "dout", qs, dev), _arg(lse, "lse", qs[:3], _F32, dev),
-                                    _rows(dq, "dq", qs, dev), _rows(dk, "dk", ks, dev), _rows(dv, "dv", ks, dev),
+                                    _rows(dout, "dout", qs, dev), _arg(lse, "lse", qs[:3], _F32, dev), tdq, tdk, tdv,
                                     at, room, _current(dev)))
     return dq, dk, dv
 
@@ -536,8 +548,9 @@ def cache_append(cache: Cache, page_table, lens, k, v, q=None, inv_freq=None, co
         qs = (c.batch, heads_q, T, c.head_dim)
         tq = _rows(q, "q", qs, dev)
         if q_out is None:
-            q_out = torch.empty_like(q)
-        tqo = _rows(q_out, "q_out", qs, dev)
+            q_out, tqo = _like(q)
+        else:
+            tqo = _rows(q_out, "q_out", qs, dev)
     elif q_out is not None:
         _refuse("q_out without q")
     freq = None if inv_freq is None else _arg(inv_freq, "inv_freq", (c.head_dim // 2,), _F32, dev)
@@ -569,13 +582,16 @@ def cache_attn(cache: Cache, page_table, lens, q, window=0, sinks=0, scale=0.0, 
     qs = (c.batch, heads_q, T, c.head_dim)
     tq = _rows(q, "q", qs, dev)
     if out is None:
-        out = torch.empty_like(q)
+        out, to = _like(q)
+    else:
+        to = _rows(out, "out", qs, dev)
     if lse is None:
         lse = torch.empty(qs[:3], dtype=_F32, device=dev)
+        tl = lse.data_ptr()
+    else:
+        tl = _arg(lse, "lse", qs[:3], _F32, dev)
     workspace, at, room = _room(workspace, lib().msparse_cache_attn_workspace(c, heads_q, T), dev)
-    _check(lib().msparse_cache_attn(c, heads_q, T, window, sinks, scale, tq, _rows(out, "out", qs, dev),
-                                    _arg(lse, "lse", qs[:3], _F32, dev), at, room,
-                                    _current(dev)))
+    _check(lib().msparse_cache_attn(c, heads_q, T, window, sinks, scale, tq, to, tl, at, room, _current(dev)))
     return out, lse
 
 
