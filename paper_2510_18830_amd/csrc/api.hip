@@ -1007,8 +1007,9 @@ static size_t carve_cache_attn(const msparse_cache* c, const CacheAttnPlan& p, c
 size_t msparse_cache_attn_workspace(const msparse_cache* cache, int32_t heads_q, int32_t tokens) {
     if (check_cache(cache, heads_q, tokens) || tokens == 0) return 0;
     CacheAttnArgs a{};
-    return carve_cache_attn(cache, cache_attn_plan(cache->batch, heads_q, cache->heads_kv, tokens, cache->width), nullptr,
-                            &a);
+    const CacheAttnPlan p = cache_attn_plan(cache->batch, heads_q, cache->heads_kv, tokens, cache->width,
+                                            cache->head_dim, INT32_MAX, 0);
+    return carve_cache_attn(cache, p, nullptr, &a);
 }
 
 msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens, int32_t window,
@@ -1024,7 +1025,8 @@ msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, i
     if ((st = check_tensor(q, "q", B, heads_q, tokens, d, false))) return st;
     if ((st = check_tensor(out, "out", B, heads_q, tokens, d, true))) return st;
     if (misaligned({lse, ws})) return fail(MSPARSE_ERR_INVALID, "lse or workspace is not 16-byte aligned");
-    const CacheAttnPlan p = cache_attn_plan(B, heads_q, cache->heads_kv, tokens, cache->width);
+    const CacheAttnPlan p = cache_attn_plan(B, heads_q, cache->heads_kv, tokens, cache->width, d,
+                                            window == 0 ? INT32_MAX : window, window == 0 ? 0 : sinks);
     if (cache_attn_groups(p, B) > kMaxGroups / cache->heads_kv)
         return fail(MSPARSE_ERR_UNSUPPORTED, "%lld row tiles of %d heads", (long long)(B * p.tiles), cache->heads_kv);
     CacheAttnArgs a{};

@@ -81,10 +81,12 @@ struct CacheAttnPlan {
     int32_t rt, wr;         // 16-row tiles per wave; waves of a workgroup over rows (1: over pages)
     int32_t rows;           // rows of a workgroup
     int32_t tiles, items, chunk, per_tile, slots;
+    bool wide;              // a workgroup of many waves per tile
 };
 // workgroups per KV head
 inline int64_t cache_attn_groups(const CacheAttnPlan& p, int64_t B) { return p.slots > 0 ? p.slots : B * p.tiles; }
-CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width);
+CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width, int d, int64_t W,
+                              int64_t S);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 
 }  // namespace msparse

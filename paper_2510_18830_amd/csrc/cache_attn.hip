@@ -33,6 +33,7 @@ constexpr int kStages = 3;           // pages staged by the kernel for many rows
 constexpr int kThreads = 256;
 constexpr int64_t kManyRows = 2048;  // rows from which the join takes one per group of lanes
 constexpr int kMinChunk = 4;         // pages: one for each wave
+constexpr int kWideWaves = 16;       // of a wide workgroup: four a SIMD, what the registers of head dim 64 allow
 constexpr int64_t kLongTile = 128;   // pages that many workgroups take without a cut
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -425,17 +426,18 @@ __device__ __forceinline__ float lane_value(float x, int i) {
 // position of a page's first token; a page that the table does not have lies beyond every row
 __device__ __forceinline__ int page_start(int page, int index) { return page < 0 ? kMaxWidth * kPage : kPage * index; }
 
-// Up to 32 rows: the four waves share them and take pages in turn, straight from
+// Up to 32 rows: the WAVES waves share them and take pages in turn, straight from
 // memory to registers.  A page is read by one wave alone, once, hence past the
 // caches (a plain read reaches 7.0 TB/s that way against 6.1).
-template <int D, int RT>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 3 : 2, RT == 1 ? 3 : 2)))
-cache_attn_kernel(CacheAttnArgs a) {
+constexpr int per_simd(int RT, int waves) { return waves == kWideWaves ? 4 : RT == 1 ? 3 : 2; }
+template <int D, int RT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
+    __attribute__((amdgpu_waves_per_eu(per_simd(RT, WAVES), per_simd(RT, WAVES)))) cache_attn_kernel(CacheAttnArgs a) {
     constexpr int KL = CacheRows<D, RT>::KL, ND = CacheRows<D, RT>::ND, ROWS = 16 * RT;
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    __shared__ __attribute__((aligned(16))) float so[2][RT * ND * 4 * 64];
-    __shared__ float sml[2][RT][2][64];
+    __shared__ __attribute__((aligned(16))) float so[WAVES / 2][RT * ND * 4 * 64];
+    __shared__ float sml[WAVES / 2][RT][2][64];
     Walk k;
     if (!open_walk(a, ROWS, lane, k)) return;
     CacheRows<D, RT> st;
@@ -456,7 +458,7 @@ cache_attn_kernel(CacheAttnArgs a) {
             vr[y] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 16 * y * kPage));
     };
     // the next page's codes are requested as soon as this one's are used up
-    constexpr int STEP = kThreads / 64;
+    constexpr int STEP = WAVES;
     for (int x0 = k.c0 + w; x0 < k.c1; x0 += 64 * STEP) {
         const Pages pages = look_up(a, k, x0, STEP, lane);
         const int n = min((k.c1 - x0 + STEP - 1) / STEP, 64);
@@ -483,7 +485,7 @@ cache_attn_kernel(CacheAttnArgs a) {
 #pragma unroll
     for (int x = 0; x < RT; ++x) st.l[x] = row_sum(st.l[x]);
 #pragma unroll
-    for (int half = 2; half >= 1; half >>= 1) {
+    for (int half = WAVES / 2; half >= 1; half >>= 1) {
         if (w >= half && w < 2 * half) {
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
@@ -641,14 +643,20 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(CacheAttnArgs a, i
 }
 
 template <int D>
+void launch_wide(const CacheAttnArgs& a, dim3 g, hipStream_t s) {
+    if constexpr (D == 64) hipLaunchKernelGGL((cache_attn_kernel<64, 1, kWideWaves>), g, dim3(64 * kWideWaves), 0, s, a);
+}
+
+template <int D>
 void launch(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
     const int64_t wgs = cache_attn_groups(p, a.c.B) * a.c.Hkv;
     const dim3 g(static_cast<unsigned>(wgs)), t(kThreads);
     {
         TraceScope _t("cache_attn", s);
         if (p.wr == 4) hipLaunchKernelGGL((cache_attn_rows_kernel<D>), g, t, 0, s, a);
-        else if (p.rt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2>), g, t, 0, s, a);
-        else hipLaunchKernelGGL((cache_attn_kernel<D, 1>), g, t, 0, s, a);
+        else if (p.wide) launch_wide<D>(a, g, s);
+        else if (p.rt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2, 4>), g, t, 0, s, a);
+        else hipLaunchKernelGGL((cache_attn_kernel<D, 1, 4>), g, t, 0, s, a);
     }
     if (p.slots > 0) {
         TraceScope _t("cache_join", s);
@@ -663,19 +671,30 @@ void launch(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
 
 }  // namespace
 
-CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width) {
+CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width, int d, int64_t W, int64_t S) {
     CacheAttnPlan p{};
     const int64_t rows = Hq / Hkv * T;
     p.rt = rows <= 16 ? 1 : 2;
     p.wr = rows <= 32 ? 1 : 4;
     p.rows = 16 * p.rt * p.wr;
     p.tiles = int32_t((rows + p.rows - 1) / p.rows);
+    // the most pages that a tile sees: the window of its tokens, the sinks' (what a plan
+    // needs grows with them, so that one without a window has room for all)
+    const int64_t span = std::min(T, p.rows / (Hq / Hkv) + 2);
+    width = std::min(width, (W + span + 61) / kPage + 1 + (S + kPage - 1) / kPage);
     const int64_t e = B * p.tiles, groups = e * Hkv;
     // One chunk per row tile, where a cut would cost a short context more than it saves
     // (a join and half the walk: 64 contexts of 512 tokens, one KV head: 10.7 -> 8.7 us)
     p.per_tile = 1;
     p.chunk = INT32_MAX;
     if (width <= (p.wr == 4 ? kMinChunk : 2 * kMinChunk)) return p;
+    // Or one workgroup of many waves, up to one a CU, which joins its pages by itself
+    // (head dim 64, one to 16 rows; both in us, equal chunks -> this): one tile of 16 pages 9.2 ->
+    // 8.0, 32 9.1 -> 9.7, 64 9.2 -> 13.4; 128 tiles of 32 16.2 -> 12.1, 64 21.5 -> 18.1,
+    // 125 29.9 -> 29.7; 240 tiles (four waves each) of 32 14.4 -> 13.4, 64 27.4 -> 23.7.
+    // With eight waves at head dim 128, or of 32 rows, it loses from 16 pages on.
+    p.wide = d == 64 && p.rt == 1 && groups <= 256 && width <= (groups < 112 ? 2 * kWideWaves : kLongTile);
+    if (p.wide) return p;
     if (groups < (p.wr == 4 ? 512 : width <= kLongTile ? 192 : 560)) {
         // Few tiles: equal chunks whatever the raggedness (find_chunk).  Where rows bound
         // the work, as many as are resident at once (three workgroups a CU; 512, 768,

@@ -352,6 +352,7 @@ def _some_lens(seed, B, top):
 @pytest.mark.parametrize("B,Hq,Hkv,d,T,top,wide", [
     (150, 2, 1, 64, 1, 700, 0),      # equal chunks over more than 64 tiles
     (100, 4, 2, 128, 1, 600, 0),     # a workgroup per tile
+    (3, 4, 2, 64, 1, 2000, 0), (40, 12, 4, 64, 1, 3000, 0), (200, 16, 1, 64, 1, 1500, 0),   # one of many waves
     (800, 1, 1, 64, 1, 300, 150),    # chunks from the table's width, most tables half empty
     (30, 12, 4, 128, 2, 400, 130), (4200, 1, 1, 64, 1, 150, 0), (2, 20, 1, 128, 1, 9000, 0),
     (40, 4, 4, 64, 40, 500, 0), (70, 8, 2, 128, 70, 300, 140),
@@ -474,3 +475,23 @@ def test_cache_two_calls_at_once(gpu):
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,d,T,top,wide,W,S", [
+    (800, 1, 1, 64, 1, 700, 150, 200, 3), (10, 4, 2, 64, 1, 4000, 0, 300, 0), (10, 4, 2, 128, 1, 4000, 0, 1000, 70),
+    (220, 2, 1, 128, 1, 3000, 140, 700, 130), (9, 12, 4, 128, 3, 5000, 0, 64, 0), (20, 8, 1, 64, 60, 2500, 0, 500, 4),
+    (150, 8, 2, 128, 70, 1500, 200, 300, 0),
+])
+def test_attn_many_sequences_in_a_window(gpu, B, Hq, Hkv, d, T, top, wide, W, S):
+    """The window bounds the pages that are walked, and with them the split; the workspace is that of any window."""
+    lens = _some_lens(B, B, top)
+    cache, table, L = _filled(B, lens, Hkv, d, gpu)
+    if wide > table.shape[1]:
+        more = torch.full((B, wide), -1, dtype=torch.int32, device=gpu)
+        more[:, :table.shape[1]] = table
+        table = more
+    q = _randn(1, (B, Hq, T, d), gpu)
+    room = torch.empty(ms.cache_attn_workspace_bytes(cache, table, Hq, T), dtype=torch.uint8, device=gpu)
+    out, lse = ms.cache_attn(cache, table, L, q, window=W, sinks=S, workspace=room)
+    torch.cuda.synchronize()
+    _attn_check(q, out, lse, cache, table, lens, W, S)
