@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
                 for (int r = 0; r < 16; ++r) acc[x][r] += mine[(x * 16 + r) * 64 + lane];
         __syncthreads();
     }
-    if (rh != 0 || j > last || !live) return;
+    if (rh != 0 || j > last || !live || (far && j >= a.S)) return;
     if (far || group < p.part_groups) {
         const int64_t at = far ? int64_t(BK) * p.part_groups * p.near_slots + u
                                : (int64_t(bk) * p.part_groups + group) * p.near_slots + slot;
@@ -591,21 +591,21 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
 }
 
 // dK and dV of the keys of part_groups: the sums of their window's chunks, then, for
-// blocks of 64 keys with a sink, those of the rows beyond, in order.  A thread per 4
-// columns.
+// sinks, those of the rows beyond, in order.  A thread per 4 columns, which waits for
+// its loads kBatch at a time.
 constexpr int kSumThreads = 256;
 template <int D>
 __device__ __forceinline__ void add_slots(f32x4& sum, const float* p, int n) {
     constexpr int64_t kStep = 2 * 64 * kKeyBlocks<D> * D;
-    int s = 0;
-    for (; s + 8 <= n; s += 8) {
-        f32x4 x[8];
+    constexpr int kBatch = 16;
+    for (int s = 0; s < n; s += kBatch) {
+        f32x4 x[kBatch];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const f32x4*>(p + (s + u) * kStep);
+        for (int u = 0; u < kBatch; ++u)
+            x[u] = s + u < n ? *reinterpret_cast<const f32x4*>(p + (s + u) * kStep) : f32x4{};
 #pragma unroll
-        for (int u = 0; u < 8; ++u) sum += x[u];
+        for (int u = 0; u < kBatch; ++u) sum += x[u];
     }
-    for (; s < n; ++s) sum += *reinterpret_cast<const f32x4*>(p + s * kStep);
 }
 template <int D>
 __global__ void __launch_bounds__(kSumThreads) window_sums_kernel(WindowArgs a) {
@@ -625,7 +625,7 @@ __global__ void __launch_bounds__(kSumThreads) window_sums_kernel(WindowArgs a) 
     f32x4 sum = f32x4{};
     add_slots<D>(sum, part + int64_t(item) * p.near_slots * (2 * KEYS * D),
                  (G * (range.hi - range.lo + 1) + p.near_chunk - 1) / p.near_chunk);
-    if ((j & ~63) < a.S && group < p.sink_groups)
+    if (j < a.S && group < p.sink_groups)
         add_slots<D>(sum,
                      part + (int64_t(a.B) * a.Hkv * p.part_groups * p.near_slots +
                              (int64_t(bk) * p.sink_groups + group) * p.far_slots) * (2 * KEYS * D),
