@@ -989,8 +989,9 @@ msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q,
     const int64_t P = (int64_t(tokens) + 2 * kPage - 2) / kPage;   // the most pages that tokens in a row touch
     if (B * P > kMaxGroups / 2) return fail(MSPARSE_ERR_UNSUPPORTED, "%lld pages in one call", (long long)(B * P));
     a.P = int32_t(P);
-    a.kv_shares = append_shares(B * P, cache->heads_kv);
-    a.q_shares = q && B * P <= kAppendApart ? append_shares(B * P, heads_q) : 0;
+    share_heads(a, B * P);
+    if (B * P > 2 * kMaxGroups / (a.kv_shares + a.q_shares))   // (of 256 threads)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%lld pages of %d heads in one call", (long long)(B * P), heads_q);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return check_hip(launch_cache_append(a, s), s, "cache append");
 }

@@ -44,19 +44,32 @@ struct AppendArgs {
     const int32_t* counts;                    // [B] or NULL: T
     int32_t Hq, T;
     int32_t P;                                // pages that T tokens can touch
-    // workgroups that share a page's KV heads, and its query heads (0: the same ones)
+    // workgroups that share a page's KV heads, and its query heads
     int32_t kv_shares, q_shares;
 };
-// Workgroups that share a page's `heads`: as many as bring their grid to about one
-// a CU, a head in one of them.
-inline int32_t append_shares(int64_t pages, int64_t heads) {
-    return int32_t(std::max<int64_t>(1, std::min<int64_t>(heads, 256 / pages)));
+// Pairs of columns that a thread takes of a query token, and how many heads' queries a
+// workgroup turns side by side where the new tokens of a page are few.
+constexpr int kAppendThreads = 256;
+constexpr int query_chunks(int d) { return d / 16; }
+constexpr int heads_aside(int tokens, int d) {
+    return tokens * query_chunks(d) < kAppendThreads ? kAppendThreads / (tokens * query_chunks(d)) : 1;
 }
-// Pages up to which the queries have workgroups of their own: few pages wait for
-// latencies (6 ragged chunks of 501 tokens, 54 pages: 7.6 us, 9.6 with the queries
-// behind the keys; 64 pages of one token each: 8.3, 7.9), many for memory, where the
-// two kinds of work mix better in one (128K tokens, 2049 pages: 457, 431).
-constexpr int64_t kAppendApart = 512;
+// The shares of a page's heads, a workgroup each, keys and queries apart.  Of the keys'
+// heads two each and four shares at the least, more where the pages are few, of 32 heads
+// four each; of the queries' steps six each, fewer where the pages are few.  (35 calls of
+// 16 to 2049 pages with 1, 2, 4, 8, .. of the one and 0 to 32 of the other: these stay
+// within a tenth or so of each call's best.  A workgroup for both, at 576 pages of 28
+// over 4 heads 133 us, waits longer than two, 94; one of all heads of 128 sequences of
+// one token for eight heads in a row: 21 us, of two 15.)
+inline int even_shares(int64_t heads, int64_t shares) {
+    const int64_t each = (heads + shares - 1) / shares;
+    return int((heads + each - 1) / each);
+}
+inline void share_heads(AppendArgs& a, int64_t pages) {
+    const int64_t hkv = a.c.Hkv, aside = heads_aside(std::min(a.T, kPage), a.c.d), steps = (a.Hq + aside - 1) / aside;
+    a.kv_shares = even_shares(hkv, std::min(hkv, std::max({int64_t(4), hkv / 4, 600 / pages})));
+    a.q_shares = a.q ? even_shares(steps, std::min(steps, std::max((steps + 5) / 6, 512 / pages - a.kv_shares))) : 0;
+}
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 
 struct CacheAttnArgs {

@@ -6,11 +6,12 @@
 // position * freq[i].  A page's scale is the smallest power of two s with
 // max |x| <= 448 s over its tokens of the head, so moving codes to a larger scale
 // when later tokens need one is exact but for values that fall below e4m3's
-// normal range.  One workgroup per (sequence, page, share of the heads) owns the
-// page's codes and scales of its KV heads and computes the page's angles once for all
-// of its heads.  Bound by memory at long T, where q read and written dominates: 128K
-// tokens of 28 over 4 heads, 2.28 GB, take 431 us (a copy of q alone 358); q passes by
-// the caches (465 us through them).  Bound by latency at one token.
+// normal range.  A workgroup per (sequence, page, share of the KV heads) owns the
+// page's codes and scales of its heads, others turn shares of the query heads; each
+// computes the page's angles once for all of its heads.  Bound by memory at long T, where
+// q read and written dominates: 128K tokens of 28 over 4 heads, 2.28 GB, take 427 us (a
+// copy of q alone 358); q passes by the caches (465 us through them).  Bound by latency
+// at one token.
 #include "cache.h"
 #include "trace.h"
 
@@ -18,7 +19,7 @@ namespace msparse {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kAppendThreads;
 
 // cos and sin of pos * freq for any position: the angle in revolutions as a sum of
 // two doubles, reduced to an eighth of a revolution, then the Taylor series (their
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3
     __shared__ __attribute__((aligned(16))) uint8_t vt[D * (kPage + kPad)];
     __shared__ float red[2][kThreads / 64];
     const int tid = threadIdx.x, shares = a.kv_shares + a.q_shares;
-    int share = blockIdx.x % shares;
+    const int share = blockIdx.x % shares;
     const int p = blockIdx.x / shares % a.P;
     const int b = blockIdx.x / (shares * a.P);
     const int len = max(ldc(a.c.lens, b), 0);
@@ -144,13 +145,13 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3
     // The queries of every shares-th head: all T tokens, the count's and those behind
     // it alike.  A thread has 8 pairs of columns of a token (of QN tokens at head dim
     // 128) and walks the heads, the next one's loads in flight; `par` heads go side by
-    // side where the tokens are few.  done: the angles are there.
+    // side where the tokens are few.
     const int mq = a.q ? int(min(int64_t(len) + a.T - base, int64_t(kPage))) - s0 : 0;
-    auto queries = [&](int share, int shares, bool done) {
+    auto queries = [&](int share, int shares) {
         const int m = mq;
         if (m <= 0) return;
-        constexpr int QC = D / 16, QN = kPage * QC / kThreads;
-        const int combos = m * QC, par = max(kThreads / combos, 1);
+        constexpr int QC = query_chunks(D), QN = kPage * QC / kThreads;
+        const int combos = m * QC, par = heads_aside(m, D);
         const int heads = (a.Hq - share + shares - 1) / shares;
         const int h0 = par > 1 ? tid / combos : 0, x0 = par > 1 ? tid % combos : tid;
         const int c = x0 % QC;                     // (kThreads is a multiple of QC)
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3
                 }
         };
         load(h0);
-        if (!done) angles(m);
+        angles(m);
         for (int k = h0; k < heads; k += par) {
             u32x4 l[QN], r[QN];
 #pragma unroll
@@ -207,14 +208,13 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3
                 }
         }
     };
-    if (share >= a.kv_shares) return queries(share - a.kv_shares, a.q_shares, false);
-    const bool both = a.q_shares == 0;   // this workgroup has queries too
+    if (share >= a.kv_shares) return queries(share - a.kv_shares, a.q_shares);
     // ---- K and V of this share's heads
     const int cnt = a.counts ? min(max(ldc(a.counts, b), 0), a.T) : a.T;
     const int s1 = int(min(int64_t(len) + cnt - base, int64_t(kPage)));   // slots [s0, s1) are new
     const int m = s1 - s0;
     const int page = m > 0 ? cache_page(a.c, b, lp) : -1;
-    if (page < 0) return both ? queries(share, a.kv_shares, false) : void();
+    if (page < 0) return;
     // K: columns 4 c .. 4 c + 3 of either half; V: columns 8 c .. 8 c + 7
     const int c = tid % C, r0 = tid / C;
     u32x2 klo[N], khi[N];
@@ -235,8 +235,8 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3
             }
         }
     };
-    if (share < a.c.Hkv) load(share);
-    angles(both ? max(m, mq) : m);
+    load(share);
+    angles(m);
     for (int hk = share; hk < a.c.Hkv; hk += a.kv_shares) {
         const int64_t at = int64_t(page) * a.c.Hkv + hk;
         uint8_t* kc = a.c.k + at * (kPage * D);
@@ -334,7 +334,6 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3
         }
         __syncthreads();   // vt and red are read
     }
-    if (both) queries(share, a.kv_shares, true);
 }
 
 }  // namespace

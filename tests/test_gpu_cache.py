@@ -410,7 +410,7 @@ def test_attn_many_rows_in_chunks(gpu, Hq, Hkv, d, T, L):
 @pytest.mark.parametrize("B,Hq,Hkv,d,T,ragged", [(300, 3, 1, 64, 3, True), (1, 2, 1, 128, 36000, False),
                                                  (260, 2, 2, 128, 1, False)])
 def test_append_of_many_pages(gpu, B, Hq, Hkv, d, T, ragged):
-    """Queries behind the keys in the same workgroups."""
+    """Several heads in a workgroup, and many pages."""
     rng = np.random.default_rng(T)
     lens = [int(x) for x in rng.integers(0, 130, B)]
     counts = [int(x) for x in rng.integers(0, T + 1, B)] if ragged else None
