@@ -841,7 +841,7 @@ static WindowArgs window_args(const msparse_window* w, const int32_t* starts) {
 // lse log2(e) and Delta of every row, the keys' partial gradients.
 static size_t carve_window_bwd(WindowArgs* a, char* base) {
     const int keys = window_key_group(a->d);
-    const KeyPlan& p = a->plan = key_plan(a->B, a->Hkv, a->Hq / a->Hkv, a->seq, a->W, a->S, keys,
+    const KeyPlan& p = a->plan = key_plan(a->B, a->Hkv, a->Hq / a->Hkv, a->seq, a->tokens, a->W, a->S, a->d, keys,
                                           window_key_resident(a->d));
     const int64_t slots = int64_t(p.part_groups) * p.near_slots + int64_t(p.sink_groups) * p.far_slots;
     a->rows_pad = a->tokens > 0 ? padded_rows(a->tokens) + 64 * (int64_t(a->B) + 1) : a->B * padded_rows(a->seq);

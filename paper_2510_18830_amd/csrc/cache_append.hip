@@ -108,7 +108,8 @@ struct Split {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, D == 128 ? 3 : 4))) cache_append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, D == 128 ? 3 : 4)))
+cache_append_kernel(AppendArgs a) {
     constexpr int H2 = D / 2, C = Split<D>::C, R = Split<D>::R, N = Split<D>::N;
     constexpr int kPad = 16;                       // V tile rows: 64 codes + pad
     __shared__ __attribute__((aligned(16))) float cosv[kPage * H2], sinv[kPage * H2];

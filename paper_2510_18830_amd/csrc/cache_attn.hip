@@ -644,7 +644,8 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(CacheAttnArgs a, i
 
 template <int D>
 void launch_wide(const CacheAttnArgs& a, dim3 g, hipStream_t s) {
-    if constexpr (D == 64) hipLaunchKernelGGL((cache_attn_kernel<64, 1, kWideWaves>), g, dim3(64 * kWideWaves), 0, s, a);
+    if constexpr (D == 64)
+        hipLaunchKernelGGL((cache_attn_kernel<64, 1, kWideWaves>), g, dim3(64 * kWideWaves), 0, s, a);
 }
 
 template <int D>
@@ -671,7 +672,8 @@ void launch(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
 
 }  // namespace
 
-CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width, int d, int64_t W, int64_t S) {
+CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width, int d, int64_t W,
+                              int64_t S) {
     CacheAttnPlan p{};
     const int64_t rows = Hq / Hkv * T;
     p.rt = rows <= 16 ? 1 : 2;

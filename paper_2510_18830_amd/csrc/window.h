@@ -27,25 +27,41 @@ struct RowView {
     int64_t batch, head, token;
 };
 
+// Blocks of `rows` rows that one head's sequences have, at most (packed: fewer than the
+// grid's, which has room for `seq` rows in every sequence).
+inline int64_t row_blocks(int64_t B, int64_t seq, int64_t tokens, int64_t rows) {
+    const int64_t all = B * ((seq + rows - 1) / rows);
+    return tokens > 0 ? std::min(all, tokens / rows + B) : all;
+}
+
 // The key-major backward's workgroups for a group of keys: near_slots for the query
 // tiles of its window (every head of the KV group: near_chunk of them each), and for
 // one with sinks far_slots for the tiles beyond (far_chunk each, no more than a
 // window's: 8 heads x 2048, window 256, sinks 4, head dim 128: dK / dV 34 us with 16
 // tiles each, 24 with 6).  A group with more than one leaves partial sums: those with
-// sinks, or, where windows are cut too, all of them.  Windows are cut, into 8 tiles at
-// least, while all workgroups are resident at once (`resident`), which pays for the
-// sums: dK / dV and sums 36 -> 30 us for 8 x 1024 causal (64 groups), 58 -> 48 for 8 x
-// 2048 (128); beyond that it costs: 16 x 2048 (256 groups, cut in two) 61 -> 85.
+// sinks, or, where windows are cut too, all of them.
 struct KeyPlan {
     int32_t near_slots, near_chunk, sink_groups, far_slots, far_chunk, part_groups;
 };
-inline KeyPlan key_plan(int64_t B, int64_t Hkv, int64_t G, int64_t seq, int64_t W, int64_t S, int64_t keys,
-                        int64_t resident) {
+// Windows are cut, into 8 tiles at least:
+//   d 64    while all workgroups are resident at once, three a CU, which pays for the sums
+//           (dK / dV and sums 36 -> 30 us for 8 x 1024 causal, 64 groups; 58 -> 48 for 8 x
+//           2048); beyond that it costs (16 x 2048, 256 groups at head dim 128: 61 -> 85)
+//   d 128   one workgroup a CU walks alone, so where that shortens the longest walk by
+//           more than the further starts and the partial sums cost, by a model of the time
+//           of sequences of the mean length: the longest walk, or all walks over the CUs
+//           and a last round, kStart steps (a tile each) for each workgroup's start, kStep
+//           us a step; the sums a launch and their bytes twice at 4 TB/s (backward in us,
+//           cut while all are resident -> by the model: 16 over 2 heads x 8192 causal 1135 ->
+//           1015, 28 over 4 x 4096 529 -> 491, 5 documents of 8000 tokens together of 8 over 2
+//           heads 342 -> 261; 10 of 3563 of 12 over 4 84 -> 88)
+inline KeyPlan key_plan(int64_t B, int64_t Hkv, int64_t G, int64_t seq, int64_t tokens, int64_t W, int64_t S, int d,
+                        int64_t keys, int64_t resident) {
     KeyPlan p{1, 1, 0, 0, 1, 0};
     if (seq <= 0) return p;
     const int64_t tiles = (seq + 63) / 64, groups = (seq + keys - 1) / keys, bk = B * Hkv;
-    const int64_t walk = G * std::min(tiles, (keys + W - 2) / 64 + 1);   // query tiles of a group's window
-    const int64_t first = W / 64;             // the rows of tiles before are inside the window of key 0
+    const int64_t wide = std::min(tiles, (keys + W - 2) / 64 + 1);   // query tiles of a group's window and head
+    const int64_t walk = G * wide, first = W / 64;   // (the rows of tiles before are inside the window of key 0)
     if (S > 0 && W < seq && first < tiles) {
         p.sink_groups = p.part_groups = int32_t((std::min(S, seq) + keys - 1) / keys);
         const int64_t beyond = G * (tiles - first);      // query tiles beyond a group's window, at most
@@ -53,14 +69,41 @@ inline KeyPlan key_plan(int64_t B, int64_t Hkv, int64_t G, int64_t seq, int64_t 
         p.far_chunk = int32_t(std::max(std::min<int64_t>(16, walk), (beyond + items - 1) / items));
         p.far_slots = int32_t((beyond + p.far_chunk - 1) / p.far_chunk);
     }
-    const int64_t room = resident - bk * p.sink_groups * p.far_slots;
-    const int64_t cuts = std::min(room / (bk * groups), walk / 8);
     p.near_chunk = int32_t(walk);
-    if (cuts > 1) {
-        p.near_chunk = int32_t((walk + cuts - 1) / cuts);
-        p.near_slots = int32_t((walk + p.near_chunk - 1) / p.near_chunk);
-        p.part_groups = int32_t(groups);
+    // (the grid and the partial sums have room for `seq` keys in every sequence)
+    const int64_t most = std::min(walk / 8, 16 * resident / (bk * groups));
+    if (d == 64) {
+        const int64_t room = resident - bk * p.sink_groups * p.far_slots;
+        const int64_t cuts = std::min(room / (Hkv * row_blocks(B, seq, tokens, keys)), most);
+        if (cuts > 1) p.near_chunk = int32_t((walk + cuts - 1) / cuts);
+    } else {
+        const int64_t length = tokens > 0 ? std::min(seq, (tokens + B - 1) / B) : seq;   // of the mean sequence
+        const int64_t n = (length + keys - 1) / keys, last = (length + 63) / 64;
+        const double kStep = 1.8, kStart = 8, part_us = double(2 * 2 * keys * d * 4) / 4e6;
+        const int64_t far = bk * p.sink_groups * G * std::max<int64_t>(last - first, 0);
+        double best = 0;
+        for (int64_t cuts = 1; cuts <= std::min<int64_t>(most, 8) && bk * n <= 4 * resident; ++cuts) {
+            const int64_t chunk = (walk + cuts - 1) / cuts;
+            int64_t chunks = 0, total = far;
+            for (int64_t g = 0; g < n; ++g) {
+                const int64_t steps = G * std::min(wide, last - g * keys / 64);
+                chunks += bk * ((steps + chunk - 1) / chunk);
+                total += bk * steps;
+            }
+            double steps = (double(total) + kStart * double(chunks)) / double(resident);
+            // a last round, of the last groups' walks (from 85 % on, as XCDs get uneven numbers)
+            const int64_t late = G * std::min(wide, last - n * 3 / 4 * keys / 64);
+            if (20 * chunks > 17 * resident) steps += double(std::min(chunk, late));
+            const double us = std::max(steps, double(chunk) + kStart) * kStep +
+                              (cuts > 1 ? 7 + part_us * double(chunks) : 0.0);
+            if (cuts == 1 || us < best) {
+                best = cuts == 1 ? 0.95 * us : us;
+                p.near_chunk = int32_t(chunk);
+            }
+        }
     }
+    p.near_slots = int32_t((walk + p.near_chunk - 1) / p.near_chunk);
+    if (p.near_slots > 1) p.part_groups = int32_t(groups);
     return p;
 }
 

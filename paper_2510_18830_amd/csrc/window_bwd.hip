@@ -25,7 +25,7 @@ namespace {
 
 // ------------------------------------------------------------------ dQ
 constexpr int kDqThreads = 256, kDqRows = 128;
-// Grids of 128-row workgroups up to which the split kernel runs (both in us, 128
+// Workgroups of 128 rows up to which the split kernel runs (both in us, 128
 // rows -> split; heads x tokens, window):
 //   d 128   28 (4 x 777, 256): 29 -> 17.5; 128: 41 -> 36 (4 x 4096, 1024), 57 -> 45 (8 x
 //           2048, all); 192: 31 -> 42 (12 x 2048, 512); 256: 33 -> 42
@@ -648,7 +648,8 @@ hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s) {
     {
         TraceScope _t("window_dq", s);
         const int64_t heads = int64_t(a.B) * a.Hq, grid = heads * ((a.seq + kDqRows - 1) / kDqRows);
-        const bool split = grid <= (wide ? kSplitGrid<128> : kSplitGrid<64>);
+        const int64_t most = wide ? kSplitGrid<128> : kSplitGrid<64>;
+        const bool split = a.Hq * row_blocks(a.B, a.seq, a.tokens, kDqRows) <= most;
         const dim3 g(unsigned(split ? heads * ((a.seq + 63) / 64) : grid)), t(kDqThreads);
         if (split && wide) hipLaunchKernelGGL(window_dq_split_kernel<128>, g, t, 0, s, a);
         else if (split) hipLaunchKernelGGL(window_dq_split_kernel<64>, g, t, 0, s, a);
@@ -669,7 +670,8 @@ hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.plan.part_groups > 0) {
         TraceScope _t("window_sums", s);
-        const dim3 g(unsigned(bk * a.plan.part_groups * (2 * window_key_group(a.d) * a.d / 4 / kSumThreads))), t(kSumThreads);
+        const int per = 2 * window_key_group(a.d) * a.d / 4 / kSumThreads;   // workgroups per group
+        const dim3 g(unsigned(bk * a.plan.part_groups * per)), t(kSumThreads);
         if (wide) hipLaunchKernelGGL(window_sums_kernel<128>, g, t, 0, s, a);
         else hipLaunchKernelGGL(window_sums_kernel<64>, g, t, 0, s, a);
     }

@@ -23,7 +23,7 @@ namespace {
 constexpr float kSlack = 8.f;        // log2 units
 constexpr int kFwdRows = 128;        // query rows per workgroup
 constexpr int kFwdThreads = 256;
-// Grids of 128-row workgroups up to which the split kernel runs instead (both in us,
+// Workgroups of 128 rows up to which the split kernel runs instead (both in us,
 // 128 rows -> split; heads x tokens, window):
 //   d 128   28 (4 x 777, 256): 16.7 -> 11.8; 128: 33.2 -> 25.9 (4 x 4096, 1024), 46.6 ->
 //           35.9 (8 x 2048, all); 192: 23.9 -> 31.8 (12 x 2048, 512); 256: 25.2 -> 32.8
@@ -301,7 +301,8 @@ window_fwd_split_kernel(WindowArgs a) {
 
 hipError_t launch_window_fwd(const WindowArgs& a, hipStream_t s) {
     const int64_t heads = int64_t(a.B) * a.Hq, grid = heads * ((a.seq + kFwdRows - 1) / kFwdRows);
-    const bool split = grid <= (a.d == 128 ? kSplitGrid<128> : kSplitGrid<64>);
+    const int64_t most = a.d == 128 ? kSplitGrid<128> : kSplitGrid<64>;
+    const bool split = a.Hq * row_blocks(a.B, a.seq, a.tokens, kFwdRows) <= most;
     TraceScope _t("window_fwd", s);
     const dim3 g(unsigned(split ? heads * ((a.seq + 63) / 64) : grid)), t(kFwdThreads);
     if (split && a.d == 128) hipLaunchKernelGGL(window_fwd_split_kernel<128>, g, t, 0, s, a);

@@ -347,3 +347,21 @@ def test_window_two_calls_at_once(gpu):
         for a, b, c in zip(got, want, outs):
             for x, y, z in zip(a, b, c):
                 assert torch.equal(x, y) and torch.equal(z, y)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,d,W,S", [
+    ([900, 0, 1700, 300], 4, 1, 128, 0, 0), ([2500, 40, 700], 2, 2, 64, 0, 0), ([1300, 1000], 14, 2, 128, 800, 4),
+])
+def test_window_packed_keys_in_several_walks(gpu, lens, Hq, Hkv, d, W, S):
+    """Documents whose key groups' walks are cut for the mean one."""
+    starts = torch.tensor([0] + lens).cumsum(0).to(torch.int32)
+    total = int(starts[-1])
+    q, k, v, do = _inputs(total, 1, Hq, Hkv, total, d, gpu)
+    win = ms.make_window(len(lens), max(lens), Hq, Hkv, d, W, S, tokens=total)
+    st = starts.to(gpu)
+    out, lse = ms.window_fwd(win, q, k, v, starts=st)
+    grads = ms.window_bwd(win, q, k, v, out, do, lse, starts=st)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        if n:
+            _check(q, k, v, do, out, lse, grads, W, S, d ** -0.5, int(starts[b]), n)
