@@ -16,7 +16,7 @@
 // One token per sequence is bound by the cache's bytes: waves walk pages with the
 // next page's loads in flight, and long contexts are cut into chunks of equal
 // length whatever the batch's raggedness, joined by a second launch: 8 contexts of
-// 13K to 128K tokens x 8 heads (1.3 GB) take 208 us, 6.2 TB/s; the join 7 us.  Many
+// 13K to 128K tokens x 8 heads (1.32 GB) take 208 us, 6.4 TB/s; the join 5 us.  Many
 // rows are bound by the products, conversions and exponentials: four waves take rows
 // of their own over the same pages, 770 TFLOP/s in the walk.
 #include "cache.h"
