@@ -17,8 +17,9 @@
 // next page's loads in flight, and long contexts are cut into chunks of equal
 // length whatever the batch's raggedness, joined by a second launch: 8 contexts of
 // 13K to 128K tokens x 8 heads (1.32 GB) take 208 us, 6.4 TB/s; the join 5 us.  Many
-// rows are bound by the products, conversions and exponentials: four waves take rows
-// of their own over the same pages, 770 TFLOP/s in the walk.
+// rows are bound by the products and exponentials: four waves take 32 rows each over
+// the same pages, whose codes are converted once for all of them (4 x 200 tokens of 16
+// over 2 heads in a window of 4096: 52 us and the join's 10).
 #include "cache.h"
 #include "tiles.h"
 #include "trace.h"
@@ -29,11 +30,12 @@ namespace msparse {
 
 namespace {
 
-constexpr int kStages = 3;           // pages staged by the kernel for many rows
 constexpr int kThreads = 256;
 constexpr int64_t kManyRows = 2048;  // rows from which the join takes one per group of lanes
 constexpr int kMinChunk = 4;         // pages: one for each wave
 constexpr int kWideWaves = 16;       // of a wide workgroup: four a SIMD, what the registers of head dim 64 allow
+// workgroups of the kernel for many rows that run at once: two or three a CU
+constexpr int64_t kRowsResident(int d) { return d == 128 ? 512 : 768; }
 constexpr int64_t kLongTile = 128;   // pages that many workgroups take without a cut
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -111,29 +113,55 @@ __device__ __forceinline__ PageList tile_pages(const CacheAttnArgs& a, const Til
 struct Chunk {
     int32_t e, first, count, index, pages;
 };
-// With few tiles their pages are cut into chunks of one length, from the sum over all
-// tiles and the number of chunks aimed at, so that whatever the raggedness the
-// workgroups take as long.  False past the last chunk.  Every wave finds its own.
+// With few tiles (up to kMaxTiles) their pages are cut into chunks of one length, the
+// smallest found that makes no more than `items` of them, so that whatever the raggedness
+// the workgroups take as long and run at once; or twice as many in two rounds, where one
+// leaves many places empty (5 x 200 tokens of 32 over 4 heads at 8192, 65 tiles for 128
+// places: 324 -> 252 us).  False past the last chunk.  Every wave finds its own.
+constexpr uint32_t kStartPages = 3;   // what a workgroup's start costs, in pages
+constexpr int kMaxTiles = 9 * 64;
 __device__ __forceinline__ bool find_chunk(const CacheAttnArgs& a, int rows, int item, int lane, Chunk& out) {
     const int E = a.c.B * a.tiles;
-    auto pages_of = [&](int e) {
-        return e < E ? tile_pages(a, tile_rows(a, e / a.tiles, e % a.tiles, rows)).count : 0;
-    };
-    const int own = pages_of(lane);   // the first 64 tiles are looked up once
-    int sum = own;
-    for (int e = 64 + lane; e < E; e += 64) sum += pages_of(e);
+    uint32_t np[kMaxTiles / 64];   // of the tiles lane, lane + 64, ..
+    int sum = 0;
+#pragma unroll
+    for (int t = 0; t < kMaxTiles / 64; ++t) {
+        const int e = 64 * t + lane;
+        np[t] = 0;
+        if (64 * t >= E) continue;
+        np[t] = e < E ? tile_pages(a, tile_rows(a, e / a.tiles, e % a.tiles, rows)).count : 0;
+        sum += np[t];
+    }
     const uint32_t total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
-    const uint32_t pages = max((total + a.items - 1) / a.items, uint32_t(kMinChunk));
+    uint32_t pages = 0;
+    auto chunks_of = [&](int t) { return 64 * t + lane < E ? max(int((np[t] + pages - 1) / pages), 1) : 0; };
+    auto fit = [&](int most) {   // into `most` chunks (E <= most: one each in the end)
+        for (pages = max((total + most - 1) / most, uint32_t(kMinChunk));; pages += max(pages / 16, 1u)) {
+            if (E == 1) return;
+            int n = 0;
+#pragma unroll
+            for (int t = 0; t < kMaxTiles / 64; ++t)
+                if (64 * t < E) n += chunks_of(t);
+            if (__builtin_amdgcn_readlane(wave_scan(n), 63) <= most) return;
+        }
+    };
+    fit(a.items);
+    if (a.slots > a.items && 10 * pages > 13 * (total / a.items)) {
+        const uint32_t one = pages;
+        fit(2 * a.items);
+        if (2 * (pages + kStartPages) > one) pages = one;
+    }
     int base = 0;
-    for (int e0 = 0; e0 < E; e0 += 64) {
-        const uint32_t np = e0 == 0 ? own : pages_of(e0 + lane);
-        const int n = e0 + lane < E ? max(int((np + pages - 1) / pages), 1) : 0;
+#pragma unroll
+    for (int t = 0; t < kMaxTiles / 64; ++t) {
+        if (64 * t >= E) break;
+        const int n = chunks_of(t);
         const int last = base + wave_scan(n);   // chunks up to this tile's end
         const uint64_t beyond = __ballot(item < last);
         if (beyond) {
             const int l = __builtin_ctzll(beyond);
             const int first = __builtin_amdgcn_readlane(last - n, l);
-            out = Chunk{e0 + l, first, __builtin_amdgcn_readlane(n, l), item - first, int32_t(pages)};
+            out = Chunk{64 * t + l, first, __builtin_amdgcn_readlane(n, l), item - first, int32_t(pages)};
             return true;
         }
         base = __builtin_amdgcn_readlane(last, 63);
@@ -211,11 +239,19 @@ __device__ __forceinline__ bool partly(int t0, int wp0, int wp1, int W, int S) {
     return !(t0 <= wp0 - 63 && (t0 > wp1 - W || t0 < S - 63));
 }
 
-// One page, its first token at position t0: key(t, j) and value(y) give this lane's
-// operands; keys_done() runs once the keys are used up, and clear(t0) before the
-// values of a page are that some row does not see in full: it clears the codes of
-// the tokens that no row sees.
-template <int D, int RT, int TS, int YS, class Key, class Value, class Done, class Clear>
+// Half p of a 16-token or 16-column operand: its codes converted, or read as bf16.
+template <int PARTS>
+__device__ __forceinline__ u32x4 operand(const u32x4* x, int p) {
+    if constexpr (PARTS == 2) return x[p];
+    const uint32_t lo = x[0][2 * p], hi = x[0][2 * p + 1];
+    return codes_to_bf16(lo, hi);
+}
+
+// One page, its first token at position t0: key(t, j, p) and value(y, p) give this lane's
+// operands, 16 codes (PARTS 1) or their halves as bf16 (2); keys_done() runs once the
+// keys are used up, and clear(t0) before the values of a page are that some row does not
+// see in full: it clears the codes of the tokens that no row sees.
+template <int D, int RT, int TS, int YS, int PARTS, class Key, class Value, class Done, class Clear>
 __device__ __forceinline__ void page_step(CacheRows<D, RT>& st, int t0, float kscale, float vscale, int W, int S,
                                           int lane, Key key, Value value, Done keys_done, Clear clear) {
     constexpr int KL = CacheRows<D, RT>::KL, ND = CacheRows<D, RT>::ND;
@@ -225,12 +261,14 @@ __device__ __forceinline__ void page_step(CacheRows<D, RT>& st, int t0, float ks
     // the accumulators of a group take turns, as an MFMA that adds to the one before
     // it waits for it
     f32x4 s[RT][4];
-    u32x4 kb[2][TS][KL];
+    u32x4 kb[2][TS][KL][PARTS];
     auto read_k = [&](int set, int t) {
 #pragma unroll
         for (int i = 0; i < TS; ++i)
 #pragma unroll
-            for (int j = 0; j < KL; ++j) kb[set][i][j] = key(t + i, j);
+            for (int j = 0; j < KL; ++j)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) kb[set][i][j][p] = key(t + i, j, p);
     };
     read_k(0, 0);
 #pragma unroll
@@ -248,8 +286,7 @@ __device__ __forceinline__ void page_step(CacheRows<D, RT>& st, int t0, float ks
             for (int p = 0; p < 2; ++p)
 #pragma unroll
                 for (int i = 0; i < TS; ++i) {
-                    const uint32_t k0 = kb[set][i][j][2 * p], k1 = kb[set][i][j][2 * p + 1];
-                    const u32x4 k = codes_to_bf16(k0, k1);
+                    const u32x4 k = operand<PARTS>(kb[set][i][j], p);
 #pragma unroll
                     for (int x = 0; x < RT; ++x) s[x][t + i] = mfma16(k, st.q[x][2 * j + p], s[x][t + i]);
                 }
@@ -305,10 +342,12 @@ __device__ __forceinline__ void page_step(CacheRows<D, RT>& st, int t0, float ks
         st.l[x] += sum;
     }
     // ---- O^T, YS column tiles at a time, likewise
-    u32x4 vb[2][YS];
+    u32x4 vb[2][YS][PARTS];
     auto read_v = [&](int set, int y) {
 #pragma unroll
-        for (int i = 0; i < YS; ++i) vb[set][i] = value(y + i);
+        for (int i = 0; i < YS; ++i)
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) vb[set][i][p] = value(y + i, p);
     };
     read_v(0, 0);
 #pragma unroll
@@ -320,8 +359,7 @@ __device__ __forceinline__ void page_step(CacheRows<D, RT>& st, int t0, float ks
         for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int i = 0; i < YS; ++i) {
-                const uint32_t v0 = vb[set][i][2 * p], v1 = vb[set][i][2 * p + 1];
-                const u32x4 v = codes_to_bf16(v0, v1);
+                const u32x4 v = operand<PARTS>(vb[set][i], p);
 #pragma unroll
                 for (int x = 0; x < RT; ++x) st.o[x][y + i] = mfma16(v, pb[x][p], st.o[x][y + i]);
             }
@@ -466,10 +504,10 @@ __global__ void __launch_bounds__(64 * WAVES)
         load_v(page_at(pages, 0));
         for (int i = 0; i < n; ++i) {
             const int next = page_at(pages, min(i + 1, 63));
-            page_step<D, RT, RT == 1 ? 2 : 1, RT == 1 ? 4 : 2>(
+            page_step<D, RT, RT == 1 ? 2 : 1, RT == 1 ? 4 : 2, 1>(
                 st, page_start(page_at(pages, i), k.pl.page(x0 + i * STEP)), lane_value(pages.ks, i),
-                lane_value(pages.vs, i), a.W, a.S, lane, [&](int t, int j) { return kr[t][j]; },
-                [&](int y) { return vr[y]; },
+                lane_value(pages.vs, i), a.W, a.S, lane, [&](int t, int j, int) { return kr[t][j]; },
+                [&](int y, int) { return vr[y]; },
                 [&] {
                     if (i + 1 < n) load_k(next);
                 },
@@ -518,15 +556,17 @@ __global__ void __launch_bounds__(64 * WAVES)
 }
 
 // More rows: each of the four waves takes 32 of its own through all pages of the
-// chunk.  A page is staged once for the workgroup, by direct global->LDS loads in
-// the order of the operands (a lane fetches what it would read itself), with the
-// loads of the next pages in flight.
+// chunk.  A page is read and converted once for the workgroup, a quarter a wave: from
+// memory to registers two pages ahead, to bf16 operands in LDS one ahead.  (Codes staged
+// in LDS and converted by every wave, which leaves room for three workgroups a CU: 14 x
+// 127 tokens of 32 over 8 heads at 4551 270 us, so 194; 4 x 200 in a window 67, 62; 16384
+// at 20480 3.52 ms, 3.63.)
 template <int D>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3)))
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3)))
 cache_attn_rows_kernel(CacheAttnArgs a) {
     constexpr int RT = 2, KL = CacheRows<D, RT>::KL, ND = CacheRows<D, RT>::ND, ROWS = 16 * RT * 4;
-    constexpr int kOps = 4 * KL + ND;              // operands of a page, 1 KB each
-    __shared__ __attribute__((aligned(16))) uint16_t buf[kStages][kOps * 512];
+    constexpr int kOps = 4 * KL + ND, NV = ND / 4;   // operands of a page, 2 KB of bf16 each
+    __shared__ __attribute__((aligned(16))) u32x4 buf[2][kOps][2][64];   // [page][operand][half][lane]
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Walk k;
@@ -535,47 +575,54 @@ cache_attn_rows_kernel(CacheAttnArgs a) {
     CacheRows<D, RT> st;
     open_rows(a, st, k.b, k.hk, k.tr.len, wr0, lane);
     const bool live = wr0 < a.T * (a.Hq / a.c.Hkv);
-    constexpr int kLoads = KL + ND / 4;            // a wave's loads of a page
-    auto stage = [&](int slot, int page) {
+    u32x4 kr[KL], vr[NV];   // this wave's codes of a page: the keys of the token tile w, the columns w, w + 4, ..
+    auto load = [&](int page) {
         const int64_t at = (int64_t(max(page, 0)) * a.c.Hkv + k.hk) * (kPage * D);
-        const uint8_t* kp = a.c.k + at + key_offset(w, 0, lane, D);   // wave w: the token tile w
+        const uint8_t* kp = a.c.k + at + key_offset(w, 0, lane, D);
 #pragma unroll
-        for (int j = 0; j < KL; ++j) dma16(kp + 64 * j, lds_addr(&buf[slot][(w * KL + j) * 512]));
-        const uint8_t* vp = a.c.v + at + value_offset(w, lane);       // columns w, w + 4, ...
+        for (int j = 0; j < KL; ++j) kr[j] = *reinterpret_cast<const u32x4*>(kp + 64 * j);
+        const uint8_t* vp = a.c.v + at + value_offset(w, lane);
 #pragma unroll
-        for (int y = 0; y < ND / 4; ++y) dma16(vp + 64 * y * kPage, lds_addr(&buf[slot][(4 * KL + w + 4 * y) * 512]));
+        for (int y = 0; y < NV; ++y) vr[y] = *reinterpret_cast<const u32x4*>(vp + 64 * y * kPage);
+    };
+    auto convert = [&](u32x4 (*b)[2][64], int t0) {
+        if (partly(t0, k.tr.p0, k.tr.p1, a.W, a.S)) {
+            keep_branch();
+            const u32x4 keep = seen_bytes(t0, k.tr.p1, max(k.tr.p0, 0) - a.W, a.S, lane);
+#pragma unroll
+            for (int y = 0; y < NV; ++y) vr[y] &= keep;
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+#pragma unroll
+            for (int j = 0; j < KL; ++j) b[w * KL + j][p][lane] = operand<1>(&kr[j], p);
+#pragma unroll
+            for (int y = 0; y < NV; ++y) b[4 * KL + w + 4 * y][p][lane] = operand<1>(&vr[y], p);
+        }
     };
     for (int x0 = k.c0; x0 < k.c1; x0 += 64) {
         const Pages pages = look_up(a, k, x0, 1, lane);
         const int n = min(k.c1 - x0, 64);
+        auto start = [&](int i) { return page_start(page_at(pages, i), k.pl.page(x0 + i)); };
         // every page of the 64 before has been read: its last step ended with a barrier
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i)
-            if (i < n) stage(i, page_at(pages, i));
-        for (int i = 0; i < n; ++i) {
-            // page i has landed when only the loads of the pages behind it are out
-            if (i + kStages - 1 <= n) __builtin_amdgcn_s_waitcnt(0x0F70 | (kLoads * (kStages - 2)));
-            else wait_vmem();
-            const int t0 = page_start(page_at(pages, i), k.pl.page(x0 + i));
-            if (partly(t0, k.tr.p0, k.tr.p1, a.W, a.S)) {   // each wave clears what it staged
-                keep_branch();
-                const u32x4 keep = seen_bytes(t0, k.tr.p1, max(k.tr.p0, 0) - a.W, a.S, lane);
-                u32x4* v = reinterpret_cast<u32x4*>(buf[i % kStages] + (4 * KL + w) * 512) + lane;
-#pragma unroll
-                for (int y = 0; y < ND / 4; ++y) v[4 * y * 64] &= keep;
-            }
-            __syncthreads();
-            if (i + kStages - 1 < n) stage((i + kStages - 1) % kStages, page_at(pages, i + kStages - 1));
-            const uint16_t* cur = buf[i % kStages];
-            if (live && t0 <= st.wp1 && (t0 + 63 > st.far || t0 < a.S))
-                page_step<D, RT, 1, 2>(
-                    st, t0, lane_value(pages.ks, i), lane_value(pages.vs, i), a.W, a.S, lane,
-                    [&](int t, int j) { return *reinterpret_cast<const u32x4*>(cur + (t * KL + j) * 512 + 8 * lane); },
-                    [&](int y) { return *reinterpret_cast<const u32x4*>(cur + (4 * KL + y) * 512 + 8 * lane); },
-                    [] {}, [](int) {});
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        load(page_at(pages, 0));
+        convert(buf[0], start(0));
+        if (n > 1) load(page_at(pages, 1));
         __syncthreads();
+        for (int i = 0; i < n; ++i) {
+            if (i + 1 < n) convert(buf[(i + 1) & 1], start(i + 1));
+            if (i + 2 < n) load(page_at(pages, i + 2));
+            __builtin_amdgcn_sched_barrier(0);
+            const u32x4 (*cur)[2][64] = buf[i & 1];
+            const int t0 = start(i);
+            if (live && t0 <= st.wp1 && (t0 + 63 > st.far || t0 < a.S))
+                page_step<D, RT, 1, 2, 2>(
+                    st, t0, lane_value(pages.ks, i), lane_value(pages.vs, i), a.W, a.S, lane,
+                    [&](int t, int j, int p) { return cur[t * KL + j][p][lane]; },
+                    [&](int y, int p) { return cur[4 * KL + y][p][lane]; }, [] {}, [](int) {});
+            __builtin_amdgcn_sched_barrier(0);
+            __syncthreads();
+        }
     }
 #pragma unroll
     for (int x = 0; x < RT; ++x) st.l[x] = row_sum(st.l[x]);
@@ -699,14 +746,15 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
     if (p.wide) return p;
     if (groups < (p.wr == 4 ? 512 : width <= kLongTile ? 192 : 560)) {
         // Few tiles: equal chunks whatever the raggedness (find_chunk).  Where rows bound
-        // the work, as many as are resident at once (three workgroups a CU; 512, 768,
-        // 1024 of them: 69, 67, 73 us for 4 x 200 tokens of 16 over 2 heads in a window
-        // of 4096), where memory does, two rounds of them (512, 768, 1024, 1536, 2048:
-        // 255, 236, 224, 211, 211 us for 8 contexts of up to 128K x 8 heads).  Each tile
-        // may have one more than its share; a chunk is no longer than the mean tile.
-        const int64_t aim = (p.rt == 1 ? 1536 : 768) / Hkv;
-        p.items = int32_t(std::max(aim - e, e));
-        p.slots = int32_t(std::min(p.items + e, e * ((width + kMinChunk - 1) / kMinChunk)));
+        // the work, as many as run at once (512, 768, 1024 of them: 63, 72, 70 us for 4 x
+        // 200 tokens of 16 over 2 heads in a window of 4096), where memory does, two
+        // rounds of them (512, 768, 1024, 1536, 2048: 255, 236, 224, 211, 211 us for 8
+        // contexts of up to 128K x 8 heads).  (e <= aim, as fewer groups than places come
+        // here, and e <= kMaxTiles.)
+        const int64_t aim = (p.wr == 4 ? kRowsResident(d) : p.rt == 1 ? 1536 : 768) / Hkv;
+        p.items = int32_t(std::max(aim, e));
+        const int64_t most = p.wr == 4 ? 2 * int64_t(p.items) : p.items;
+        p.slots = int32_t(std::min(most, e * ((width + kMinChunk - 1) / kMinChunk)));
         return p;
     }
     // Many tiles fill the card by themselves; every wave's search for its chunk among
@@ -714,14 +762,14 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
     // -> these): one token, 8 KV heads: 256 ragged contexts of up to 512 tokens 60 -> 37,
     // 1024 of 4096 952 -> 788, 4096 of 512 4207 -> 535, 64 of 4096 63 -> 69 (all of one
     // length 100 -> 90); of 16K: 52: 180 -> 213 (302 -> 325), 72: 245 -> 259 (466 -> 417),
-    // 90: 330 -> 335 (736 -> 506).  128 rows: 4 x 1024 new tokens, 8 heads of 4 each, at
-    // 5120: 518 -> 403; 4096 at 8192, one head: 512 tiles 368 -> 343, 128 tiles 102 -> 244.
+    // 90: 330 -> 335 (736 -> 506).  Of 128 rows, from about a workgroup for every place on.
     // Contexts longer than kLongTile pages are still cut, at even lengths from the
     // table's width, so that one long context among short ones is not a walk of one
     // workgroup's; the slots of their chunks take about 1/2 GB at most.
-    const int64_t most = std::min<int64_t>(8, (p.wr == 4 ? 8192 : 32768) / groups);
+    const int64_t most = p.wr == 4 ? std::min<int64_t>(16, 8192 / groups) : std::min<int64_t>(8, 32768 / groups);
     if (width > kLongTile && most > 1) {
-        p.chunk = int32_t(std::max<int64_t>(kLongTile, (width + most - 1) / most));
+        const int64_t least = p.wr == 4 ? kLongTile / 2 : kLongTile;
+        p.chunk = int32_t(std::max(least, (width + most - 1) / most));
         p.per_tile = int32_t((width + p.chunk - 1) / p.chunk);
         p.slots = int32_t(e * p.per_tile);
     }
