@@ -19,7 +19,7 @@
 // 13K to 128K tokens x 8 heads (1.32 GB) take 208 us, 6.4 TB/s; the join 5 us.  Many
 // rows are bound by the products and exponentials: four waves take 32 rows each over
 // the same pages, whose codes are converted once for all of them (4 x 200 tokens of 16
-// over 2 heads in a window of 4096: 52 us and the join's 10).
+// over 2 heads in a window of 4096: 62 us, 7 of them the join's).
 #include "cache.h"
 #include "tiles.h"
 #include "trace.h"
@@ -113,55 +113,52 @@ __device__ __forceinline__ PageList tile_pages(const CacheAttnArgs& a, const Til
 struct Chunk {
     int32_t e, first, count, index, pages;
 };
-// With few tiles (up to kMaxTiles) their pages are cut into chunks of one length, the
-// smallest found that makes no more than `items` of them, so that whatever the raggedness
-// the workgroups take as long and run at once; or twice as many in two rounds, where one
-// leaves many places empty (5 x 200 tokens of 32 over 4 heads at 8192, 65 tiles for 128
-// places: 324 -> 252 us).  False past the last chunk.  Every wave finds its own.
+// With few tiles their pages are cut into chunks of one length, so that whatever the
+// raggedness the workgroups take as long: from the sum over all tiles and the number of
+// chunks aimed at, a tile having one more at most.  FIT: the smallest length found that
+// makes no more than `items` chunks, which run at once, or twice as many in two rounds,
+// where one leaves many places empty (5 x 200 tokens of 32 over 4 heads at 8192, 65 tiles
+// for 128 places: 324 -> 252 us).  False past the last chunk.  Every wave finds its own.
 constexpr uint32_t kStartPages = 3;   // what a workgroup's start costs, in pages
-constexpr int kMaxTiles = 9 * 64;
+template <bool FIT>
 __device__ __forceinline__ bool find_chunk(const CacheAttnArgs& a, int rows, int item, int lane, Chunk& out) {
     const int E = a.c.B * a.tiles;
-    uint32_t np[kMaxTiles / 64];   // of the tiles lane, lane + 64, ..
-    int sum = 0;
-#pragma unroll
-    for (int t = 0; t < kMaxTiles / 64; ++t) {
-        const int e = 64 * t + lane;
-        np[t] = 0;
-        if (64 * t >= E) continue;
-        np[t] = e < E ? tile_pages(a, tile_rows(a, e / a.tiles, e % a.tiles, rows)).count : 0;
-        sum += np[t];
-    }
-    const uint32_t total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
-    uint32_t pages = 0;
-    auto chunks_of = [&](int t) { return 64 * t + lane < E ? max(int((np[t] + pages - 1) / pages), 1) : 0; };
-    auto fit = [&](int most) {   // into `most` chunks (E <= most: one each in the end)
-        for (pages = max((total + most - 1) / most, uint32_t(kMinChunk));; pages += max(pages / 16, 1u)) {
-            if (E == 1) return;
-            int n = 0;
-#pragma unroll
-            for (int t = 0; t < kMaxTiles / 64; ++t)
-                if (64 * t < E) n += chunks_of(t);
-            if (__builtin_amdgcn_readlane(wave_scan(n), 63) <= most) return;
-        }
+    auto pages_of = [&](int e) {
+        return e < E ? tile_pages(a, tile_rows(a, e / a.tiles, e % a.tiles, rows)).count : 0;
     };
-    fit(a.items);
-    if (a.slots > a.items && 10 * pages > 13 * (total / a.items)) {
-        const uint32_t one = pages;
-        fit(2 * a.items);
-        if (2 * (pages + kStartPages) > one) pages = one;
+    const int own = pages_of(lane);   // the first 64 tiles are looked up once
+    int sum = own;
+    for (int e = 64 + lane; e < E; e += 64) sum += pages_of(e);
+    const uint32_t total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
+    uint32_t pages = max((total + a.items - 1) / a.items, uint32_t(kMinChunk));
+    auto chunks_of = [&](int e0) {
+        const uint32_t np = e0 == 0 ? own : pages_of(e0 + lane);
+        return e0 + lane < E ? max(int((np + pages - 1) / pages), 1) : 0;
+    };
+    if constexpr (FIT) {
+        auto fit = [&](int most) {   // (E <= most: one chunk each in the end)
+            for (pages = max((total + most - 1) / most, uint32_t(kMinChunk));; pages += max(pages / 16, 1u)) {
+                int n = 0;
+                for (int e0 = 0; e0 < E; e0 += 64) n += chunks_of(e0);
+                if (__builtin_amdgcn_readlane(wave_scan(n), 63) <= most) return;
+            }
+        };
+        fit(a.items);
+        if (10 * pages > 13 * (total / a.items)) {
+            const uint32_t one = pages;
+            fit(2 * a.items);
+            if (2 * (pages + kStartPages) > one) pages = one;
+        }
     }
     int base = 0;
-#pragma unroll
-    for (int t = 0; t < kMaxTiles / 64; ++t) {
-        if (64 * t >= E) break;
-        const int n = chunks_of(t);
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        const int n = chunks_of(e0);
         const int last = base + wave_scan(n);   // chunks up to this tile's end
         const uint64_t beyond = __ballot(item < last);
         if (beyond) {
             const int l = __builtin_ctzll(beyond);
             const int first = __builtin_amdgcn_readlane(last - n, l);
-            out = Chunk{64 * t + l, first, __builtin_amdgcn_readlane(n, l), item - first, int32_t(pages)};
+            out = Chunk{e0 + l, first, __builtin_amdgcn_readlane(n, l), item - first, int32_t(pages)};
             return true;
         }
         base = __builtin_amdgcn_readlane(last, 63);
@@ -412,11 +409,12 @@ __device__ __forceinline__ void close_rows(const CacheAttnArgs& a, const CacheRo
     }
 }
 
+template <bool FIT>
 __device__ __forceinline__ bool open_walk(const CacheAttnArgs& a, int rows, int lane, Walk& k) {
     k.hk = blockIdx.x % a.c.Hkv;
     const int item = blockIdx.x / a.c.Hkv, E = a.c.B * a.tiles;
     if (a.items > 0) {
-        if (!find_chunk(a, rows, item, lane, k.ch)) return false;
+        if (!find_chunk<FIT>(a, rows, item, lane, k.ch)) return false;
     } else {   // the tiles' first chunks, then their second ones, ..
         k.ch = Chunk{item % E, item % E * a.per_tile, 1, item / E, a.chunk};
     }
@@ -477,7 +475,7 @@ __global__ void __launch_bounds__(64 * WAVES)
     __shared__ __attribute__((aligned(16))) float so[WAVES / 2][RT * ND * 4 * 64];
     __shared__ float sml[WAVES / 2][RT][2][64];
     Walk k;
-    if (!open_walk(a, ROWS, lane, k)) return;
+    if (!open_walk<false>(a, ROWS, lane, k)) return;
     CacheRows<D, RT> st;
     open_rows(a, st, k.b, k.hk, k.tr.len, k.tr.r0, lane);
     u32x4 kr[4][KL], vr[ND];
@@ -559,8 +557,9 @@ __global__ void __launch_bounds__(64 * WAVES)
 // chunk.  A page is read and converted once for the workgroup, a quarter a wave: from
 // memory to registers two pages ahead, to bf16 operands in LDS one ahead.  (Codes staged
 // in LDS and converted by every wave, which leaves room for three workgroups a CU: 14 x
-// 127 tokens of 32 over 8 heads at 4551 270 us, so 194; 4 x 200 in a window 67, 62; 16384
-// at 20480 3.52 ms, 3.63.)
+// 127 tokens of 32 over 8 heads at 4551 270 us, so 194; 4 x 200 in a window 67, 62; 1 x
+// 4096 at 8192 526, 499; 3 x 500 of 64 heads at 8192 534, 568; 1 x 16384 at 20480 3.52
+// ms, 3.63.)
 template <int D>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3)))
 cache_attn_rows_kernel(CacheAttnArgs a) {
@@ -570,7 +569,7 @@ cache_attn_rows_kernel(CacheAttnArgs a) {
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Walk k;
-    if (!open_walk(a, ROWS, lane, k)) return;
+    if (!open_walk<true>(a, ROWS, lane, k)) return;
     const int wr0 = k.tr.r0 + 16 * RT * w;
     CacheRows<D, RT> st;
     open_rows(a, st, k.b, k.hk, k.tr.len, wr0, lane);
@@ -749,11 +748,10 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
         // the work, as many as run at once (512, 768, 1024 of them: 63, 72, 70 us for 4 x
         // 200 tokens of 16 over 2 heads in a window of 4096), where memory does, two
         // rounds of them (512, 768, 1024, 1536, 2048: 255, 236, 224, 211, 211 us for 8
-        // contexts of up to 128K x 8 heads).  (e <= aim, as fewer groups than places come
-        // here, and e <= kMaxTiles.)
+        // contexts of up to 128K x 8 heads), each tile one more than its share at most.
         const int64_t aim = (p.wr == 4 ? kRowsResident(d) : p.rt == 1 ? 1536 : 768) / Hkv;
-        p.items = int32_t(std::max(aim, e));
-        const int64_t most = p.wr == 4 ? 2 * int64_t(p.items) : p.items;
+        p.items = int32_t(std::max(p.wr == 4 ? aim : aim - e, e));
+        const int64_t most = p.wr == 4 ? 2 * int64_t(p.items) : p.items + e;
         p.slots = int32_t(std::min(most, e * ((width + kMinChunk - 1) / kMinChunk)));
         return p;
     }
