@@ -16,7 +16,8 @@
 namespace msparse {
 
 constexpr int kPage = 64;
-constexpr int kMaxWidth = 1 << 24;   // pages of a sequence: positions stay below 2^30
+constexpr int kMaxWidth = 1 << 24;   // pages of a sequence: tokens with a page stay below 2^30
+constexpr int kMaxLength = INT32_MAX - (kPage - 1);   // longest sequence; a page that starts here is beyond every row
 
 struct CacheView {
     uint8_t* k;           // [pages, Hkv, 64, d]

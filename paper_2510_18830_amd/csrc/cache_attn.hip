@@ -87,7 +87,7 @@ struct TileRows {
 __device__ __forceinline__ TileRows tile_rows(const CacheAttnArgs& a, int b, int tile, int rows) {
     TileRows t;
     const int G = a.Hq / a.c.Hkv;
-    t.len = min(max(ldc(a.c.lens, b), 0), a.c.width * kPage);
+    t.len = min(max(ldc(a.c.lens, b), 0), kMaxLength);   // past the table too: page_list ends with the table
     t.r0 = tile * rows;
     t.p0 = t.len - a.T + t.r0 / G;
     t.p1 = t.len - a.T + min(t.r0 + rows, a.T * G) / G - (min(t.r0 + rows, a.T * G) % G == 0);
@@ -189,7 +189,7 @@ __device__ __forceinline__ void open_rows(const CacheAttnArgs& a, CacheRows<D, R
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int r = min(wr0 + 16 * x + m, R - 1);
-        st.pos[x] = len - a.T + r / G;
+        st.pos[x] = max(len - a.T + r / G, -1);   // (a row before the sequence: no difference to a key overflows)
         const uint16_t* qp = a.q + b * a.qs[0] + (hk * G + r % G) * a.qs[1] + (r / G) * a.qs[2];
 #pragma unroll
         for (int s = 0; s < CacheRows<D, RT>::KS; ++s)
@@ -460,7 +460,7 @@ __device__ __forceinline__ float lane_value(float x, int i) {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i));
 }
 // position of a page's first token; a page that the table does not have lies beyond every row
-__device__ __forceinline__ int page_start(int page, int index) { return page < 0 ? kMaxWidth * kPage : kPage * index; }
+__device__ __forceinline__ int page_start(int page, int index) { return page < 0 ? kMaxLength : kPage * index; }
 
 // Up to 32 rows: the WAVES waves share them and take pages in turn, straight from
 // memory to registers.  A page is read by one wave alone, once, hence past the

@@ -1,0 +1,42 @@
+"""The paged cache at the ends of its ranges: sequences longer than their tables, rows that are not finite, tables
+whose pages pass 32 bits together.  Against the fp64 oracle as in test_gpu_cache.py."""
+import pytest
+import torch
+
+import paper_2510_18830_amd as ms
+from tests.test_gpu_cache import _attn_check, _filled, _randn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,T,width,W,S", [
+    (4, 2, 64, 3, 5, 0, 0), (4, 2, 64, 3, 5, 70, 5), (4, 2, 64, 1, 5, 40, 0),
+    (4, 2, 128, 3, 12, 0, 0), (4, 2, 128, 3, 12, 100, 70), (4, 2, 128, 1, 12, 40, 0), (4, 1, 64, 9, 12, 75, 0),
+    (4, 1, 128, 40, 3, 0, 0), (4, 1, 64, 40, 12, 0, 0), (4, 1, 128, 40, 12, 90, 3), (2, 2, 64, 200, 12, 33, 0),
+])
+def test_attn_past_the_table(gpu, Hq, Hkv, d, T, width, W, S):
+    """Rows keep the positions of the whole length: those past the table see what their window and the sinks leave of
+    the tokens that have a page, the rows before them what their own positions see."""
+    print(f"past the table Hq{Hq} Hkv{Hkv} d{d} T{T} width{width} W{W} S{S}", flush=True)
+    room = 64 * width
+    cache, table, _ = _filled(T + width, [room] * 6, Hkv, d, gpu)
+    lens = [room, room + 1, room + 5, room + 64, room + T - 1, room + 1000]
+    q = _randn(1, (len(lens), Hq, T, d), gpu)
+    out, lse = ms.cache_attn(cache, table, torch.tensor(lens, dtype=torch.int32, device=gpu), q, window=W, sinks=S)
+    torch.cuda.synchronize()
+    _attn_check(q, out, lse, cache, table, lens, W, S)
+
+
+@pytest.mark.parametrize("W,S", [(0, 0), (50, 0), (50, 7), (2 ** 31 - 1, 3)])
+@pytest.mark.parametrize("d,T", [(64, 1), (128, 3), (64, 70)])
+def test_attn_lengths_up_to_32_bits(gpu, d, T, W, S):
+    """A far length sees what any length past the window sees: all tokens that have a page, the sinks', or none."""
+    cache, table, _ = _filled(31, [640] * 4, 2, d, gpu)
+    q = _randn(1, (1, 4, T, d), gpu).expand(4, 4, T, d).contiguous()
+    got = []
+    for n in (100000, 2 ** 31 - 64):
+        lens = torch.full((4,), n, dtype=torch.int32, device=gpu)
+        got.append(ms.cache_attn(cache, table, lens, q, window=W, sinks=S))
+    torch.cuda.synchronize()
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert not torch.isneginf(got[1][1]).any() if W != 50 or S else torch.isneginf(got[1][1]).all()
