@@ -497,7 +497,8 @@ MSPARSE_API msparse_status msparse_cache_append(const msparse_cache* cache, int3
  *   q, out   bf16 [batch, heads_q, tokens, head_dim]
  *   lse      fp32 [batch, heads_q, tokens] (natural log) or NULL
  * Codes of free slots, and of tokens that no row of the call sees, may hold
- * anything.  A NaN among a call's own tokens may reach its other rows.
+ * anything.  A NaN among a call's own tokens may reach its other rows; one in a query
+ * makes out and lse of its own row NaN.
  * The workspace depends on the sizes alone, never on lens. */
 MSPARSE_API size_t msparse_cache_attn_workspace(const msparse_cache* cache, int32_t heads_q, int32_t tokens);
 MSPARSE_API msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens,

@@ -65,6 +65,10 @@ __device__ __forceinline__ float row_sum(float x) {
     return half_swap_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// Whether a row with this maximum and sum of weights saw no key.  (Logits that are all
+// NaN leave the maximum at -inf too, but a sum that is NaN, as out and lse then are.)
+__device__ __forceinline__ bool no_key(float mx, float l) { return mx == -INFINITY && l == 0.f; }
+
 // The pages that the rows at the positions p0 .. p1 (p1 >= 0) see: the sinks'
 // pages, then those of the window.
 struct PageList {
@@ -394,7 +398,7 @@ __device__ __forceinline__ void close_rows(const CacheAttnArgs& a, const CacheRo
             continue;
         }
         const int t = r / G, h = k.hk * G + r % G;
-        const bool empty = st.mx[x] == -INFINITY;
+        const bool empty = no_key(st.mx[x], st.l[x]);
         const float inv = empty ? 0.f : 1.f / st.l[x];
         uint16_t* op = a.out + k.b * a.os[0] + h * a.os[1] + t * a.os[2] + 4 * g4;
 #pragma unroll
@@ -678,7 +682,7 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(CacheAttnArgs a, i
             o += *reinterpret_cast<const f32x4*>(&so[s][4 * c]) * f;
         }
     }
-    const bool empty = mx == -INFINITY;
+    const bool empty = no_key(mx, l);
     const float inv = empty ? 0.f : 1.f / l;
     const int t = r / G, h = hk * G + r % G;
     u32x2 pk;

@@ -40,3 +40,19 @@ def test_attn_lengths_up_to_32_bits(gpu, d, T, W, S):
     torch.cuda.synchronize()
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
     assert not torch.isneginf(got[1][1]).any() if W != 50 or S else torch.isneginf(got[1][1]).all()
+
+
+@pytest.mark.parametrize("d,T,lens", [(64, 1, [40, 700, 9000]), (128, 1, [40, 700, 9000]), (128, 5, [40, 3000]),
+                                      (64, 70, [200, 3000]), (128, 600, [1500])])
+def test_attn_queries_that_are_not_finite(gpu, d, T, lens):
+    """A NaN in a query: its row's out and lse are NaN (not the -inf of a row without a key), the others' unchanged."""
+    cache, table, L = _filled(37, lens, 2, d, gpu)
+    q = _randn(1, (len(lens), 4, T, d), gpu)
+    want = ms.cache_attn(cache, table, L, q)
+    bad = torch.zeros((len(lens), 4, T), dtype=torch.bool, device=gpu)
+    bad[:, 1, T - 1] = bad[0, 2, 0] = True
+    q[bad] = torch.where(torch.arange(d, device=gpu) == 5, float("nan"), 1.0).to(q.dtype)
+    out, lse = ms.cache_attn(cache, table, L, q)
+    torch.cuda.synchronize()
+    assert torch.isnan(lse[bad]).all() and torch.isnan(out[bad]).all()
+    assert torch.equal(out[~bad], want[0][~bad]) and torch.equal(lse[~bad], want[1][~bad])
