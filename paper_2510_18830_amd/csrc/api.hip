@@ -1049,6 +1049,7 @@ msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, i
     a.items = p.items;
     a.chunk = p.chunk;
     a.per_tile = p.per_tile;
+    a.unit = p.unit;
     a.slots = p.slots;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return check_hip(launch_cache_attn(a, p, s), s, "cache attn");

@@ -84,6 +84,7 @@ struct CacheAttnArgs {
     int32_t tiles;          // row tiles of a (sequence, KV head): its G T rows
     int32_t items;          // chunks aimed at per KV head; 0: chunks of `chunk` pages, up to per_tile of a row tile
     int32_t chunk, per_tile;
+    int32_t unit;           // log2 of the pages that the sum over all tiles counts in
     // workspace (slots > 0)
     int32_t* info;          // [B tiles][2]: first chunk, chunks
     float* po;              // [slots, Hkv, rows, d]: sums of the weighted values
@@ -94,7 +95,7 @@ struct CacheAttnArgs {
 struct CacheAttnPlan {
     int32_t rt, wr;         // 16-row tiles per wave; waves of a workgroup over rows (1: over pages)
     int32_t rows;           // rows of a workgroup
-    int32_t tiles, items, chunk, per_tile, slots;
+    int32_t tiles, items, chunk, per_tile, unit, slots;
     bool wide;              // a workgroup of many waves per tile
 };
 // workgroups per KV head

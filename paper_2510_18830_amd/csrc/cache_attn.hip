@@ -130,25 +130,28 @@ __device__ __forceinline__ bool find_chunk(const CacheAttnArgs& a, int rows, int
     auto pages_of = [&](int e) {
         return e < E ? tile_pages(a, tile_rows(a, e / a.tiles, e % a.tiles, rows)).count : 0;
     };
+    // the sum counts units of 2^unit pages, a tile's rounded up, so that it stays below 2^31
+    auto units = [&](int np) { return int((uint32_t(np) + (1u << a.unit) - 1) >> a.unit); };
     const int own = pages_of(lane);   // the first 64 tiles are looked up once
-    int sum = own;
-    for (int e = 64 + lane; e < E; e += 64) sum += pages_of(e);
+    int sum = units(own);
+    for (int e = 64 + lane; e < E; e += 64) sum += units(pages_of(e));
     const uint32_t total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
-    uint32_t pages = max((total + a.items - 1) / a.items, uint32_t(kMinChunk));
+    auto share = [&](int chunks) { return max(((total + chunks - 1) / chunks) << a.unit, uint32_t(kMinChunk)); };
+    uint32_t pages = share(a.items);
     auto chunks_of = [&](int e0) {
         const uint32_t np = e0 == 0 ? own : pages_of(e0 + lane);
         return e0 + lane < E ? max(int((np + pages - 1) / pages), 1) : 0;
     };
     if constexpr (FIT) {
         auto fit = [&](int most) {   // (E <= most: one chunk each in the end)
-            for (pages = max((total + most - 1) / most, uint32_t(kMinChunk));; pages += max(pages / 16, 1u)) {
+            for (pages = share(most);; pages += max(pages / 16, 1u)) {
                 int n = 0;
                 for (int e0 = 0; e0 < E; e0 += 64) n += chunks_of(e0);
                 if (__builtin_amdgcn_readlane(wave_scan(n), 63) <= most) return;
             }
         };
         fit(a.items);
-        if (10 * pages > 13 * (total / a.items)) {
+        if (10 * pages > 13 * ((total / a.items) << a.unit)) {
             const uint32_t one = pages;
             fit(2 * a.items);
             if (2 * (pages + kStartPages) > one) pages = one;
@@ -757,6 +760,7 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
         p.items = int32_t(std::max(p.wr == 4 ? aim : aim - e, e));
         const int64_t most = p.wr == 4 ? 2 * int64_t(p.items) : p.items + e;
         p.slots = int32_t(std::min(most, e * ((width + kMinChunk - 1) / kMinChunk)));
+        while (e * ((width >> p.unit) + 1) > INT32_MAX) ++p.unit;
         return p;
     }
     // Many tiles fill the card by themselves; every wave's search for its chunk among

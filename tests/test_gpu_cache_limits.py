@@ -56,3 +56,20 @@ def test_attn_queries_that_are_not_finite(gpu, d, T, lens):
     torch.cuda.synchronize()
     assert torch.isnan(lse[bad]).all() and torch.isnan(out[bad]).all()
     assert torch.equal(out[~bad], want[0][~bad]) and torch.equal(lse[~bad], want[1][~bad])
+
+
+def test_attn_pages_beyond_32_bits(gpu):
+    """260 sequences of 2^30 tokens: more than 2^32 pages together, of which each sequence's table holds seven.  The
+    result is that of the seven pages alone."""
+    B, Hkv, d, width, held = 260, 1, 64, 1 << 24, 7
+    cache, table, L = _filled(41, [64 * held] * B, Hkv, d, gpu)
+    wide = torch.full((B, width), -1, dtype=torch.int32, device=gpu)
+    for i, at in enumerate((0, 3, 70000, 1 << 22, (1 << 23) + 5, (1 << 24) - 9, (1 << 24) - 1)):
+        wide[:, at] = table[:, i]
+    lens = torch.full((B,), 64 * width, dtype=torch.int32, device=gpu)
+    q = _randn(1, (B, 4, 1, d), gpu)
+    torch.cuda.synchronize()
+    print("tables made", flush=True)
+    out, lse = ms.cache_attn(cache, wide, lens, q)
+    torch.cuda.synchronize()
+    _attn_check(q, out, lse, cache, table, [64 * held] * B, 0, 0)
