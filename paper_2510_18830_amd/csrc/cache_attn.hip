@@ -84,14 +84,18 @@ __device__ __forceinline__ PageList page_list(int p0, int p1, int W, int S, int 
     l.count = l.sinks + end - l.lo;
     return l;
 }
-// positions of the first and last row of tile `tile` of sequence b
+// tokens of sequence b, past the table too (page_list ends with the table)
+__device__ __forceinline__ int32_t length_of(const CacheAttnArgs& a, int b) {
+    return min(max(ldc(a.c.lens, b), 0), kMaxLength);
+}
+// positions of the first and last row of tile `tile` of a sequence of `len` tokens
 struct TileRows {
     int32_t r0, len, p0, p1;
 };
-__device__ __forceinline__ TileRows tile_rows(const CacheAttnArgs& a, int b, int tile, int rows) {
+__device__ __forceinline__ TileRows tile_rows(const CacheAttnArgs& a, int32_t len, int tile, int rows) {
     TileRows t;
     const int G = a.Hq / a.c.Hkv;
-    t.len = min(max(ldc(a.c.lens, b), 0), kMaxLength);   // past the table too: page_list ends with the table
+    t.len = len;
     t.r0 = tile * rows;
     t.p0 = t.len - a.T + t.r0 / G;
     t.p1 = t.len - a.T + min(t.r0 + rows, a.T * G) / G - (min(t.r0 + rows, a.T * G) % G == 0);
@@ -128,7 +132,7 @@ template <bool FIT>
 __device__ __forceinline__ bool find_chunk(const CacheAttnArgs& a, int rows, int item, int lane, Chunk& out) {
     const int E = a.c.B * a.tiles;
     auto pages_of = [&](int e) {
-        return e < E ? tile_pages(a, tile_rows(a, e / a.tiles, e % a.tiles, rows)).count : 0;
+        return e < E ? tile_pages(a, tile_rows(a, length_of(a, e / a.tiles), e % a.tiles, rows)).count : 0;
     };
     // the sum counts units of 2^unit pages, a tile's rounded up, so that it stays below 2^31
     auto units = [&](int np) { return int((uint32_t(np) + (1u << a.unit) - 1) >> a.unit); };
@@ -426,7 +430,9 @@ __device__ __forceinline__ bool open_walk(const CacheAttnArgs& a, int rows, int 
         k.ch = Chunk{item % E, item % E * a.per_tile, 1, item / E, a.chunk};
     }
     k.b = k.ch.e / a.tiles;
-    k.tr = tile_rows(a, k.b, k.ch.e % a.tiles, rows);
+    // (the clamp is a vector instruction; left in a vector register, the length takes the
+    // positions that follow from it along, and they spill: 8 x 128K 210 us, so 226)
+    k.tr = tile_rows(a, __builtin_amdgcn_readfirstlane(length_of(a, k.b)), k.ch.e % a.tiles, rows);
     k.pl = tile_pages(a, k.tr);
     if (a.items == 0) {
         k.ch.count = max(int((int64_t(k.pl.count) + a.chunk - 1) / a.chunk), 1);
