@@ -851,6 +851,16 @@ static size_t carve_window_bwd(WindowArgs* a, char* base) {
     return c.off;
 }
 
+// The key-major pass has the sink groups' chunks beside all groups: 512 threads each, below 2^32 together.
+static msparse_status check_window_keys(const WindowArgs& a) {
+    const KeyPlan& p = a.plan;
+    const int keys = window_key_group(a.d);
+    const int64_t each = int64_t(p.sink_groups) * p.far_slots + (int64_t(a.seq) + keys - 1) / keys * p.near_slots;
+    if (int64_t(a.B) * a.Hkv * each >= 2 * kMaxGroups)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%lld workgroups of keys exceed 2^23", (long long)(int64_t(a.B) * a.Hkv * each));
+    return MSPARSE_OK;
+}
+
 msparse_status msparse_window_fwd(const msparse_window* win, const int32_t* starts, const msparse_tensor* q,
                                   const msparse_tensor* k, const msparse_tensor* v, const msparse_tensor* out,
                                   float* lse, void* stream) {
@@ -878,7 +888,8 @@ size_t msparse_window_bwd_workspace(const msparse_window* win) {
     static const int32_t present = 0;   // only whether starts are given counts
     if (check_window(win, win && win->tokens > 0 ? &present : nullptr)) return 0;
     WindowArgs a = window_args(win, nullptr);
-    return carve_window_bwd(&a, nullptr);
+    const size_t need = carve_window_bwd(&a, nullptr);
+    return check_window_keys(a) ? 0 : need;
 }
 
 msparse_status msparse_window_bwd(const msparse_window* win, const int32_t* starts, const msparse_tensor* q,
@@ -902,6 +913,7 @@ msparse_status msparse_window_bwd(const msparse_window* win, const int32_t* star
     if (misaligned({lse, ws})) return fail(MSPARSE_ERR_INVALID, "lse or workspace is not 16-byte aligned");
     WindowArgs a = window_args(win, starts);
     const size_t need = carve_window_bwd(&a, static_cast<char*>(ws));
+    if ((st = check_window_keys(a))) return st;
     if (need && (!ws || ws_bytes < need))
         return fail(MSPARSE_ERR_WORKSPACE, "window bwd workspace %zu < %zu bytes", ws_bytes, need);
     a.q = row_view(q);

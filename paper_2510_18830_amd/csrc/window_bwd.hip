@@ -614,10 +614,9 @@ template <int D>
 __global__ void __launch_bounds__(kSumThreads) window_sums_kernel(WindowArgs a) {
     constexpr int C = D / 4, KEYS = 64 * kKeyBlocks<D>;
     const KeyPlan& p = a.plan;
-    const int per = 2 * KEYS * C / kSumThreads;   // workgroups per group
-    const int item = blockIdx.x / per;
+    const int item = blockIdx.x;   // (sequence, KV head, group)
     const int bk = item / p.part_groups, group = item % p.part_groups;
-    const int t = (blockIdx.x % per) * kSumThreads + threadIdx.x;
+    const int t = blockIdx.y * kSumThreads + threadIdx.x;
     const int which = t / (KEYS * C), key = t / C % KEYS, c = 4 * (t % C);
     const int b = bk / a.Hkv, hk = bk % a.Hkv, G = a.Hq / a.Hkv;
     const Sequence sq = sequence(a, b);
@@ -673,8 +672,9 @@ hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.plan.part_groups > 0) {
         TraceScope _t("window_sums", s);
-        const int per = 2 * window_key_group(a.d) * a.d / 4 / kSumThreads;   // workgroups per group
-        const dim3 g(unsigned(bk * a.plan.part_groups * per)), t(kSumThreads);
+        // 8 or 32 workgroups per group, along y: along x too, a launch of 2^19 groups would have 2^32 threads
+        const dim3 g(unsigned(bk * a.plan.part_groups), unsigned(2 * window_key_group(a.d) * a.d / 4 / kSumThreads));
+        const dim3 t(kSumThreads);
         if (wide) hipLaunchKernelGGL(window_sums_kernel<128>, g, t, 0, s, a);
         else hipLaunchKernelGGL(window_sums_kernel<64>, g, t, 0, s, a);
     }
