@@ -391,10 +391,13 @@ MSPARSE_API msparse_status msparse_attn_bwd(const msparse_dims* dims, const void
  *   tokens > 0   every tensor has `tokens` rows per head and no batch axis (its
  *                batch stride is not used); sequence b is the rows starts[b] to
  *                starts[b + 1] - 1, starts int32 [batch + 1] on the device,
- *                ascending, none longer than seq; lse [heads_q, tokens].  A
- *                sequence may be empty.  Rows of no sequence are left as they
- *                were, in every output.  (Starts outside [0, tokens] are cut to
- *                it, and a longer sequence to its first seq rows.)
+ *                ascending, none longer than seq (which may be `tokens`, where the
+ *                longest is not known); lse [heads_q, tokens].  A sequence may
+ *                be empty.  Rows of no sequence are left as they were, in every
+ *                output.  (Starts outside [0, tokens] are cut to it, and a longer
+ *                sequence to its first seq rows.)
+ * A call takes up to 2^22 blocks of 64 rows over all query heads; of packed tensors
+ * their rows count, and a block for each sequence.
  * All values of a sequence have to be finite: a row that is not may spread to
  * rows of the same sequence that do not see it, but never to another sequence. */
 typedef struct {

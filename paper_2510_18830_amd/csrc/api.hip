@@ -796,9 +796,6 @@ static RowView row_view(const msparse_tensor* t) {
     return RowView{static_cast<uint16_t*>(t->data), t->batch, t->head, t->token};
 }
 
-// Most workgroups of a launch: 512 threads each stay below 2^32
-constexpr int64_t kMaxGroups = int64_t(1) << 22;
-
 static msparse_status check_window(const msparse_window* w, const int32_t* starts) {
     if (!w) return fail(MSPARSE_ERR_INVALID, "window is NULL");
     if (w->batch < 1 || w->heads_q < 1 || w->heads_kv < 1 || w->seq < 0 || w->tokens < 0)
@@ -815,9 +812,10 @@ static msparse_status check_window(const msparse_window* w, const int32_t* start
     const int64_t rows = w->tokens > 0 ? w->tokens : int64_t(w->batch) * w->seq;
     if (rows > ((int64_t(1) << 31) - 1) / w->heads_q || w->seq > (1 << 30))
         return fail(MSPARSE_ERR_UNSUPPORTED, "heads * tokens exceeds 2^31 rows");
-    if (int64_t(w->batch) * w->heads_q > kMaxGroups / std::max<int64_t>(1, (int64_t(w->seq) + 63) / 64))
-        return fail(MSPARSE_ERR_UNSUPPORTED, "%d sequences of up to %d tokens exceed 2^22 blocks of 64 rows", w->batch,
-                    w->seq);
+    const bool by_rows = grid_by_rows(w->batch, w->heads_q, w->seq, w->tokens);
+    if (grid_blocks(by_rows, w->batch, w->seq, w->tokens, 64) > kMaxGroups / w->heads_q)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%d sequences of up to %d tokens%s exceed 2^22 blocks of 64 rows", w->batch,
+                    w->seq, by_rows ? " (packed: their rows and one block each)" : "");
     return MSPARSE_OK;
 }
 
@@ -835,6 +833,7 @@ static WindowArgs window_args(const msparse_window* w, const int32_t* starts) {
     a.W = all ? INT32_MAX : w->window;
     a.S = all ? 0 : w->sinks;
     a.scale = w->scale > 0.f ? w->scale : 1.0f / std::sqrt(float(w->head_dim));
+    a.by_rows = grid_by_rows(w->batch, w->heads_q, w->seq, w->tokens);
     return a;
 }
 
@@ -842,12 +841,13 @@ static WindowArgs window_args(const msparse_window* w, const int32_t* starts) {
 static size_t carve_window_bwd(WindowArgs* a, char* base) {
     const int keys = window_key_group(a->d);
     const KeyPlan& p = a->plan = key_plan(a->B, a->Hkv, a->Hq / a->Hkv, a->seq, a->tokens, a->W, a->S, a->d, keys,
-                                          window_key_resident(a->d));
-    const int64_t slots = int64_t(p.part_groups) * p.near_slots + int64_t(p.sink_groups) * p.far_slots;
+                                          window_key_resident(a->d), a->by_rows);
+    const int64_t near = (a->by_rows ? p.far_docs : a->B) * int64_t(p.part_groups) * p.near_slots;
+    const int64_t far = (a->by_rows ? 1 : a->B) * int64_t(p.sink_groups) * p.far_slots;
     a->rows_pad = a->tokens > 0 ? padded_rows(a->tokens) + 64 * (int64_t(a->B) + 1) : a->B * padded_rows(a->seq);
     Carve c{base};
     a->rows = c.take<float>(size_t(2) * a->Hq * a->rows_pad);
-    a->part = c.take<float>(size_t(a->B) * a->Hkv * slots * 2 * keys * a->d);
+    a->part = c.take<float>(size_t(a->Hkv) * (near + far) * 2 * keys * a->d);
     return c.off;
 }
 
@@ -855,9 +855,10 @@ static size_t carve_window_bwd(WindowArgs* a, char* base) {
 static msparse_status check_window_keys(const WindowArgs& a) {
     const KeyPlan& p = a.plan;
     const int keys = window_key_group(a.d);
-    const int64_t each = int64_t(p.sink_groups) * p.far_slots + (int64_t(a.seq) + keys - 1) / keys * p.near_slots;
-    if (int64_t(a.B) * a.Hkv * each >= 2 * kMaxGroups)
-        return fail(MSPARSE_ERR_UNSUPPORTED, "%lld workgroups of keys exceed 2^23", (long long)(int64_t(a.B) * a.Hkv * each));
+    const int64_t each = (a.by_rows ? 1 : a.B) * int64_t(p.sink_groups) * p.far_slots +
+                         grid_blocks(a.by_rows, a.B, a.seq, a.tokens, keys) * p.near_slots;
+    if (each >= 2 * kMaxGroups / a.Hkv)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%lld workgroups of keys exceed 2^23", (long long)(each * a.Hkv));
     return MSPARSE_OK;
 }
 

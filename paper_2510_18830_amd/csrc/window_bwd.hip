@@ -191,7 +191,7 @@ __device__ __forceinline__ void store_dq(const WindowArgs& a, const Sequence& sq
         }
 }
 
-template <int D>
+template <int D, bool BY_ROWS>
 __global__ void __launch_bounds__(kDqThreads)
     __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) window_dq_kernel(WindowArgs a) {
     constexpr int TE = DmaTile<D, kDualPad>::kElems;
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kDqThreads)
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     int b, hq, tile;
-    window_tile_of(a, blockIdx.x, (a.seq + kDqRows - 1) / kDqRows, b, hq, tile);
+    if (!window_tile_of<BY_ROWS>(a, blockIdx.x, kDqRows, b, hq, tile)) return;
     const Sequence sq = sequence(a, b);
     const int i0 = tile * kDqRows;
     if (i0 >= sq.n) return;
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kDqThreads)
 
 // Small grids: 64 rows per workgroup, two halves on alternate tiles (as the
 // forward's); the second half's sum is added to the first's.
-template <int D>
+template <int D, bool BY_ROWS>
 __global__ void __launch_bounds__(kDqThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 window_dq_split_kernel(WindowArgs a) {
     constexpr int ND = WinDq<D>::ND;
@@ -262,7 +262,7 @@ window_dq_split_kernel(WindowArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), half = w >> 1, rh = w & 1;
     int b, hq, tile;
-    window_tile_of(a, blockIdx.x, (a.seq + 63) >> 6, b, hq, tile);
+    if (!window_tile_of<BY_ROWS>(a, blockIdx.x, 64, b, hq, tile)) return;
     const Sequence sq = sequence(a, b);
     const int i0 = 64 * tile;
     if (i0 >= sq.n) return;
@@ -442,9 +442,10 @@ __device__ __forceinline__ QueryRange query_range(const Sequence& sq, int j0, in
     return r;
 }
 
-// Workgroups 0 .. B Hkv sink_groups far_slots - 1: the chunks of the sink keys' rows
-// beyond the window; the rest: groups of kKeyBlocks key blocks, near_slots for each.
-template <int D>
+// Workgroups 0 .. B Hkv sink_groups far_slots - 1 (by rows: Hkv for B Hkv): the chunks of
+// the sink keys' rows beyond the window; the rest: groups of kKeyBlocks key blocks,
+// near_slots for each.
+template <int D, bool BY_ROWS>
 __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
     __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3))) window_dkdv_kernel(WindowArgs a) {
     constexpr int KD = D / 16, ND = D / 32, KB = kKeyBlocks<D>, KEYS = 64 * KB, NW = 4 * KB;
@@ -454,13 +455,13 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = w >> 2, kh = (w >> 1) & 1, rh = w & 1;
-    const int BK = a.B * a.Hkv, G = a.Hq / a.Hkv;
-    const int groups = (a.seq + KEYS - 1) / KEYS;
+    const int BK = BY_ROWS ? a.Hkv : a.B * a.Hkv, G = a.Hq / a.Hkv;
+    const int groups = BY_ROWS ? int(a.tokens / KEYS) + a.B : (a.seq + KEYS - 1) / KEYS;
     const KeyPlan& p = a.plan;
     const int64_t extra = int64_t(BK) * p.sink_groups * p.far_slots;
     const bool far = int64_t(blockIdx.x) < extra;
     const int64_t u = far ? blockIdx.x : xcd_chunk(blockIdx.x - extra, int64_t(BK) * groups * p.near_slots);
-    const int slot = int(u % (far ? p.far_slots : p.near_slots));
+    int slot = int(u % (far ? p.far_slots : p.near_slots));
     const int item = int(u / (far ? p.far_slots : p.near_slots));
     int group, bk;
     if (far) {
@@ -469,7 +470,16 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
     } else {
         cell_of(item, BK, groups, bk, group);
     }
-    const int b = bk / a.Hkv, hk = bk % a.Hkv;
+    const int hk = bk % a.Hkv;
+    int b = bk / a.Hkv;
+    if (BY_ROWS && far) {
+        b = last_sequence(a, slot, [&](int64_t start, int i) { return far_slot(a, start, i); });
+        slot -= int(far_slot(a, cut_start(a, ldc(a.starts, b)), b));
+        if (slot < 0) return;
+    } else if (BY_ROWS) {
+        block_of(a, group, KEYS, b, group);
+        if (group < 0) return;
+    }
     const Sequence sq = sequence(a, b);
     if (KEYS * group >= sq.n) return;
     const int last = sq.n - 1;
@@ -478,6 +488,7 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
     const int base = far ? range.hi + 1 : range.lo;
     const int width = far ? range.end - base : range.hi - range.lo + 1;
     const int chunk = far ? p.far_chunk : p.near_chunk;
+    if (BY_ROWS && int64_t(slot) * chunk >= G * width) return;   // (a slot that no sequence has may be far out)
     const int e0 = slot * chunk, e1 = min(e0 + chunk, G * width);
     if (e0 >= e1) return;
     const int key = 32 * kh + l32;
@@ -558,9 +569,11 @@ __global__ void __launch_bounds__(256 * kKeyBlocks<D>)
         __syncthreads();
     }
     if (rh != 0 || j > last || !live || (far && j >= a.S)) return;
-    if (far || group < p.part_groups) {
-        const int64_t at = far ? int64_t(BK) * p.part_groups * p.near_slots + u
-                               : (int64_t(bk) * p.part_groups + group) * p.near_slots + slot;
+    if (far || (group < p.part_groups && (!BY_ROWS || range.end - 1 > range.hi))) {
+        const int64_t lines = BY_ROWS ? int64_t(a.Hkv) * p.far_docs : BK;
+        const int64_t line = BY_ROWS ? int64_t(hk) * p.far_docs + far_index(a, sq.row, b) : bk;
+        const int64_t at = far ? lines * p.part_groups * p.near_slots + u
+                               : (line * p.part_groups + group) * p.near_slots + slot;
         float* o = a.part + at * (2 * KEYS * D) + (64 * half + key) * D + 4 * h;
 #pragma unroll
         for (int x = 0; x < ND; ++x)
@@ -614,23 +627,31 @@ template <int D>
 __global__ void __launch_bounds__(kSumThreads) window_sums_kernel(WindowArgs a) {
     constexpr int C = D / 4, KEYS = 64 * kKeyBlocks<D>;
     const KeyPlan& p = a.plan;
-    const int item = blockIdx.x;   // (sequence, KV head, group)
-    const int bk = item / p.part_groups, group = item % p.part_groups;
+    const int item = blockIdx.x;   // (line, group); a line: (sequence, KV head), by rows (KV head, far_index)
+    const int line = item / p.part_groups, group = item % p.part_groups;
     const int t = blockIdx.y * kSumThreads + threadIdx.x;
     const int which = t / (KEYS * C), key = t / C % KEYS, c = 4 * (t % C);
-    const int b = bk / a.Hkv, hk = bk % a.Hkv, G = a.Hq / a.Hkv;
+    const int hk = a.by_rows ? line / p.far_docs : line % a.Hkv, G = a.Hq / a.Hkv;
+    int b = line / a.Hkv;
+    if (a.by_rows) {   // of the sequences with this index the last, as one with rows beyond its window is
+        const int index = line % p.far_docs;
+        b = last_sequence(a, index, [&](int64_t start, int i) { return far_index(a, start, i); });
+        if (far_index(a, cut_start(a, ldc(a.starts, b)), b) != index) return;
+    }
     const Sequence sq = sequence(a, b);
     const int j = KEYS * group + key;
     if (j >= sq.n) return;
     const QueryRange range = query_range(sq, KEYS * group, KEYS * group + KEYS - 1, a.W);
+    if (a.by_rows && range.end - 1 <= range.hi) return;
+    const int64_t lines = a.by_rows ? int64_t(a.Hkv) * p.far_docs : int64_t(a.B) * a.Hkv;
+    const int64_t far0 = a.by_rows ? (int64_t(hk) * p.sink_groups + group) * p.far_slots + far_slot(a, sq.row, b)
+                                   : (int64_t(line) * p.sink_groups + group) * p.far_slots;
     const float* part = a.part + which * (KEYS * D) + key * D + c;
     f32x4 sum = f32x4{};
     add_slots<D>(sum, part + int64_t(item) * p.near_slots * (2 * KEYS * D),
                  (G * (range.hi - range.lo + 1) + p.near_chunk - 1) / p.near_chunk);
     if (j < a.S && group < p.sink_groups)
-        add_slots<D>(sum,
-                     part + (int64_t(a.B) * a.Hkv * p.part_groups * p.near_slots +
-                             (int64_t(bk) * p.sink_groups + group) * p.far_slots) * (2 * KEYS * D),
+        add_slots<D>(sum, part + (lines * p.part_groups * p.near_slots + far0) * (2 * KEYS * D),
                      (G * (range.end - 1 - range.hi) + p.far_chunk - 1) / p.far_chunk);
     const RowView& v = which == 0 ? a.dk : a.dv;
     const float f = which == 0 ? a.scale : 1.f;
@@ -649,31 +670,35 @@ hipError_t launch_window_bwd(const WindowArgs& a, hipStream_t s) {
     const bool wide = a.d == 128;
     {
         TraceScope _t("window_dq", s);
-        const int64_t heads = int64_t(a.B) * a.Hq, grid = heads * ((a.seq + kDqRows - 1) / kDqRows);
         const int64_t most = wide ? kSplitGrid<128> : kSplitGrid<64>;
         const bool split = a.Hq * row_blocks(a.B, a.seq, a.tokens, kDqRows) <= most;
-        const dim3 g(unsigned(split ? heads * ((a.seq + 63) / 64) : grid)), t(kDqThreads);
-        if (split && wide) hipLaunchKernelGGL(window_dq_split_kernel<128>, g, t, 0, s, a);
-        else if (split) hipLaunchKernelGGL(window_dq_split_kernel<64>, g, t, 0, s, a);
-        else if (wide) hipLaunchKernelGGL(window_dq_kernel<128>, g, t, 0, s, a);
-        else hipLaunchKernelGGL(window_dq_kernel<64>, g, t, 0, s, a);
+        const dim3 g(unsigned(a.Hq * grid_blocks(a.by_rows, a.B, a.seq, a.tokens, split ? 64 : kDqRows))), t(kDqThreads);
+        window_variant(a, [&](auto dim, auto by_rows) {
+            constexpr int D = decltype(dim)::value;
+            constexpr bool R = decltype(by_rows)::value;
+            if (split) hipLaunchKernelGGL((window_dq_split_kernel<D, R>), g, t, 0, s, a);
+            else hipLaunchKernelGGL((window_dq_kernel<D, R>), g, t, 0, s, a);
+        });
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t bk = int64_t(a.B) * a.Hkv;
+    const int64_t bk = (a.by_rows ? 1 : int64_t(a.B)) * a.Hkv;
     {
         TraceScope _t("window_dkdv", s);
         const int keys = window_key_group(a.d);
-        const int64_t groups = (a.seq + keys - 1) / keys;
-        const dim3 g(unsigned(bk * (a.plan.sink_groups * int64_t(a.plan.far_slots) + groups * a.plan.near_slots)));
-        if (wide) hipLaunchKernelGGL(window_dkdv_kernel<128>, g, dim3(256 * kKeyBlocks<128>), 0, s, a);
-        else hipLaunchKernelGGL(window_dkdv_kernel<64>, g, dim3(256 * kKeyBlocks<64>), 0, s, a);
+        const int64_t groups = a.Hkv * grid_blocks(a.by_rows, a.B, a.seq, a.tokens, keys);
+        const dim3 g(unsigned(bk * a.plan.sink_groups * a.plan.far_slots + groups * a.plan.near_slots));
+        window_variant(a, [&](auto dim, auto by_rows) {
+            constexpr int D = decltype(dim)::value;
+            hipLaunchKernelGGL((window_dkdv_kernel<D, decltype(by_rows)::value>), g, dim3(256 * kKeyBlocks<D>), 0, s, a);
+        });
     }
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.plan.part_groups > 0) {
         TraceScope _t("window_sums", s);
         // 8 or 32 workgroups per group, along y: along x too, a launch of 2^19 groups would have 2^32 threads
-        const dim3 g(unsigned(bk * a.plan.part_groups), unsigned(2 * window_key_group(a.d) * a.d / 4 / kSumThreads));
+        const int64_t lines = a.by_rows ? int64_t(a.Hkv) * a.plan.far_docs : bk;
+        const dim3 g(unsigned(lines * a.plan.part_groups), unsigned(2 * window_key_group(a.d) * a.d / 4 / kSumThreads));
         const dim3 t(kSumThreads);
         if (wide) hipLaunchKernelGGL(window_sums_kernel<128>, g, t, 0, s, a);
         else hipLaunchKernelGGL(window_sums_kernel<64>, g, t, 0, s, a);

@@ -167,7 +167,7 @@ __device__ __forceinline__ void store_rows(const WindowArgs& a, const WinRows<D>
 }
 
 // Two waves per SIMD at head dim 128 (256 registers), three at 64.
-template <int D>
+template <int D, bool BY_ROWS>
 __global__ void __launch_bounds__(kFwdThreads) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 3 : 2)))
 window_fwd_kernel(WindowArgs a) {
     constexpr int KD = WinRows<D>::KD, ND = WinRows<D>::ND;
@@ -176,7 +176,7 @@ window_fwd_kernel(WindowArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     int b, hq, tile;
-    window_tile_of(a, blockIdx.x, (a.seq + kFwdRows - 1) / kFwdRows, b, hq, tile);
+    if (!window_tile_of<BY_ROWS>(a, blockIdx.x, kFwdRows, b, hq, tile)) return;
     const Sequence sq = sequence(a, b);
     const int i0 = tile * kFwdRows;
     if (i0 >= sq.n) return;
@@ -225,7 +225,7 @@ window_fwd_kernel(WindowArgs a) {
 // half of it by half the rows each is faster while twice the workgroups, of which one
 // fits a CU where two do otherwise (two where three do, at head dim 64), are resident
 // at once.
-template <int D>
+template <int D, bool BY_ROWS>
 __global__ void __launch_bounds__(kFwdThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 window_fwd_split_kernel(WindowArgs a) {
     constexpr int KD = WinRows<D>::KD, ND = WinRows<D>::ND;
@@ -235,7 +235,7 @@ window_fwd_split_kernel(WindowArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), half = w >> 1, rh = w & 1;
     int b, hq, tile;
-    window_tile_of(a, blockIdx.x, (a.seq + 63) >> 6, b, hq, tile);
+    if (!window_tile_of<BY_ROWS>(a, blockIdx.x, 64, b, hq, tile)) return;
     const Sequence sq = sequence(a, b);
     const int i0 = 64 * tile;
     if (i0 >= sq.n) return;
@@ -300,15 +300,16 @@ window_fwd_split_kernel(WindowArgs a) {
 }  // namespace
 
 hipError_t launch_window_fwd(const WindowArgs& a, hipStream_t s) {
-    const int64_t heads = int64_t(a.B) * a.Hq, grid = heads * ((a.seq + kFwdRows - 1) / kFwdRows);
     const int64_t most = a.d == 128 ? kSplitGrid<128> : kSplitGrid<64>;
     const bool split = a.Hq * row_blocks(a.B, a.seq, a.tokens, kFwdRows) <= most;
     TraceScope _t("window_fwd", s);
-    const dim3 g(unsigned(split ? heads * ((a.seq + 63) / 64) : grid)), t(kFwdThreads);
-    if (split && a.d == 128) hipLaunchKernelGGL(window_fwd_split_kernel<128>, g, t, 0, s, a);
-    else if (split) hipLaunchKernelGGL(window_fwd_split_kernel<64>, g, t, 0, s, a);
-    else if (a.d == 128) hipLaunchKernelGGL(window_fwd_kernel<128>, g, t, 0, s, a);
-    else hipLaunchKernelGGL(window_fwd_kernel<64>, g, t, 0, s, a);
+    const dim3 g(unsigned(a.Hq * grid_blocks(a.by_rows, a.B, a.seq, a.tokens, split ? 64 : kFwdRows))), t(kFwdThreads);
+    window_variant(a, [&](auto dim, auto by_rows) {
+        constexpr int D = decltype(dim)::value;
+        constexpr bool R = decltype(by_rows)::value;
+        if (split) hipLaunchKernelGGL((window_fwd_split_kernel<D, R>), g, t, 0, s, a);
+        else hipLaunchKernelGGL((window_fwd_kernel<D, R>), g, t, 0, s, a);
+    });
     return hipGetLastError();
 }
 
