@@ -796,6 +796,11 @@ static RowView row_view(const msparse_tensor* t) {
     return RowView{static_cast<uint16_t*>(t->data), t->batch, t->head, t->token};
 }
 
+// The most tokens that a sequence can have.
+static int32_t longest(const msparse_window* w) {
+    return w->tokens > 0 ? int32_t(std::min<int64_t>(w->seq, w->tokens)) : w->seq;
+}
+
 static msparse_status check_window(const msparse_window* w, const int32_t* starts) {
     if (!w) return fail(MSPARSE_ERR_INVALID, "window is NULL");
     if (w->batch < 1 || w->heads_q < 1 || w->heads_kv < 1 || w->seq < 0 || w->tokens < 0)
@@ -812,10 +817,11 @@ static msparse_status check_window(const msparse_window* w, const int32_t* start
     const int64_t rows = w->tokens > 0 ? w->tokens : int64_t(w->batch) * w->seq;
     if (rows > ((int64_t(1) << 31) - 1) / w->heads_q || w->seq > (1 << 30))
         return fail(MSPARSE_ERR_UNSUPPORTED, "heads * tokens exceeds 2^31 rows");
-    const bool by_rows = grid_by_rows(w->batch, w->heads_q, w->seq, w->tokens);
-    if (grid_blocks(by_rows, w->batch, w->seq, w->tokens, 64) > kMaxGroups / w->heads_q)
+    const int32_t seq = longest(w);
+    const bool by_rows = grid_by_rows(w->batch, w->heads_q, seq, w->tokens);
+    if (grid_blocks(by_rows, w->batch, seq, w->tokens, 64) > kMaxGroups / w->heads_q)
         return fail(MSPARSE_ERR_UNSUPPORTED, "%d sequences of up to %d tokens%s exceed 2^22 blocks of 64 rows", w->batch,
-                    w->seq, by_rows ? " (packed: their rows and one block each)" : "");
+                    seq, by_rows ? " (packed: their rows and one block each)" : "");
     return MSPARSE_OK;
 }
 
@@ -826,14 +832,14 @@ static WindowArgs window_args(const msparse_window* w, const int32_t* starts) {
     a.B = w->batch;
     a.Hq = w->heads_q;
     a.Hkv = w->heads_kv;
-    a.seq = w->seq;
+    a.seq = longest(w);
     a.d = w->head_dim;
     // a window or sinks over the whole sequence leave the causal mask alone
-    const bool all = w->window == 0 || w->window >= w->seq || w->sinks >= w->seq;
+    const bool all = w->window == 0 || w->window >= a.seq || w->sinks >= a.seq;
     a.W = all ? INT32_MAX : w->window;
     a.S = all ? 0 : w->sinks;
     a.scale = w->scale > 0.f ? w->scale : 1.0f / std::sqrt(float(w->head_dim));
-    a.by_rows = grid_by_rows(w->batch, w->heads_q, w->seq, w->tokens);
+    a.by_rows = grid_by_rows(w->batch, w->heads_q, a.seq, w->tokens);
     return a;
 }
 

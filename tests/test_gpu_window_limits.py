@@ -160,3 +160,16 @@ def test_window_packed_by_rows_captured(gpu):
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("W,S", [(0, 0), (50, 3)])
+def test_window_packed_longest_beyond_the_rows(gpu, W, S):
+    """`seq` of 2^30, 128 heads on one: the walks (2^31 tiles by that length) are those of the tensors' rows."""
+    lens, d = [200, 0, 100], 64
+    x, starts, total = _packed(11, lens, 0, 0, 128, 1, d, gpu)
+    st = starts.to(gpu)
+    want = _run(ms.make_window(3, total, 128, 1, d, W, S, tokens=total), x, st)
+    got = _run(ms.make_window(3, 1 << 30, 128, 1, d, W, S, tokens=total), x, st)
+    for a, b in zip((*got[:2], *got[2]), (*want[:2], *want[2])):
+        assert torch.equal(a, b)
+    _check(*x, *got, W, S, d ** -0.5, 200, 100)

@@ -2,6 +2,8 @@
 0 for a call that is refused)."""
 import ctypes
 
+import pytest
+
 import paper_2510_18830_amd as ms
 
 P16 = 4096
@@ -37,3 +39,10 @@ def test_window_packed_is_limited_by_its_rows():
             assert rows <= need <= 1.02 * rows + (3 * groups + 2048 * heads_kv) * 2 * 128 * d * 4 * (S > 0)
     win = ms.make_window(1 << 21, 1 << 20, 8, 8, 64, 100, 4, tokens=1 << 20)
     assert ms.window_bwd_workspace_bytes(win) == 0 and "blocks of 64 rows" in ms.lib().msparse_last_error().decode()
+
+
+@pytest.mark.parametrize("W,S", [(0, 0), (100, 4), (100, 290)])
+def test_window_packed_longest_beyond_the_rows(W, S):
+    """No document is longer than the tensors: `seq` beyond them plans what `tokens` plans."""
+    need = [ms.window_bwd_workspace_bytes(ms.make_window(3, seq, 128, 1, 64, W, S, tokens=300)) for seq in (300, 301, 1 << 30)]
+    assert need[0] == need[1] == need[2] > 0
