@@ -450,8 +450,7 @@ MSPARSE_API msparse_status msparse_window_bwd(const msparse_window* win, const i
  *   page_table int32 [batch, width]: page of the tokens 64 i .. 64 i + 63 of
  *            sequence b at [b, i].  Sequences may share pages that neither
  *            appends to.  Entries that no token needs are not read.
- *   lens     int32 [batch]: tokens in the cache (0: none; at most 2^31 - 64, and a
- *            longer one counts as that)
+ *   lens     int32 [batch]: tokens in the cache (0: none)
  * An entry outside [0, pages), and a token at or beyond 64 width, has no page: it
  * is not written by an append and not seen by the attention. */
 typedef struct {
@@ -495,8 +494,8 @@ MSPARSE_API msparse_status msparse_cache_append(const msparse_cache* cache, int3
  * and values (their own included: append first, then add the counts to lens):
  * row t of sequence b has position lens[b] - tokens + t, past the table's end too,
  * and sees what a row of msparse_window_fwd at that position sees, where it has a
- * page.  A row before the sequence's start (lens[b] < tokens) or without a key gets
- * out = 0 and lse = -inf.
+ * page (lens above 2^31 - 64 count as that).  A row before the sequence's start
+ * (lens[b] < tokens) or without a key gets out = 0 and lse = -inf.
  *   q, out   bf16 [batch, heads_q, tokens, head_dim]
  *   lse      fp32 [batch, heads_q, tokens] (natural log) or NULL
  * Codes of free slots, and of tokens that no row of the call sees, may hold

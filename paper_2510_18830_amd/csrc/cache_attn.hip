@@ -736,6 +736,11 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
     CacheAttnPlan p{};
     const int64_t rows = Hq / Hkv * T;
     p.rt = rows <= 16 ? 1 : 2;
+    // From 33 rows on one tile over four waves, also where some stay without rows (us, tiles
+    // of 32 rows that walk the pages each -> this: 32 contexts of up to 16K, 28 over 4 heads,
+    // 5 to 9 tokens 146-150 -> 112-116; 16 of up to 8K, 32 over 8, head dim 64, 9 to 16
+    // tokens 46-49 -> 39-40; 4 of up to 8K, 16 over 2, 5 to 8 tokens 17.5-18.7 -> 17.9-19.4;
+    // 64 of up to 2K, 32 over 4, head dim 64, 6 to 8 tokens 24.4 -> 29.6)
     p.wr = rows <= 32 ? 1 : 4;
     p.rows = 16 * p.rt * p.wr;
     p.tiles = int32_t((rows + p.rows - 1) / p.rows);

@@ -1,6 +1,6 @@
 // Forward of the attention with a sliding window and sinks.  Bound by the matrix
 // cores and the softmax terms beside them, at long lengths by the power they take:
-// 16 over 2 heads x 32K, window 4096, 64 sinks, head dim 128: 1.07 ms, 980 TFLOP/s on
+// 16 over 2 heads x 32K, window 4096, 64 sinks, head dim 128: 1.09 ms, 960 TFLOP/s on
 // the visible pairs.
 //
 // One workgroup of four wavefronts per (sequence, query head, 128 rows), 32 rows
