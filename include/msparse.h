@@ -15,7 +15,9 @@
  * (merge_out_and_lse of Algorithm 2).  Beside it stand attention with a static
  * window-and-sinks pattern (forward and backward, any length, packed documents)
  * and a paged 8-bit cache for decoding after the prefill (append with rotation,
- * attention over the pages).
+ * attention over the pages, of consecutive tokens or of drafted trees, the
+ * moves of an accepted path's tokens and of whole sequences among the pages),
+ * and rotation by positions on several axes for training.
  *
  * Conventions shared by every entry point (the static pattern and the cache say
  * where theirs differ: strides, lengths, gradient types)
@@ -440,6 +442,37 @@ MSPARSE_API msparse_status msparse_window_bwd(const msparse_window* win, const i
                                               size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Rotation by positions on several axes (text: one; images and video: time, row,
+ * column).  Columns (i, i + head_dim / 2) of token t turn by the angle
+ * p[axis[i]][t] inv_freq[i]:
+ *   x1' = x1 cos - x2 sin,   x2' = x2 cos + x1 sin.
+ * All arrays are on the device:
+ *   at       int32 [axes, batch, tokens], any values (angles are reduced in 64 bits)
+ *   axis     int32 [head_dim / 2], NULL: axis 0 for every pair.  An axis outside
+ *            [0, axes) leaves its pairs as they are (rotation of a part of the columns)
+ *   inv_freq fp32 [head_dim / 2]
+ * axes is 1 to 4. */
+typedef struct {
+    const int32_t* at;
+    const int32_t* axis;
+    const float* inv_freq;
+    int32_t axes;
+} msparse_positions;
+
+enum { MSPARSE_BF16 = 0, MSPARSE_F32 = 1 };
+
+/* Queries [batch, heads_q, tokens, head_dim] and keys [batch, heads_kv, ...] of one type
+ * (MSPARSE_BF16 or MSPARSE_F32), rotated into q_out and k_out, which may be q and k (same
+ * strides).  heads_kv = 0: no keys (k and k_out NULL).  Products and sums are fp32, the
+ * result is rounded once.  inverse != 0 turns back: the gradients of q and k from those of
+ * q_out and k_out (fp32 as msparse_attn_bwd gives them, bf16 as msparse_window_bwd does).
+ * tokens = 0 does nothing.  No workspace. */
+MSPARSE_API msparse_status msparse_rotate(int32_t batch, int32_t tokens, int32_t heads_q, int32_t heads_kv,
+                                          int32_t head_dim, int32_t type, const msparse_positions* positions,
+                                          int32_t inverse, const msparse_tensor* q, const msparse_tensor* k,
+                                          const msparse_tensor* q_out, const msparse_tensor* k_out, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Paged 8-bit cache of keys and values, for decoding after a prefill.  A page
  * holds 64 tokens of every KV head as e4m3 codes (OCP float8, 4 exponent and 3
  * mantissa bits), with an fp32 scale per page and head for keys and one for
@@ -490,6 +523,16 @@ MSPARSE_API msparse_status msparse_cache_append(const msparse_cache* cache, int3
                                                 const msparse_tensor* v, const msparse_tensor* q_out,
                                                 const float* inv_freq, const int32_t* counts, void* stream);
 
+/* msparse_cache_append with the tokens' positions given: token t still takes the place
+ * lens[b] + t of its sequence, but its key and query turn by positions (of [batch, tokens],
+ * those behind the counts too, since all queries are rotated).  For several axes, and for
+ * the nodes of a drafted tree, which share positions (msparse_tree_mask). */
+MSPARSE_API msparse_status msparse_cache_append_at(const msparse_cache* cache, int32_t heads_q, int32_t tokens,
+                                                   const msparse_tensor* q, const msparse_tensor* k,
+                                                   const msparse_tensor* v, const msparse_tensor* q_out,
+                                                   const msparse_positions* positions, const int32_t* counts,
+                                                   void* stream);
+
 /* Attention of the newest `tokens` tokens of every sequence over its cached keys
  * and values (their own included: append first, then add the counts to lens):
  * row t of sequence b has position lens[b] - tokens + t, past the table's end too,
@@ -507,6 +550,83 @@ MSPARSE_API msparse_status msparse_cache_attn(const msparse_cache* cache, int32_
                                               int32_t window, int32_t sinks, float scale, const msparse_tensor* q,
                                               const msparse_tensor* out, float* lse, void* workspace,
                                               size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Drafted trees over the cache.  A sequence's tree has counts[b] <= tokens nodes (counts
+ * int32 [batch] on the device; NULL: `tokens` each, up to 1024), which lie behind its
+ * context in the cache, node t in the place context + t.  Node t follows the node
+ * parents[b, t] < t (anything else: the context's last token); its position is context +
+ * the number of its ancestors.  One step of decoding:
+ *   msparse_tree_mask         positions and masks, once for all layers
+ *   msparse_cache_append_at   the nodes into the cache; add the counts to lens
+ *   msparse_cache_tree_attn   their attention
+ *   msparse_cache_keep        the accepted nodes to the places behind the context; set lens
+ *                             to context + kept
+ *
+ * msparse_tree_mask (lens: the contexts' lengths):
+ *   parents   int32 [batch, tokens]
+ *   positions int32 [batch, tokens]; of rows behind the counts: the context's length
+ *   seen      int32 [batch, tokens, (tokens + 31) / 32]: bit u % 32 of word u / 32 of row t
+ *             says whether node t sees node u: itself and its ancestors, as far as
+ *             window and sinks leave them visible by their positions (see
+ *             msparse_window; window = 0: all) */
+MSPARSE_API msparse_status msparse_tree_mask(int32_t batch, int32_t tokens, const int32_t* parents,
+                                             const int32_t* lens, const int32_t* counts, int32_t window,
+                                             int32_t sinks, int32_t* positions, int32_t* seen, void* stream);
+
+/* Attention of the trees' nodes over the cached tokens.  cache->lens counts the nodes (counts
+ * above it count as it).  Row t < counts[b] sees the context's tokens that a row of
+ * msparse_window_fwd at positions[b, t] sees, and the nodes u < counts[b] of its bits of seen
+ * (any, not only a tree's), where they have a page.  positions is read with a window only (NULL without; values outside
+ * the nodes' places count as the nearest of them).  A row behind the counts, or without a
+ * key, gets out = 0 and lse = -inf.  All else as msparse_cache_attn. */
+MSPARSE_API size_t msparse_cache_tree_attn_workspace(const msparse_cache* cache, int32_t heads_q, int32_t tokens);
+MSPARSE_API msparse_status msparse_cache_tree_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens,
+                                                   int32_t window, int32_t sinks, float scale,
+                                                   const msparse_tensor* q, const int32_t* seen,
+                                                   const int32_t* positions, const int32_t* counts,
+                                                   const msparse_tensor* out, float* lse, void* workspace,
+                                                   size_t workspace_bytes, void* stream);
+
+/* Moves the kept tokens among the last counts[b] (NULL: `tokens`) of each sequence to the
+ * front of these: with L0 = lens[b] - counts[b], the place L0 + i takes the key and value of
+ * the place L0 + path[b, i], for i < kept[b] (at most counts[b]).  path int32 [batch,
+ * tokens] ascends, each node once; kept int32 [batch].  lens is read, not written: the
+ * sequence has L0 + kept[b] tokens afterwards.
+ * Values move exactly while their page's scale holds them.  A page whose moved tokens come
+ * from other pages takes the smallest power of two that these need if that is above its
+ * scale; its tokens then change codes as in an append.  Places from L0 + kept[b] on are left
+ * as they are.  An entry path[b, i] <= i or beyond the counts, and one without a page, leaves
+ * its place as it is.  Pages that a call writes to stand in the tables once, as in an append. */
+MSPARSE_API msparse_status msparse_cache_keep(const msparse_cache* cache, int32_t tokens, const int32_t* path,
+                                              const int32_t* kept, const int32_t* counts, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Sequences that continue others: forks, growth and release of pages in one call.
+ * refs int32 [pages] says how many table entries hold a page (of this table, and of
+ * others that share the pool); a page is free where it is 0.  Every entry of
+ * cache->page_table inside [0, pages) holds its page, those of places without tokens too;
+ * write -1 where there is none.  New sequence n of `sequences` (1 to 65536, as many as the
+ * cache has or not) continues sequence src[n] (int32, device; outside [0, batch): an empty
+ * one) with all its tokens and gets the pages for max(room[n], its tokens) tokens, as far
+ * as the width goes (room NULL: its tokens alone):
+ *   - full pages are shared;
+ *   - the page that holds the last tokens but is not full, and pages without tokens, stay
+ *     with the first n that continues the sequence; the others get a copy of the one and
+ *     new pages for the rest, so that no page is shared that a sequence appends to;
+ *   - entries that no new sequence keeps are given back.
+ * Free pages (those given back among them) are allotted in the order of n and of the places,
+ * the lowest page first.  A place for which none is left, and one of tokens that had no page,
+ * holds -1; where that is the page to be copied, the sequence ends with its full pages.
+ * Outputs: refs_out int32 [pages] (may be refs), table_out int32 [sequences, width] and
+ * lens_out int32 [sequences] (neither may share memory with the inputs), missing int32
+ * [sequences]: pages that were asked for and not there.
+ * Equal calls give equal tables.  A call that only frees continues nothing: src = -1. */
+MSPARSE_API size_t msparse_cache_fork_workspace(const msparse_cache* cache, int32_t sequences);
+MSPARSE_API msparse_status msparse_cache_fork(const msparse_cache* cache, int32_t sequences, const int32_t* src,
+                                              const int32_t* room, const int32_t* refs, int32_t* refs_out,
+                                              int32_t* table_out, int32_t* lens_out, int32_t* missing,
+                                              void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Kernel-level tracing for measurement.  While enabled, every kernel the

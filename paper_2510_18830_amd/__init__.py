@@ -59,6 +59,10 @@ class CacheStruct(ctypes.Structure):
                 ("pages", c_i32), ("width", c_i32), ("batch", c_i32), ("heads_kv", c_i32), ("head_dim", c_i32)]
 
 
+class PositionsStruct(ctypes.Structure):
+    _fields_ = [("at", c_vp), ("axis", c_vp), ("inv_freq", c_vp), ("axes", c_i32)]
+
+
 class TraceEntry(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", c_i32), ("total_ms", ctypes.c_double)]
 
@@ -98,6 +102,16 @@ _SIGS = {
     "msparse_cache_attn_workspace": (c_sz, [_P(CacheStruct), c_i32, c_i32]),
     "msparse_cache_attn": (c_i32, [_P(CacheStruct), c_i32, c_i32, c_i32, c_i32, c_f32, _P(Tensor), _P(Tensor), c_vp,
                                    c_vp, c_sz, c_vp]),
+    "msparse_rotate": (c_i32, [c_i32] * 6 + [_P(PositionsStruct), c_i32] + [_P(Tensor)] * 4 + [c_vp]),
+    "msparse_cache_append_at": (c_i32, [_P(CacheStruct), c_i32, c_i32] + [_P(Tensor)] * 4 + [_P(PositionsStruct), c_vp,
+                                                                                            c_vp]),
+    "msparse_tree_mask": (c_i32, [c_i32, c_i32, c_vp, c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp]),
+    "msparse_cache_tree_attn_workspace": (c_sz, [_P(CacheStruct), c_i32, c_i32]),
+    "msparse_cache_tree_attn": (c_i32, [_P(CacheStruct), c_i32, c_i32, c_i32, c_i32, c_f32, _P(Tensor), c_vp, c_vp,
+                                        c_vp, _P(Tensor), c_vp, c_vp, c_sz, c_vp]),
+    "msparse_cache_keep": (c_i32, [_P(CacheStruct), c_i32, c_vp, c_vp, c_vp, c_vp]),
+    "msparse_cache_fork_workspace": (c_sz, [_P(CacheStruct), c_i32]),
+    "msparse_cache_fork": (c_i32, [_P(CacheStruct), c_i32] + [c_vp] * 8 + [c_sz, c_vp]),
     "msparse_attn_bwd": (c_i32, [_P(Dims), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, _P(IndexStruct), c_vp, c_vp,
                                  c_vp, c_i32, c_vp, c_sz, c_vp]),
 }
@@ -378,10 +392,11 @@ def _arg(t, name, shape, dtype, device):
     return t.data_ptr()
 
 
-def _rows(t, name, shape, device):
-    """A bf16 tensor [batch, heads, tokens, head_dim] of any strides with contiguous rows, as an msparse_tensor."""
-    if t.dtype != _BF16 or t.shape != shape or t.device != device:
-        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}; expected {_BF16} {tuple(shape)} on {device}")
+def _rows(t, name, shape, device, dtype=_BF16):
+    """A tensor [batch, heads, tokens, head_dim] (bf16, if no other type is named) of any strides with contiguous rows,
+    as an msparse_tensor."""
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}; expected {dtype} {tuple(shape)} on {device}")
     batch, head, token, column = t.stride()
     if column != 1:
         _refuse(f"{name} has rows of stride {column}")
@@ -493,6 +508,47 @@ def window_bwd(win: Window, q, k, v, out, dout, lse, starts=None, dq=None, dk=No
     return dq, dk, dv
 
 
+# ------------------------------------------------------------------ rotation
+def _positions(positions, inv_freq, axis, batch, tokens, head_dim, device):
+    """msparse_positions of int32 positions [axes, batch, tokens] ([batch, tokens]: one axis)."""
+    axes = positions.shape[0] if positions.dim() == 3 else 1
+    shape = (axes, batch, tokens) if positions.dim() == 3 else (batch, tokens)
+    return PositionsStruct(_arg(positions, "positions", shape, _I32, device),
+                           None if axis is None else _arg(axis, "axis", (head_dim // 2,), _I32, device),
+                           _arg(inv_freq, "inv_freq", (head_dim // 2,), _F32, device), axes)
+
+
+def rotate(q, k, positions, inv_freq, axis=None, inverse=False, q_out=None, k_out=None, stream=None):
+    """msparse_rotate: q [B, Hq, N, d] and k [B, Hkv, N, d] (None: no keys), both bf16 or both fp32, turned by int32
+    positions [axes, B, N] ([B, N]: one axis); pair i of the columns goes by positions[axis[i]] (None: the first) and
+    inv_freq [d / 2].  inverse: turned back, the gradients of q and k from those of the results.  Returns (q_out,
+    k_out)."""
+    dev = q.device
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return rotate(q, k, positions, inv_freq, axis, inverse, q_out, k_out)
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        _refuse(f"q is {tuple(q.shape)}, k {None if k is None else tuple(k.shape)}")
+    if q.dtype not in (_BF16, _F32):
+        _refuse(f"q is {q.dtype}; expected {_BF16} or {_F32}")
+    B, heads_q, N, d = q.shape
+    to = q.dtype
+    tq = _rows(q, "q", q.shape, dev, to)
+    q_out, tqo = _like(q) if q_out is None else (q_out, _rows(q_out, "q_out", q.shape, dev, to))
+    heads_kv, tk, tko = 0, None, None
+    if k is not None:
+        heads_kv = k.shape[1]
+        ks = (B, heads_kv, N, d)
+        tk = _rows(k, "k", ks, dev, to)
+        k_out, tko = _like(k) if k_out is None else (k_out, _rows(k_out, "k_out", ks, dev, to))
+    elif k_out is not None:
+        _refuse("k_out without k")
+    pos = _positions(positions, inv_freq, axis, B, N, d, dev)
+    _check(lib().msparse_rotate(B, N, heads_q, heads_kv, d, int(to == _F32), pos, int(bool(inverse)), tq, tk, tqo, tko,
+                                _current(dev)))
+    return q_out, k_out
+
+
 # ------------------------------------------------------------------ paged cache
 @dataclass
 class Cache:
@@ -525,14 +581,15 @@ def _cache(cache, page_table, lens, device):
                        pages, width, B, heads, d)
 
 
-def cache_append(cache: Cache, page_table, lens, k, v, q=None, inv_freq=None, counts=None, q_out=None, stream=None):
+def cache_append(cache: Cache, page_table, lens, k, v, q=None, inv_freq=None, counts=None, q_out=None, stream=None,
+                 positions=None, axis=None):
     """msparse_cache_append: k, v bf16 [B, Hkv, T, d] after the lens [B] tokens that the sequences hold (counts [B] of
     the T tokens; None: all); returns the rotated q (bf16 [B, Hq, T, d], all T rows), None without one.  lens is not
-    changed."""
+    changed.  With positions (int32 [axes, B, T] or [B, T]) and axis as in rotate: msparse_cache_append_at."""
     dev = k.device
     if _elsewhere(dev, stream):
         with _enter(dev, stream):
-            return cache_append(cache, page_table, lens, k, v, q, inv_freq, counts, q_out)
+            return cache_append(cache, page_table, lens, k, v, q, inv_freq, counts, q_out, None, positions, axis)
     c = _cache(cache, page_table, lens, dev)
     if k.dim() != 4:
         _refuse(f"k is {tuple(k.shape)}")
@@ -553,8 +610,16 @@ def cache_append(cache: Cache, page_table, lens, k, v, q=None, inv_freq=None, co
             tqo = _rows(q_out, "q_out", qs, dev)
     elif q_out is not None:
         _refuse("q_out without q")
-    freq = None if inv_freq is None else _arg(inv_freq, "inv_freq", (c.head_dim // 2,), _F32, dev)
     cnt = None if counts is None else _arg(counts, "counts", (c.batch,), _I32, dev)
+    if positions is not None:
+        if inv_freq is None:
+            _refuse("positions without inv_freq")
+        pos = _positions(positions, inv_freq, axis, c.batch, T, c.head_dim, dev)
+        _check(lib().msparse_cache_append_at(c, heads_q, T, tq, tk, tv, tqo, pos, cnt, _current(dev)))
+        return q_out
+    if axis is not None:
+        _refuse("axis without positions")
+    freq = None if inv_freq is None else _arg(inv_freq, "inv_freq", (c.head_dim // 2,), _F32, dev)
     _check(lib().msparse_cache_append(c, heads_q, T, tq, tk, tv, tqo, freq, cnt,
                                       _current(dev)))
     return q_out
@@ -593,6 +658,121 @@ def cache_attn(cache: Cache, page_table, lens, q, window=0, sinks=0, scale=0.0, 
     workspace, at, room = _room(workspace, lib().msparse_cache_attn_workspace(c, heads_q, T), dev)
     _check(lib().msparse_cache_attn(c, heads_q, T, window, sinks, scale, tq, to, tl, at, room, _current(dev)))
     return out, lse
+
+
+# ------------------------------------------------------------------ drafted trees, pages
+def tree_mask(parents, lens, counts=None, window=0, sinks=0, positions=None, seen=None, stream=None):
+    """msparse_tree_mask: of trees with int32 parents [B, T] behind contexts of lens [B] tokens (counts [B] nodes; None:
+    T), returns (positions int32 [B, T], seen int32 [B, T, (T + 31) // 32])."""
+    dev = parents.device
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return tree_mask(parents, lens, counts, window, sinks, positions, seen)
+    if parents.dim() != 2:
+        _refuse(f"parents is {tuple(parents.shape)}")
+    B, T = parents.shape
+    positions = torch.empty((B, T), dtype=_I32, device=dev) if positions is None else positions
+    seen = torch.empty((B, T, (T + 31) // 32), dtype=_I32, device=dev) if seen is None else seen
+    _check(lib().msparse_tree_mask(B, T, _arg(parents, "parents", (B, T), _I32, dev), _arg(lens, "lens", (B,), _I32, dev),
+                                   None if counts is None else _arg(counts, "counts", (B,), _I32, dev), window, sinks,
+                                   _arg(positions, "positions", (B, T), _I32, dev),
+                                   _arg(seen, "seen", (B, T, (T + 31) // 32), _I32, dev), _current(dev)))
+    return positions, seen
+
+
+def cache_tree_attn_workspace_bytes(cache: Cache, page_table, heads_q, tokens) -> int:
+    pages, heads, _, d = cache.k.shape
+    B, width = page_table.shape
+    return int(lib().msparse_cache_tree_attn_workspace(CacheStruct(None, None, None, None, None, None, pages, width, B,
+                                                                   heads, d), heads_q, tokens))
+
+
+def cache_tree_attn(cache: Cache, page_table, lens, q, seen, positions=None, counts=None, window=0, sinks=0, scale=0.0,
+                    out=None, lse=None, workspace=None, stream=None):
+    """msparse_cache_tree_attn: the nodes' queries (bf16 [B, Hq, T, d], rotated) over the cached contexts and the nodes of
+    seen (tree_mask); lens [B] counts the nodes (counts [B] of them; None: T).  positions are needed with a window.
+    Returns (out bf16 like q, lse fp32 [B, Hq, T])."""
+    dev = q.device
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return cache_tree_attn(cache, page_table, lens, q, seen, positions, counts, window, sinks, scale, out, lse,
+                                   workspace)
+    c = _cache(cache, page_table, lens, dev)
+    if q.dim() != 4:
+        _refuse(f"q is {tuple(q.shape)}")
+    heads_q, T = q.shape[1], q.shape[2]
+    qs = (c.batch, heads_q, T, c.head_dim)
+    tq = _rows(q, "q", qs, dev)
+    if out is None:
+        out, to = _like(q)
+    else:
+        to = _rows(out, "out", qs, dev)
+    if lse is None:
+        lse = torch.empty(qs[:3], dtype=_F32, device=dev)
+        tl = lse.data_ptr()
+    else:
+        tl = _arg(lse, "lse", qs[:3], _F32, dev)
+    workspace, at, room = _room(workspace, lib().msparse_cache_tree_attn_workspace(c, heads_q, T), dev)
+    _check(lib().msparse_cache_tree_attn(
+        c, heads_q, T, window, sinks, scale, tq, _arg(seen, "seen", (c.batch, T, (T + 31) // 32), _I32, dev),
+        None if positions is None else _arg(positions, "positions", (c.batch, T), _I32, dev),
+        None if counts is None else _arg(counts, "counts", (c.batch,), _I32, dev), to, tl, at, room, _current(dev)))
+    return out, lse
+
+
+def cache_keep(cache: Cache, page_table, lens, path, kept, counts=None, stream=None):
+    """msparse_cache_keep: of the last counts [B] tokens of each sequence (None: T), the kept [B] ones of the ascending
+    int32 path [B, T] move to the front of them.  lens is not changed: the new lengths are lens - counts + kept."""
+    dev = path.device
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return cache_keep(cache, page_table, lens, path, kept, counts)
+    c = _cache(cache, page_table, lens, dev)
+    if path.dim() != 2:
+        _refuse(f"path is {tuple(path.shape)}")
+    T = path.shape[1]
+    _check(lib().msparse_cache_keep(c, T, _arg(path, "path", (c.batch, T), _I32, dev),
+                                    _arg(kept, "kept", (c.batch,), _I32, dev),
+                                    None if counts is None else _arg(counts, "counts", (c.batch,), _I32, dev),
+                                    _current(dev)))
+
+
+def cache_fork_workspace_bytes(cache: Cache, page_table, sequences) -> int:
+    pages, heads, _, d = cache.k.shape
+    B, width = page_table.shape
+    return int(lib().msparse_cache_fork_workspace(CacheStruct(None, None, None, None, None, None, pages, width, B, heads,
+                                                              d), sequences))
+
+
+def cache_fork(cache: Cache, page_table, lens, refs, src, room=None, refs_out=None, page_table_out=None, lens_out=None,
+               missing=None, workspace=None, stream=None):
+    """msparse_cache_fork: new sequences that continue the sequences src [N] (int32; -1: an empty one), with pages for
+    room [N] tokens each (None: for those they hold); refs int32 [pages] counts the holders of a page.  Returns
+    (page_table int32 [N, width], lens [N], refs, missing [N])."""
+    dev = src.device
+    if _elsewhere(dev, stream):
+        with _enter(dev, stream):
+            return cache_fork(cache, page_table, lens, refs, src, room, refs_out, page_table_out, lens_out, missing,
+                              workspace)
+    c = _cache(cache, page_table, lens, dev)
+    if src.dim() != 1:
+        _refuse(f"src is {tuple(src.shape)}")
+    N = src.shape[0]
+
+    def new(t, name, shape):
+        t = torch.empty(shape, dtype=_I32, device=dev) if t is None else t
+        return t, _arg(t, name, shape, _I32, dev)
+
+    refs_out, to_refs = new(refs_out, "refs_out", (c.pages,))
+    page_table_out, to_table = new(page_table_out, "page_table_out", (N, c.width))
+    lens_out, to_lens = new(lens_out, "lens_out", (N,))
+    missing, to_missing = new(missing, "missing", (N,))
+    workspace, at, size = _room(workspace, lib().msparse_cache_fork_workspace(c, N), dev)
+    _check(lib().msparse_cache_fork(c, N, _arg(src, "src", (N,), _I32, dev),
+                                    None if room is None else _arg(room, "room", (N,), _I32, dev),
+                                    _arg(refs, "refs", (c.pages,), _I32, dev), to_refs, to_table, to_lens, to_missing, at,
+                                    size, _current(dev)))
+    return page_table_out, lens_out, refs_out, missing
 
 
 def default_scale(head_dim: int) -> float:

@@ -15,6 +15,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "operands.h"
+#include "rotate.h"
 #include "window.h"
 
 using namespace msparse;
@@ -969,9 +970,30 @@ static void set_strides(int64_t* s, const msparse_tensor* t) {
     s[2] = t->token;
 }
 
-msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q, int32_t tokens, const msparse_tensor* q,
-                                    const msparse_tensor* k, const msparse_tensor* v, const msparse_tensor* q_out,
-                                    const float* inv_freq, const int32_t* counts, void* stream) {
+// A rotation's output in its input's place has its strides.
+static msparse_status check_in_place(const msparse_tensor* x, const msparse_tensor* y, const char* name, int64_t batch,
+                                     int64_t heads, int64_t tokens) {
+    const bool same = (batch <= 1 || x->batch == y->batch) && (heads <= 1 || x->head == y->head) &&
+                      (tokens <= 1 || x->token == y->token);
+    if (x->data == y->data && !same) return fail(MSPARSE_ERR_INVALID, "%s rotated in place with other strides", name);
+    return MSPARSE_OK;
+}
+
+static msparse_status check_positions(const msparse_positions* p) {
+    if (!p || !p->at || !p->inv_freq) return fail(MSPARSE_ERR_INVALID, "positions or inv_freq NULL");
+    if (p->axes < 1 || p->axes > kMaxAxes) return fail(MSPARSE_ERR_INVALID, "%d axes (1 to %d)", p->axes, kMaxAxes);
+    if (odd_words({p->at, p->axis, p->inv_freq}))
+        return fail(MSPARSE_ERR_INVALID, "positions, axis or inv_freq not 4-byte aligned");
+    return MSPARSE_OK;
+}
+static Positions positions_of(const msparse_positions* p, int64_t batch, int64_t tokens) {
+    return Positions{p->at, p->axis, p->inv_freq, p->axes, batch * tokens};
+}
+
+static msparse_status append_impl(const msparse_cache* cache, int32_t heads_q, int32_t tokens, const msparse_tensor* q,
+                                  const msparse_tensor* k, const msparse_tensor* v, const msparse_tensor* q_out,
+                                  const float* inv_freq, const msparse_positions* pos, const int32_t* counts,
+                                  void* stream) {
     msparse_status st = check_cache(cache, heads_q, tokens);
     if (st) return st;
     if ((st = check_cache_memory(cache)) || tokens == 0) return st;
@@ -984,11 +1006,9 @@ msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q,
     if (q) {
         if ((st = check_tensor(q, "q", B, heads_q, tokens, d, false))) return st;
         if ((st = check_tensor(q_out, "q_out", B, heads_q, tokens, d, true))) return st;
-        const bool same = (B <= 1 || q->batch == q_out->batch) && (heads_q <= 1 || q->head == q_out->head) &&
-                          (tokens <= 1 || q->token == q_out->token);
-        if (q->data == q_out->data && !same)
-            return fail(MSPARSE_ERR_INVALID, "q rotated in place with other strides");
+        if ((st = check_in_place(q, q_out, "q", B, heads_q, tokens))) return st;
     }
+    if (pos && (st = check_positions(pos))) return st;
     AppendArgs a{};
     a.c = cache_view(cache);
     a.k = static_cast<const uint16_t*>(k->data);
@@ -1002,6 +1022,7 @@ msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q,
         set_strides(a.qos, q_out);
     }
     a.freq = inv_freq;
+    if (pos) a.pos = positions_of(pos, B, tokens);
     a.counts = counts;
     a.Hq = heads_q;
     a.T = tokens;
@@ -1013,6 +1034,75 @@ msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q,
         return fail(MSPARSE_ERR_UNSUPPORTED, "%lld pages of %d heads in one call", (long long)(B * P), heads_q);
     hipStream_t s = static_cast<hipStream_t>(stream);
     return check_hip(launch_cache_append(a, s), s, "cache append");
+}
+
+msparse_status msparse_cache_append(const msparse_cache* cache, int32_t heads_q, int32_t tokens, const msparse_tensor* q,
+                                    const msparse_tensor* k, const msparse_tensor* v, const msparse_tensor* q_out,
+                                    const float* inv_freq, const int32_t* counts, void* stream) {
+    return append_impl(cache, heads_q, tokens, q, k, v, q_out, inv_freq, nullptr, counts, stream);
+}
+
+msparse_status msparse_cache_append_at(const msparse_cache* cache, int32_t heads_q, int32_t tokens,
+                                       const msparse_tensor* q, const msparse_tensor* k, const msparse_tensor* v,
+                                       const msparse_tensor* q_out, const msparse_positions* positions,
+                                       const int32_t* counts, void* stream) {
+    if (!positions) return fail(MSPARSE_ERR_INVALID, "positions are NULL");
+    return append_impl(cache, heads_q, tokens, q, k, v, q_out, nullptr, positions, counts, stream);
+}
+
+msparse_status msparse_rotate(int32_t batch, int32_t tokens, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                              int32_t type, const msparse_positions* positions, int32_t inverse,
+                              const msparse_tensor* q, const msparse_tensor* k, const msparse_tensor* q_out,
+                              const msparse_tensor* k_out, void* stream) {
+    if (batch < 1 || heads_q < 1 || heads_kv < 0 || tokens < 0)
+        return fail(MSPARSE_ERR_INVALID, "batch, heads_q must be >= 1, heads_kv and tokens >= 0");
+    if (head_dim != 64 && head_dim != 128)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", head_dim);
+    if (type != MSPARSE_BF16 && type != MSPARSE_F32) return fail(MSPARSE_ERR_INVALID, "type %d", type);
+    const int64_t heads = int64_t(heads_q) + heads_kv;
+    if (tokens > (1 << 30) || int64_t(batch) * tokens > ((int64_t(1) << 31) - 1) / heads)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "batch * heads * tokens exceeds 2^31 rows");
+    if (tokens == 0) return MSPARSE_OK;
+    msparse_status st = check_positions(positions);
+    if (st) return st;
+    if (heads_kv == 0 ? k || k_out : !k || !k_out)
+        return fail(MSPARSE_ERR_INVALID, "k and k_out go with heads_kv (%d)", heads_kv);
+    RotateArgs a{};
+    if ((st = check_tensor(q, "q", batch, heads_q, tokens, head_dim, false))) return st;
+    if ((st = check_tensor(q_out, "q_out", batch, heads_q, tokens, head_dim, true))) return st;
+    if ((st = check_in_place(q, q_out, "q", batch, heads_q, tokens))) return st;
+    a.q = q->data;
+    a.qout = q_out->data;
+    set_strides(a.qs, q);
+    set_strides(a.qos, q_out);
+    if (k) {
+        if ((st = check_tensor(k, "k", batch, heads_kv, tokens, head_dim, false))) return st;
+        if ((st = check_tensor(k_out, "k_out", batch, heads_kv, tokens, head_dim, true))) return st;
+        if ((st = check_in_place(k, k_out, "k", batch, heads_kv, tokens))) return st;
+        a.k = k->data;
+        a.kout = k_out->data;
+        set_strides(a.ks, k);
+        set_strides(a.kos, k_out);
+    }
+    a.pos = positions_of(positions, batch, tokens);
+    a.B = batch;
+    a.T = tokens;
+    a.Hq = heads_q;
+    a.Hkv = heads_kv;
+    a.d = head_dim;
+    a.inverse = inverse != 0;
+    a.f32 = type == MSPARSE_F32;
+    a.blocks = (tokens + kRotateTokens - 1) / kRotateTokens;
+    share_heads(a);
+    if (int64_t(batch) * a.blocks > 2 * kMaxGroups / a.shares)   // (of 256 threads)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%lld blocks of tokens in one call", (long long)batch * a.blocks);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return check_hip(launch_rotate(a, s), s, "rotate");
+}
+
+static msparse_status check_nodes(int32_t tokens) {
+    if (tokens > kMaxNodes) return fail(MSPARSE_ERR_UNSUPPORTED, "trees of %d nodes (up to %d)", tokens, kMaxNodes);
+    return MSPARSE_OK;
 }
 
 static size_t carve_cache_attn(const msparse_cache* c, const CacheAttnPlan& p, char* base, CacheAttnArgs* a) {
@@ -1032,11 +1122,20 @@ size_t msparse_cache_attn_workspace(const msparse_cache* cache, int32_t heads_q,
     return carve_cache_attn(cache, p, nullptr, &a);
 }
 
-msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens, int32_t window,
-                                  int32_t sinks, float scale, const msparse_tensor* q, const msparse_tensor* out,
-                                  float* lse, void* ws, size_t ws_bytes, void* stream) {
+size_t msparse_cache_tree_attn_workspace(const msparse_cache* cache, int32_t heads_q, int32_t tokens) {
+    if (check_cache(cache, heads_q, tokens) || check_nodes(tokens) || tokens == 0) return 0;
+    CacheAttnArgs a{};
+    const CacheAttnPlan p = cache_attn_plan(cache->batch, heads_q, cache->heads_kv, tokens, cache->width,
+                                            cache->head_dim, INT32_MAX, 0, true);
+    return carve_cache_attn(cache, p, nullptr, &a);
+}
+
+// tree: NULL, or the tree's part of the arguments (seen, at, counts)
+static msparse_status attn_impl(const msparse_cache* cache, int32_t heads_q, int32_t tokens, int32_t window,
+                                int32_t sinks, float scale, const msparse_tensor* q, const msparse_tensor* out,
+                                float* lse, const CacheAttnArgs* tree, void* ws, size_t ws_bytes, void* stream) {
     msparse_status st = check_cache(cache, heads_q, tokens);
-    if (st) return st;
+    if (st || (tree && (st = check_nodes(tokens)))) return st;
     if ((st = check_cache_memory(cache)) || tokens == 0) return st;
     if (window < 0 || sinks < 0) return fail(MSPARSE_ERR_INVALID, "window %d, sinks %d", window, sinks);
     if (!std::isfinite(scale)) return fail(MSPARSE_ERR_INVALID, "scale is not finite");
@@ -1046,10 +1145,16 @@ msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, i
     if ((st = check_tensor(out, "out", B, heads_q, tokens, d, true))) return st;
     if (misaligned({lse, ws})) return fail(MSPARSE_ERR_INVALID, "lse or workspace is not 16-byte aligned");
     const CacheAttnPlan p = cache_attn_plan(B, heads_q, cache->heads_kv, tokens, cache->width, d,
-                                            window == 0 ? INT32_MAX : window, window == 0 ? 0 : sinks);
+                                            window == 0 ? INT32_MAX : window, window == 0 ? 0 : sinks, tree != nullptr);
     if (cache_attn_groups(p, B) > kMaxGroups / cache->heads_kv)
         return fail(MSPARSE_ERR_UNSUPPORTED, "%lld row tiles of %d heads", (long long)(B * p.tiles), cache->heads_kv);
-    CacheAttnArgs a{};
+    if (tree) {
+        if (!tree->seen) return fail(MSPARSE_ERR_INVALID, "seen is NULL");
+        if (window > 0 && !tree->at) return fail(MSPARSE_ERR_INVALID, "a window without positions");
+        if (odd_words({tree->seen, tree->at, tree->counts}))
+            return fail(MSPARSE_ERR_INVALID, "seen, positions or counts not 4-byte aligned");
+    }
+    CacheAttnArgs a = tree ? *tree : CacheAttnArgs{};
     const size_t need = carve_cache_attn(cache, p, static_cast<char*>(ws), &a);
     if (need && (!ws || ws_bytes < need))
         return fail(MSPARSE_ERR_WORKSPACE, "cache attn workspace %zu < %zu bytes", ws_bytes, need);
@@ -1072,6 +1177,113 @@ msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, i
     a.slots = p.slots;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return check_hip(launch_cache_attn(a, p, s), s, "cache attn");
+}
+
+msparse_status msparse_cache_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens, int32_t window,
+                                  int32_t sinks, float scale, const msparse_tensor* q, const msparse_tensor* out,
+                                  float* lse, void* ws, size_t ws_bytes, void* stream) {
+    return attn_impl(cache, heads_q, tokens, window, sinks, scale, q, out, lse, nullptr, ws, ws_bytes, stream);
+}
+
+msparse_status msparse_cache_tree_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens, int32_t window,
+                                       int32_t sinks, float scale, const msparse_tensor* q, const int32_t* seen,
+                                       const int32_t* positions, const int32_t* counts, const msparse_tensor* out,
+                                       float* lse, void* ws, size_t ws_bytes, void* stream) {
+    CacheAttnArgs tree{};
+    tree.seen = seen;
+    tree.at = window > 0 ? positions : nullptr;
+    tree.counts = counts;
+    tree.words = (tokens + 31) / 32;
+    return attn_impl(cache, heads_q, tokens, window, sinks, scale, q, out, lse, &tree, ws, ws_bytes, stream);
+}
+
+// ------------------------------------------------------------------ drafted trees, pages
+msparse_status msparse_tree_mask(int32_t batch, int32_t tokens, const int32_t* parents, const int32_t* lens,
+                                 const int32_t* counts, int32_t window, int32_t sinks, int32_t* positions, int32_t* seen,
+                                 void* stream) {
+    if (batch < 1 || tokens < 0) return fail(MSPARSE_ERR_INVALID, "batch must be >= 1 and tokens >= 0");
+    msparse_status st = check_nodes(tokens);
+    if (st) return st;
+    if (batch > kMaxGroups) return fail(MSPARSE_ERR_UNSUPPORTED, "%d trees exceed 2^22", batch);
+    if (window < 0 || sinks < 0) return fail(MSPARSE_ERR_INVALID, "window %d, sinks %d", window, sinks);
+    if (tokens == 0) return MSPARSE_OK;
+    if (!parents || !lens || !positions || !seen) return fail(MSPARSE_ERR_INVALID, "tree array is NULL");
+    if (odd_words({parents, lens, counts, positions, seen}))
+        return fail(MSPARSE_ERR_INVALID, "tree array not 4-byte aligned");
+    const TreeMaskArgs a{parents, lens,   counts, positions, seen, batch, tokens, (tokens + 31) / 32,
+                         window == 0 ? INT32_MAX : window, window == 0 ? 0 : sinks};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return check_hip(launch_tree_mask(a, s), s, "tree mask");
+}
+
+msparse_status msparse_cache_keep(const msparse_cache* cache, int32_t tokens, const int32_t* path, const int32_t* kept,
+                                  const int32_t* counts, void* stream) {
+    msparse_status st = check_cache(cache, cache ? cache->heads_kv : 1, tokens);
+    if (st) return st;
+    if ((st = check_cache_memory(cache)) || tokens == 0) return st;
+    if (!path || !kept) return fail(MSPARSE_ERR_INVALID, "path or kept is NULL");
+    if (odd_words({path, kept, counts})) return fail(MSPARSE_ERR_INVALID, "path, kept or counts not 4-byte aligned");
+    if (cache->batch > kMaxGroups / cache->heads_kv)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "%d sequences of %d heads", cache->batch, cache->heads_kv);
+    KeepArgs a{};
+    a.c = cache_view(cache);
+    a.counts = counts;
+    a.path = path;
+    a.kept = kept;
+    a.T = tokens;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return check_hip(launch_cache_keep(a, s), s, "cache keep");
+}
+
+static msparse_status check_fork(const msparse_cache* c, int32_t sequences) {
+    msparse_status st = check_cache(c, c ? c->heads_kv : 1, 1);
+    if (st) return st;
+    if (sequences < 1) return fail(MSPARSE_ERR_INVALID, "%d sequences", sequences);
+    if (sequences > kMaxForks || c->batch > kMaxForks)
+        return fail(MSPARSE_ERR_UNSUPPORTED, "more than %d sequences", kMaxForks);
+    return MSPARSE_OK;
+}
+static size_t carve_cache_fork(const msparse_cache* c, int32_t sequences, char* base, ForkArgs* a) {
+    Carve w{base};
+    a->cap = int32_t(std::min(int64_t(sequences) * c->width, int64_t(c->pages)));
+    a->need = w.take<int32_t>(size_t(sequences));
+    a->list = w.take<int32_t>(size_t(1) + a->cap);
+    return w.off;
+}
+
+size_t msparse_cache_fork_workspace(const msparse_cache* cache, int32_t sequences) {
+    if (check_fork(cache, sequences)) return 0;
+    ForkArgs a{};
+    return carve_cache_fork(cache, sequences, nullptr, &a);
+}
+
+msparse_status msparse_cache_fork(const msparse_cache* cache, int32_t sequences, const int32_t* src, const int32_t* room,
+                                  const int32_t* refs, int32_t* refs_out, int32_t* table_out, int32_t* lens_out,
+                                  int32_t* missing, void* ws, size_t ws_bytes, void* stream) {
+    msparse_status st = check_fork(cache, sequences);
+    if (st) return st;
+    if ((st = check_cache_memory(cache))) return st;
+    if (!src || !refs || !refs_out || !table_out || !lens_out || !missing)
+        return fail(MSPARSE_ERR_INVALID, "fork array is NULL");
+    if (odd_words({src, room, refs, refs_out, table_out, lens_out, missing}))
+        return fail(MSPARSE_ERR_INVALID, "fork array not 4-byte aligned");
+    if (table_out == cache->page_table || lens_out == cache->lens)
+        return fail(MSPARSE_ERR_INVALID, "the new table or lens in the old ones' place");
+    if (misaligned({ws})) return fail(MSPARSE_ERR_INVALID, "workspace is not 16-byte aligned");
+    ForkArgs a{};
+    const size_t need = carve_cache_fork(cache, sequences, static_cast<char*>(ws), &a);
+    if (!ws || ws_bytes < need) return fail(MSPARSE_ERR_WORKSPACE, "cache fork workspace %zu < %zu bytes", ws_bytes, need);
+    a.c = cache_view(cache);
+    a.refs = refs;
+    a.src = src;
+    a.room = room;
+    a.refs_out = refs_out;
+    a.table_out = table_out;
+    a.lens_out = lens_out;
+    a.missing = missing;
+    a.N = sequences;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return check_hip(launch_cache_fork(a, s), s, "cache fork");
 }
 
 }  // extern "C"

@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "rotary.h"
 
 namespace msparse {
 
@@ -42,6 +43,7 @@ struct AppendArgs {
     int64_t qs[3], ks[3], vs[3], qos[3];      // strides: sequence, head, token
     uint16_t* qout;
     const float* freq;                        // [d / 2] or NULL: no rotation
+    Positions pos;                            // pos.at != NULL: in place of lens[b] + t and freq
     const int32_t* counts;                    // [B] or NULL: T
     int32_t Hq, T;
     int32_t P;                                // pages that T tokens can touch
@@ -90,6 +92,11 @@ struct CacheAttnArgs {
     float* po;              // [slots, Hkv, rows, d]: sums of the weighted values
     float* pml;             // [slots, Hkv, rows, 2]: running maximum (log2 units), sum of the weights
     int32_t slots;          // 0: one chunk per row tile, nothing to join
+    // a tree's nodes (seen != NULL): what row t of a sequence sees among them, its position, their number
+    const int32_t* seen;    // [B, T, words]
+    const int32_t* at;      // [B, T], NULL without a window
+    const int32_t* counts;  // [B] or NULL: T
+    int32_t words;
 };
 // Row tiles and chunks of a call.  rows = G T rows of a (sequence, KV head).
 struct CacheAttnPlan {
@@ -101,7 +108,45 @@ struct CacheAttnPlan {
 // workgroups per KV head
 inline int64_t cache_attn_groups(const CacheAttnPlan& p, int64_t B) { return p.slots > 0 ? p.slots : B * p.tiles; }
 CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width, int d, int64_t W,
-                              int64_t S);
+                              int64_t S, bool tree = false);
+constexpr int kMaxNodes = 1024;    // of a tree
+struct TreeMaskArgs {
+    const int32_t* parents; // [B, T]
+    const int32_t* lens;    // [B]: tokens before the tree
+    const int32_t* counts;  // [B] or NULL: T
+    int32_t* at;            // [B, T]
+    int32_t* seen;          // [B, T, words]
+    int32_t B, T, words, W, S;
+};
+hipError_t launch_tree_mask(const TreeMaskArgs& a, hipStream_t s);
+
+struct KeepArgs {
+    CacheView c;
+    const int32_t* counts;  // [B] or NULL: T
+    const int32_t* path;    // [B, T]
+    const int32_t* kept;    // [B]
+    int32_t T;
+};
+hipError_t launch_cache_keep(const KeepArgs& a, hipStream_t s);
+
+constexpr int kMaxForks = 65536;   // sequences: each looks through all sources
+struct ForkArgs {
+    CacheView c;
+    const int32_t* refs;    // [pages]
+    const int32_t* src;     // [N]
+    const int32_t* room;    // [N] or NULL
+    int32_t* refs_out;      // [pages], may be refs
+    int32_t* table_out;     // [N, width]
+    int32_t* lens_out;      // [N]
+    int32_t* missing;       // [N]
+    int32_t N;
+    // workspace
+    int32_t* need;          // [N]: pages asked for, then those asked for before
+    int32_t* list;          // [1 + N width at most, or pages]: their number, the free pages
+    int32_t cap;            // of the list
+};
+hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s);
+
 hipError_t launch_cache_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 
 }  // namespace msparse

@@ -13,6 +13,8 @@
 // copy of q alone 358); q passes by the caches (465 us through them).  Bound by latency
 // at one token.
 #include "cache.h"
+#include "codes.h"
+#include "rotary.h"
 #include "trace.h"
 
 namespace msparse {
@@ -21,85 +23,6 @@ namespace {
 
 constexpr int kThreads = kAppendThreads;
 
-// cos and sin of pos * freq for any position: the angle in revolutions as a sum of
-// two doubles, reduced to an eighth of a revolution, then the Taylor series (their
-// first missing terms are below 1e-12).
-struct Turn {
-    double c, s;
-};
-__device__ __forceinline__ Turn turn_by(double pos, float freq) {
-    constexpr double kInv = 0.15915494309189535, kInvLo = -9.839338337591243e-18;   // 1 / (2 pi) in two parts
-    const double x = pos * double(freq);
-    const double hi = x * kInv;
-    const double lo = __builtin_fma(x, kInv, -hi) + x * kInvLo;
-    const double r = (hi - __builtin_rint(hi)) + lo;        // revolutions in [-1/2, 1/2]
-    const double quarter = __builtin_rint(4.0 * r);
-    const double y = (r - 0.25 * quarter) * 6.283185307179586;   // [-pi/4, pi/4]
-    const double y2 = y * y;
-    double ps = 1.0 / 6227020800.0, pc = 1.0 / 479001600.0;
-    ps = __builtin_fma(ps, y2, -1.0 / 39916800.0);
-    pc = __builtin_fma(pc, y2, -1.0 / 3628800.0);
-    ps = __builtin_fma(ps, y2, 1.0 / 362880.0);
-    pc = __builtin_fma(pc, y2, 1.0 / 40320.0);
-    ps = __builtin_fma(ps, y2, -1.0 / 5040.0);
-    pc = __builtin_fma(pc, y2, -1.0 / 720.0);
-    ps = __builtin_fma(ps, y2, 1.0 / 120.0);
-    pc = __builtin_fma(pc, y2, 1.0 / 24.0);
-    ps = __builtin_fma(ps, y2, -1.0 / 6.0);
-    pc = __builtin_fma(pc, y2, -0.5);
-    const double fs = __builtin_fma(ps * y2, y, y), fc = __builtin_fma(pc, y2, 1.0);
-    const int n = int(quarter) & 3;
-    const double a = (n & 1) ? fs : fc, b = (n & 1) ? fc : fs;
-    return Turn{(n == 1 || n == 2) ? -a : a, (n & 2) ? -b : b};
-}
-
-// x1 c - x2 s and x2 c + x1 s, every product rounded: the same values whichever
-// of the two a fused form would leave unrounded
-__device__ __forceinline__ void rotate(float& x1, float& x2, float c, float s) {
-#pragma clang fp contract(off)
-    const float a = x1 * c, b = x2 * s, e = x2 * c, f = x1 * s;
-    x1 = a - b;
-    x2 = e + f;
-}
-
-__device__ __forceinline__ void unpack8(const u32x4& w, float* x) {
-    const uint32_t a[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        x[2 * j] = bf16_lo(a[j]);
-        x[2 * j + 1] = bf16_hi(a[j]);
-    }
-}
-
-// smallest power of two s >= 2^-126 with amax <= 448 s (448 = 0.875 * 2^9)
-__device__ __forceinline__ float code_scale(float amax) {
-    int e;
-    const float m = frexpf(amax, &e);
-    e = m <= 0.875f ? e - 9 : e - 8;
-    return amax > 0.f ? ldexpf(1.f, max(e, -126)) : 0x1p-126f;
-}
-__device__ __forceinline__ float finite_abs(float x) {
-    const float a = fabsf(x);
-    return a < INFINITY ? a : 0.f;
-}
-// e4m3 of x * inv, to nearest even; what is not finite becomes NaN
-__device__ __forceinline__ float code_input(float x, float inv) {
-    return fabsf(x) < INFINITY ? x * inv : __builtin_nanf("");
-}
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(code_input(a, inv), code_input(b, inv), 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(code_input(c, inv), code_input(d, inv), w, true);
-    return uint32_t(w);
-}
-// codes moved to a scale 1 / ratio times larger
-__device__ __forceinline__ uint32_t rescale4(uint32_t w, float ratio) {
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(w, 0) * ratio,
-                                            __builtin_amdgcn_cvt_f32_fp8(w, 1) * ratio, 0, false);
-    r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(w, 2) * ratio,
-                                        __builtin_amdgcn_cvt_f32_fp8(w, 3) * ratio, r, true);
-    return uint32_t(r);
-}
-
 // A head's new tokens of one page, 64 x d values over 256 threads: thread u takes
 // chunk u % C of the tokens u / C, u / C + R, ... (C chunks of 8 columns a row).
 template <int D>
@@ -107,7 +30,8 @@ struct Split {
     static constexpr int C = D / 8, R = kThreads / C, N = kPage / R;
 };
 
-template <int D>
+// AT: the tokens' positions are given.
+template <int D, bool AT>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, D == 128 ? 3 : 4)))
 cache_append_kernel(AppendArgs a) {
     constexpr int H2 = D / 2, C = Split<D>::C, R = Split<D>::R, N = Split<D>::N;
@@ -125,8 +49,18 @@ cache_append_kernel(AppendArgs a) {
     const int s0 = int(max(int64_t(len) - base, int64_t(0)));   // the page's first new slot
     const int t0 = int(base + s0 - len);           // its token of the call
     // The angles of the page's new tokens: a thread has one frequency and every
-    // STEP-th token, each turned on from the one before by a product in 64 bits.
+    // STEP-th token, each turned on from the one before by a product in 64 bits (AT: each
+    // from its own position).
     auto angles = [&](int tokens) {
+        if constexpr (AT) {
+            for (int x = tid; x < tokens * H2; x += kThreads) {
+                const Turn z = turn_at(a.pos, x % H2, int64_t(b) * a.T + t0 + x / H2);
+                cosv[x] = float(z.c);
+                sinv[x] = float(z.s);
+            }
+            __syncthreads();
+            return;
+        }
         if (a.freq) {
             constexpr int STEP = kThreads / H2;
             const int t = tid / H2;
@@ -190,7 +124,7 @@ cache_append_kernel(AppendArgs a) {
 #pragma unroll
             for (int u = 0; u < QN; ++u)
                 if (mine[u]) {
-                    if (a.freq) {
+                    if (AT || a.freq) {
                         const int at = (x0 + u * kThreads) / QC * H2 + 8 * c;
                         float x1[8], x2[8];
                         unpack8(l[u], x1);
@@ -257,7 +191,7 @@ cache_append_kernel(AppendArgs a) {
             const int t = min(r0 + n * R, m - 1);   // (past the last: zeros)
             unpack8(u32x4{klo[n].x, klo[n].y, khi[n].x, khi[n].y}, kx[n]);
             unpack8(vraw[n], vx[n]);
-            if (a.freq) {
+            if (AT || a.freq) {
                 const f32x4 cs = *reinterpret_cast<const f32x4*>(cosv + t * H2 + 4 * c);
                 const f32x4 sn = *reinterpret_cast<const f32x4*>(sinv + t * H2 + 4 * c);
 #pragma unroll
@@ -342,8 +276,13 @@ cache_append_kernel(AppendArgs a) {
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
     TraceScope _t("cache_append", s);
     const dim3 g(unsigned(int64_t(a.c.B) * a.P * (a.kv_shares + a.q_shares))), t(kThreads);
-    if (a.c.d == 128) hipLaunchKernelGGL(cache_append_kernel<128>, g, t, 0, s, a);
-    else hipLaunchKernelGGL(cache_append_kernel<64>, g, t, 0, s, a);
+    if (a.pos.at) {
+        if (a.c.d == 128) hipLaunchKernelGGL((cache_append_kernel<128, true>), g, t, 0, s, a);
+        else hipLaunchKernelGGL((cache_append_kernel<64, true>), g, t, 0, s, a);
+    } else {
+        if (a.c.d == 128) hipLaunchKernelGGL((cache_append_kernel<128, false>), g, t, 0, s, a);
+        else hipLaunchKernelGGL((cache_append_kernel<64, false>), g, t, 0, s, a);
+    }
     return hipGetLastError();
 }
 

@@ -1,0 +1,354 @@
+// Rearranging what the paged cache holds: the tokens of an accepted path move to the
+// places behind the context, and sequences continue others, their full pages shared.
+#include "cache.h"
+#include "codes.h"
+#include "trace.h"
+
+namespace msparse {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---------------------------------------------------------------- tokens
+// Slot L0 + i takes what slot L0 + path[i] holds (L0: the context's length).  A path ascends, so a
+// target's source lies at or behind it, and pages done in ascending order read what no earlier one
+// has written.  A workgroup owns the keys or the values of one head of a sequence and takes its
+// pages in turn: it reads the moved tokens' codes into LDS, finds the page's scale (its own, or what
+// tokens from other pages need) and writes them, older tokens too where the scale has grown.
+// Bound by latency: lengths, path, table, scales, codes, one after the other.
+template <int D>
+__global__ void __launch_bounds__(kThreads) cache_keep_kernel(KeepArgs a) {
+    constexpr int kRow = D + 16;
+    __shared__ __attribute__((aligned(16))) uint8_t tok[kPage * kRow];   // the moved tokens' codes, [slot][column]
+    __shared__ int from[kPage], slot_of[kPage];   // where a slot's token lies: page (-1: it stays) and slot in it
+    __shared__ float was_of[kPage];  // and its scale there
+    __shared__ float red[kThreads / 64];
+    const int tid = threadIdx.x;
+    const bool value = blockIdx.x & 1;
+    const int hk = (blockIdx.x >> 1) % a.c.Hkv, b = (blockIdx.x >> 1) / a.c.Hkv;
+    const int len = min(max(ldc(a.c.lens, b), 0), kMaxLength);
+    const int nodes = min(a.counts ? min(max(ldc(a.counts, b), 0), a.T) : a.T, len);
+    const int first = len - nodes, kept = min(max(ldc(a.kept, b), 0), nodes);
+    if (kept == 0) return;
+    uint8_t* codes = value ? a.c.v : a.c.k;
+    float* scales = value ? a.c.vs : a.c.ks;
+    auto base = [&](int page) { return codes + (int64_t(page) * a.c.Hkv + hk) * (kPage * D); };
+    for (int lp = first / kPage; lp <= (first + kept - 1) / kPage; ++lp) {
+        const int page = cache_page(a.c, b, lp);
+        if (page < 0) continue;
+        const int s0 = max(first - lp * kPage, 0), s1 = min(first + kept - lp * kPage, kPage);   // slots that take a token
+        float* scale = scales + int64_t(page) * a.c.Hkv + hk;
+        const float was = *scale;
+        if (tid < kPage) {
+            int f = -1;
+            if (tid >= s0 && tid < s1) {
+                const int i = lp * kPage + tid - first, u = a.path[int64_t(b) * a.T + i];
+                if (u > i && u < nodes) {
+                    const int slot = first + u, p = cache_page(a.c, b, slot / kPage);
+                    f = p;
+                    slot_of[tid] = slot % kPage;
+                }
+            }
+            from[tid] = f;
+            was_of[tid] = f < 0 || f == page ? was : scales[int64_t(f) * a.c.Hkv + hk];
+        }
+        __syncthreads();
+        // the moved tokens' codes; the largest value among those of other pages
+        float top = 0.f;
+        const int n = s1 - s0;
+        auto largest = [&](uint32_t w, float sc) {
+            const float x[4] = {__builtin_amdgcn_cvt_f32_fp8(w, 0), __builtin_amdgcn_cvt_f32_fp8(w, 1),
+                                __builtin_amdgcn_cvt_f32_fp8(w, 2), __builtin_amdgcn_cvt_f32_fp8(w, 3)};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, finite_abs(x[j] * sc));
+        };
+        if (!value) {
+            for (int x = tid; x < n * (D / 16); x += kThreads) {
+                const int s = s0 + x / (D / 16), c = x % (D / 16), f = from[s];
+                if (f < 0) continue;
+                const u32x4 w = *reinterpret_cast<const u32x4*>(base(f) + slot_of[s] * D + 16 * c);
+                *reinterpret_cast<u32x4*>(tok + s * kRow + 16 * c) = w;
+                if (f != page)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) largest(w[j], was_of[s]);
+            }
+        } else {
+            for (int x = tid; x < n * D; x += kThreads) {
+                const int s = s0 + x / D, row = x % D, f = from[s];
+                if (f < 0) continue;
+                const uint8_t w = base(f)[row * kPage + slot_of[s]];
+                tok[s * kRow + row] = w;
+                if (f != page) top = fmaxf(top, finite_abs(__builtin_amdgcn_cvt_f32_fp8(w, 0) * was_of[s]));
+            }
+        }
+        top = wave_max(top);
+        if ((tid & 63) == 0) red[tid >> 6] = top;
+        bool other = false;
+        for (int s = s0; s < s1; ++s) other |= from[s] >= 0 && from[s] != page;
+        __syncthreads();   // also: every read of this page is done
+        top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        const float now = other ? fmaxf(was, code_scale(top)) : was;
+        const bool grown = now > was;
+        // every word that holds a slot of a moved token, or, where the scale has grown, an older one
+        auto moved = [&](int s, uint32_t held, uint8_t own) -> uint32_t {   // the code of slot s
+            if (s >= s1) return held;
+            const int f = s < s0 ? -1 : from[s];
+            const uint32_t code = f < 0 ? held : own;
+            const float sc = f < 0 ? was : was_of[s];
+            return sc == now ? code : rescale4(code, sc / now) & 0xffu;
+        };
+        if (!value) {
+            const int r0 = grown ? 0 : s0;
+            for (int x = tid; x < (s1 - r0) * (D / 4); x += kThreads) {
+                const int s = r0 + x / (D / 4), c = x % (D / 4);
+                const int f = s < s0 ? -1 : from[s];
+                if (f < 0 && !grown) continue;
+                uint32_t* at = reinterpret_cast<uint32_t*>(base(page) + s * D) + c;
+                const uint32_t w = f < 0 ? *at : *reinterpret_cast<const uint32_t*>(tok + s * kRow + 4 * c);
+                const float sc = f < 0 ? was : was_of[s];
+                *at = sc == now ? w : rescale4(w, sc / now);
+            }
+        } else {
+            const int w0 = grown ? 0 : s0 / 4, w1 = (s1 + 3) / 4;
+            for (int x = tid; x < D * (w1 - w0); x += kThreads) {
+                const int row = x / (w1 - w0), w = w0 + x % (w1 - w0);
+                uint32_t* at = reinterpret_cast<uint32_t*>(base(page) + row * kPage) + w;
+                const uint32_t held = *at;
+                uint32_t r = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int s = 4 * w + e;
+                    r |= moved(s, (held >> (8 * e)) & 0xffu, tok[s * kRow + row]) << (8 * e);
+                }
+                *at = r;
+            }
+        }
+        if (grown && tid == 0) *scale = now;
+        __syncthreads();   // LDS is read
+    }
+}
+
+// ---------------------------------------------------------------- sequences
+// Sequence n of the result continues sequence src[n]: it shares that one's full pages; the page
+// that is not full goes to the first that continues it and is copied for the others, so that no
+// page that a sequence appends to is shared.  refs counts the table entries that hold a page: a
+// page is free at 0.  Integers throughout; every choice is by order of sequences, entries and page
+// numbers, so that equal calls give equal tables.
+constexpr int32_t kAsked = -2;   // an entry that waits for a page
+
+struct Want {
+    int32_t s, len, full, held, room;   // pages: full ones, those that hold tokens, those wanted
+};
+__device__ __forceinline__ Want want_of(const ForkArgs& a, int n) {
+    Want w{};
+    w.s = ldc(a.src, n);
+    if (uint32_t(w.s) >= uint32_t(a.c.B)) {
+        w.s = -1;
+    } else {
+        w.len = int32_t(min(int64_t(max(ldc(a.c.lens, w.s), 0)), int64_t(a.c.width) * kPage));
+    }
+    const int32_t tokens = max(a.room ? ldc(a.room, n) : 0, w.len);
+    w.full = w.len / kPage;
+    w.held = (w.len + kPage - 1) / kPage;
+    w.room = int32_t(min((int64_t(tokens) + kPage - 1) / kPage, int64_t(a.c.width)));
+    return w;
+}
+__device__ __forceinline__ int block_sum(int x, int* red) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    int r = 0;
+    for (int w = 0; w < int(blockDim.x) / 64; ++w) r += red[w];
+    return r;
+}
+// sum over the threads before this one; `all`: over all
+__device__ __forceinline__ int block_before(int x, int* red, int& all) {
+    int inc = x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(inc, o);
+        if (lane >= o) inc += y;
+    }
+    __syncthreads();
+    if (lane == 63) red[wave] = inc;
+    __syncthreads();
+    int before = 0;
+    all = 0;
+    for (int w = 0; w < int(blockDim.x) / 64; ++w) {
+        if (w < wave) before += red[w];
+        all += red[w];
+    }
+    return before + inc - x;
+}
+
+__global__ void __launch_bounds__(kThreads) fork_refs_kernel(ForkArgs a) {
+    const int p = blockIdx.x * kThreads + threadIdx.x;
+    if (p < a.c.pages) a.refs_out[p] = a.refs[p];
+}
+
+// Workgroups 0 .. B - 1: an old sequence's pages, counted down or up.  The others: a new row, its
+// shared pages and how many it asks for.
+__global__ void __launch_bounds__(kThreads) fork_rows_kernel(ForkArgs a) {
+    __shared__ int red[kThreads / 64];
+    const int tid = threadIdx.x;
+    if (int(blockIdx.x) < a.c.B) {
+        const int s = blockIdx.x;
+        int first = INT32_MAX, takers = 0;
+        for (int n = tid; n < a.N; n += kThreads)
+            if (a.src[n] == s) {
+                first = min(first, n);
+                ++takers;
+            }
+        takers = block_sum(takers, red);
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) first = min(first, __shfl_xor(first, o));
+        __syncthreads();
+        if ((tid & 63) == 0) red[tid >> 6] = first;
+        __syncthreads();
+        first = min(min(red[0], red[1]), min(red[2], red[3]));
+        const Want w = takers ? want_of(a, first) : Want{};
+        for (int i = tid; i < a.c.width; i += kThreads) {
+            const int p = cache_page(a.c, s, i);
+            if (p < 0) continue;
+            const int change = !takers ? -1 : i < w.full ? takers - 1 : i < w.room ? 0 : -1;
+            if (change) atomicAdd(a.refs_out + p, change);
+        }
+        return;
+    }
+    const int n = blockIdx.x - a.c.B;
+    const Want w = want_of(a, n);
+    int before = 0;
+    if (w.s >= 0)
+        for (int i = tid; i < n; i += kThreads) before += a.src[i] == w.s;
+    const bool leads = w.s >= 0 && block_sum(before, red) == 0;
+    int asked = 0;
+    for (int i = tid; i < a.c.width; i += kThreads) {
+        int32_t e = -1;
+        if (i < w.room) {
+            const int p = w.s >= 0 ? cache_page(a.c, w.s, i) : -1;
+            if (p >= 0 && (leads || i < w.full)) e = p;
+            else if (p >= 0 || i >= w.held) e = kAsked;   // (tokens without a page stay without one)
+        }
+        asked += e == kAsked;
+        a.table_out[int64_t(n) * a.c.width + i] = e;
+    }
+    asked = block_sum(asked, red);
+    if (tid == 0) a.need[n] = asked;
+}
+
+// One workgroup: what the rows before each ask for, and as many free pages as all do.
+constexpr int kListThreads = 1024;
+__global__ void __launch_bounds__(kListThreads) fork_list_kernel(ForkArgs a) {
+    __shared__ int red[kListThreads / 64];
+    const int tid = threadIdx.x;
+    int64_t total = 0;
+    for (int n0 = 0; n0 < a.N; n0 += kListThreads) {
+        const int n = n0 + tid, x = n < a.N ? a.need[n] : 0;
+        int all;
+        const int before = block_before(x, red, all);
+        if (n < a.N) a.need[n] = int32_t(min(total + before, int64_t(INT32_MAX)));
+        total += all;
+    }
+    const int most = int(min(total, int64_t(a.cap)));
+    int found = 0;
+    constexpr int E = 8;
+    for (int p0 = 0; p0 < a.c.pages && found < most; p0 += E * kListThreads) {
+        int free[E], mine = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + E * tid + e;
+            free[e] = p < a.c.pages && a.refs_out[p] == 0;
+            mine += free[e];
+        }
+        int all, at = found + block_before(mine, red, all);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (free[e]) {
+                if (at < most) a.list[1 + at] = p0 + E * tid + e;
+                ++at;
+            }
+        found = min(found + all, most);
+    }
+    if (tid == 0) a.list[0] = found;
+}
+
+// A row's pages, and a share of the copy of its last one.
+constexpr int kCopyShares = 4;
+__global__ void __launch_bounds__(kThreads) fork_fill_kernel(ForkArgs a) {
+    __shared__ int red[kThreads / 64];
+    const int n = blockIdx.x / kCopyShares, share = blockIdx.x % kCopyShares, tid = threadIdx.x;
+    const Want w = want_of(a, n);
+    const int found = a.list[0], first = a.need[n];
+    int32_t* row = a.table_out + int64_t(n) * a.c.width;
+    // The page that is not full is asked for first, by all but the one that keeps it.  Every share
+    // goes by the sources' table, as share 0 rewrites the row.
+    int copy = -1, of = -1;
+    if (w.s >= 0 && w.held > w.full) {
+        of = cache_page(a.c, w.s, w.full);
+        int before = 0;
+        for (int i = tid; i < n; i += kThreads) before += a.src[i] == w.s;
+        const bool leads = block_sum(before, red) == 0;
+        if (of >= 0 && !leads) copy = first < found ? a.list[1 + first] : -2;
+    }
+    if (copy >= 0) {
+        const int64_t bytes = int64_t(a.c.Hkv) * kPage * a.c.d, part = bytes / 16;
+        const u32x4* k0 = reinterpret_cast<const u32x4*>(a.c.k + of * bytes);
+        const u32x4* v0 = reinterpret_cast<const u32x4*>(a.c.v + of * bytes);
+        u32x4* k1 = reinterpret_cast<u32x4*>(a.c.k + copy * bytes);
+        u32x4* v1 = reinterpret_cast<u32x4*>(a.c.v + copy * bytes);
+        for (int64_t x = share * kThreads + tid; x < part; x += kCopyShares * kThreads) {
+            k1[x] = k0[x];
+            v1[x] = v0[x];
+        }
+        for (int h = share * kThreads + tid; h < a.c.Hkv; h += kCopyShares * kThreads) {
+            a.c.ks[int64_t(copy) * a.c.Hkv + h] = a.c.ks[int64_t(of) * a.c.Hkv + h];
+            a.c.vs[int64_t(copy) * a.c.Hkv + h] = a.c.vs[int64_t(of) * a.c.Hkv + h];
+        }
+    }
+    if (share != 0) return;
+    int rank = first, asked = 0;
+    for (int i0 = 0; i0 < a.c.width; i0 += kThreads) {
+        const int i = i0 + tid;
+        const bool ask = i < a.c.width && row[i] == kAsked;
+        int all;
+        const int at = rank + block_before(ask, red, all);
+        if (ask) {
+            const int p = at < found ? a.list[1 + at] : -1;
+            row[i] = p;
+            if (p >= 0) a.refs_out[p] = 1;
+        }
+        rank += all;
+        asked += all;
+    }
+    if (tid == 0) {
+        a.missing[n] = asked - min(max(found - first, 0), asked);
+        a.lens_out[n] = copy == -2 ? w.full * kPage : w.len;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_cache_keep(const KeepArgs& a, hipStream_t s) {
+    TraceScope _t("cache_keep", s);
+    const dim3 g(unsigned(int64_t(a.c.B) * a.c.Hkv * 2)), t(kThreads);
+    if (a.c.d == 128) hipLaunchKernelGGL(cache_keep_kernel<128>, g, t, 0, s, a);
+    else hipLaunchKernelGGL(cache_keep_kernel<64>, g, t, 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s) {
+    TraceScope _t("cache_fork", s);
+    const dim3 t(kThreads);
+    if (a.refs != a.refs_out)
+        hipLaunchKernelGGL(fork_refs_kernel, dim3(unsigned((int64_t(a.c.pages) + kThreads - 1) / kThreads)), t, 0, s, a);
+    hipLaunchKernelGGL(fork_rows_kernel, dim3(unsigned(int64_t(a.c.B) + a.N)), t, 0, s, a);
+    hipLaunchKernelGGL(fork_list_kernel, dim3(1), dim3(kListThreads), 0, s, a);
+    hipLaunchKernelGGL(fork_fill_kernel, dim3(unsigned(int64_t(a.N) * kCopyShares)), t, 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace msparse

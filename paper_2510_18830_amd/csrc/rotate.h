@@ -1,0 +1,28 @@
+// Rotation of queries and keys by positions on several axes.
+#pragma once
+
+#include <algorithm>
+
+#include "rotary.h"
+
+namespace msparse {
+
+constexpr int kRotateTokens = 64;   // of a workgroup
+struct RotateArgs {
+    Positions pos;
+    const void *q, *k;                      // [B, heads, T, d], bf16 or fp32
+    void *qout, *kout;
+    int64_t qs[3], ks[3], qos[3], kos[3];   // strides: sequence, head, token
+    int32_t B, T, Hq, Hkv, d;               // Hkv = 0: no keys
+    bool inverse, f32;
+    int32_t blocks, shares;                 // of the tokens, of the heads
+};
+// Workgroups that share a block of tokens, the heads dealt out: enough of them to fill the
+// card, as few as that takes since each forms the angles for itself.
+inline void share_heads(RotateArgs& a) {
+    const int64_t heads = a.Hq + a.Hkv, groups = int64_t(a.B) * a.blocks;
+    a.shares = int32_t(std::min(heads, std::max<int64_t>(1, 1536 / groups)));
+}
+hipError_t launch_rotate(const RotateArgs& a, hipStream_t s);
+
+}  // namespace msparse

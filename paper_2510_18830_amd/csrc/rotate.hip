@@ -1,0 +1,136 @@
+// Rotation of queries and keys by positions on several axes, and its transpose for
+// their gradients.
+//
+// Columns (i, i + d/2) turn by the angle p[axis[i]] freq[i] of their token: x1' = x1 cos -
+// x2 sin, x2' = x2 cos + x1 sin.  The map is orthogonal, so the gradient of its input is
+// the gradient of its output turned back (the sine negated).  Angles are formed in 64 bits
+// for positions of any size and rounded to 32 once, products and sums are in 32 bits, and
+// the result is rounded once.
+//
+// Bound by memory.  A workgroup takes up to 64 tokens and a share of the heads of q and k,
+// forms the tokens' angles once for all of them in LDS, and passes the heads' rows by the
+// caches: they are read and written once.
+#include "rotate.h"
+#include "trace.h"
+
+namespace msparse {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+template <class T>
+struct Row8;   // eight columns of a row in memory
+template <>
+struct Row8<uint16_t> {
+    u32x4 w;
+    __device__ __forceinline__ void load(const uint16_t* p) {
+        w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    }
+    __device__ __forceinline__ void get(float* x) const { unpack8(w, x); }
+    __device__ __forceinline__ void put(const float* x) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+    }
+    __device__ __forceinline__ void store(uint16_t* p) const {
+        __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
+    }
+};
+template <>
+struct Row8<float> {
+    f32x4 lo, hi;
+    __device__ __forceinline__ void load(const float* p) {
+        lo = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+        hi = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + 4));
+    }
+    __device__ __forceinline__ void get(float* x) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[j] = lo[j];
+            x[4 + j] = hi[j];
+        }
+    }
+    __device__ __forceinline__ void put(const float* x) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            lo[j] = x[j];
+            hi[j] = x[4 + j];
+        }
+    }
+    __device__ __forceinline__ void store(float* p) const {
+        __builtin_nontemporal_store(lo, reinterpret_cast<f32x4*>(p));
+        __builtin_nontemporal_store(hi, reinterpret_cast<f32x4*>(p + 4));
+    }
+};
+
+template <int D, class T>
+__global__ void __launch_bounds__(kThreads) rotate_kernel(RotateArgs a) {
+    constexpr int H2 = D / 2, C = D / 16;   // chunks of eight pairs of a row
+    __shared__ __attribute__((aligned(16))) float cosv[kRotateTokens * H2], sinv[kRotateTokens * H2];
+    const int share = blockIdx.x % a.shares;
+    const int blk = blockIdx.x / a.shares % a.blocks, b = blockIdx.x / a.shares / a.blocks;
+    const int t0 = blk * kRotateTokens, m = min(a.T - t0, kRotateTokens);
+    for (int x = threadIdx.x; x < m * H2; x += kThreads) {
+        const Turn z = turn_at(a.pos, x % H2, int64_t(b) * a.T + t0 + x / H2);
+        cosv[x] = float(z.c);
+        sinv[x] = a.inverse ? -float(z.s) : float(z.s);
+    }
+    __syncthreads();
+    // the share's heads, every shares-th of q's and then k's; items are (head, token, chunk)
+    const int heads = (a.Hq + a.Hkv - share + a.shares - 1) / a.shares, each = m * C;
+    const T* q = static_cast<const T*>(a.q);
+    const T* k = static_cast<const T*>(a.k);
+    T* qo = static_cast<T*>(a.qout);
+    T* ko = static_cast<T*>(a.kout);
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;   // items in flight
+    for (int x0 = threadIdx.x; x0 < heads * each; x0 += U * kThreads) {
+        Row8<T> r1[U], r2[U];
+        T* to[U];
+        int at[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int x = x0 + u * kThreads;
+            to[u] = nullptr;
+            if (x >= heads * each) continue;
+            const int h = share + x / each * a.shares, y = x % each, t = y / C, c = y % C;
+            const bool isq = h < a.Hq;
+            const T* from = isq ? q + b * a.qs[0] + h * a.qs[1] + (t0 + t) * a.qs[2]
+                                : k + b * a.ks[0] + (h - a.Hq) * a.ks[1] + (t0 + t) * a.ks[2];
+            to[u] = (isq ? qo + b * a.qos[0] + h * a.qos[1] + (t0 + t) * a.qos[2]
+                         : ko + b * a.kos[0] + (h - a.Hq) * a.kos[1] + (t0 + t) * a.kos[2]) + 8 * c;
+            at[u] = t * H2 + 8 * c;
+            r1[u].load(from + 8 * c);
+            r2[u].load(from + 8 * c + H2);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!to[u]) continue;
+            float x1[8], x2[8];
+            r1[u].get(x1);
+            r2[u].get(x2);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) rotate(x1[j], x2[j], cosv[at[u] + j], sinv[at[u] + j]);
+            r1[u].put(x1);
+            r2[u].put(x2);
+            r1[u].store(to[u]);
+            r2[u].store(to[u] + H2);
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_rotate(const RotateArgs& a, hipStream_t s) {
+    TraceScope _t("rotate", s);
+    const dim3 g(unsigned(int64_t(a.B) * a.blocks * a.shares)), t(kThreads);
+    if (a.f32) {
+        if (a.d == 128) hipLaunchKernelGGL((rotate_kernel<128, float>), g, t, 0, s, a);
+        else hipLaunchKernelGGL((rotate_kernel<64, float>), g, t, 0, s, a);
+    } else {
+        if (a.d == 128) hipLaunchKernelGGL((rotate_kernel<128, uint16_t>), g, t, 0, s, a);
+        else hipLaunchKernelGGL((rotate_kernel<64, uint16_t>), g, t, 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace msparse
