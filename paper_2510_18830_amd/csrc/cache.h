@@ -104,9 +104,12 @@ struct CacheAttnPlan {
     int32_t rows;           // rows of a workgroup
     int32_t tiles, items, chunk, per_tile, unit, slots;
     bool wide;              // a workgroup of many waves per tile
+    bool even;              // a tree's many rows: pages dealt to `items` workgroups per KV head, across tiles
 };
 // workgroups per KV head
-inline int64_t cache_attn_groups(const CacheAttnPlan& p, int64_t B) { return p.slots > 0 ? p.slots : B * p.tiles; }
+inline int64_t cache_attn_groups(const CacheAttnPlan& p, int64_t B) {
+    return p.even ? p.items : p.slots > 0 ? p.slots : B * p.tiles;
+}
 CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int64_t width, int d, int64_t W,
                               int64_t S, bool tree = false);
 constexpr int kMaxNodes = 1024;    // of a tree
@@ -119,6 +122,7 @@ struct TreeMaskArgs {
     int32_t B, T, words, W, S;
 };
 hipError_t launch_tree_mask(const TreeMaskArgs& a, hipStream_t s);
+
 
 struct KeepArgs {
     CacheView c;
@@ -147,6 +151,8 @@ struct ForkArgs {
 };
 hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s);
 
+// a tree's rows in tiles of 128, a workgroup of 256 threads for each place of the grid
+void launch_tree_rows(const CacheAttnArgs& a, dim3 grid, hipStream_t s);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 
 }  // namespace msparse

@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(64 * WAVES)
 // 127 tokens of 32 over 8 heads at 4551 270 us, so 194; 4 x 200 in a window 67, 62; 1 x
 // 4096 at 8192 526, 499; 3 x 500 of 64 heads at 8192 534, 568; 1 x 16384 at 20480 3.52
 // ms, 3.63.)
-template <int D, bool TREE>
+template <int D>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3)))
 cache_attn_rows_kernel(CacheAttnArgs a) {
     constexpr int RT = 2, KL = CacheRows<D, RT>::KL, ND = CacheRows<D, RT>::ND, ROWS = 16 * RT * 4;
@@ -144,10 +144,10 @@ cache_attn_rows_kernel(CacheAttnArgs a) {
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Walk k;
-    if (!open_walk<true, TREE>(a, ROWS, lane, k)) return;
+    if (!open_walk<true, false>(a, ROWS, lane, k)) return;
     const int wr0 = k.tr.r0 + 16 * RT * w;
     CacheRows<D, RT> st;
-    open_rows<D, RT, TREE>(a, st, k.b, k.hk, k.tr, wr0, lane);
+    open_rows<D, RT, false>(a, st, k.b, k.hk, k.tr, wr0, lane);
     const bool live = wr0 < a.T * (a.Hq / a.c.Hkv);
     u32x4 kr[KL], vr[NV];   // this wave's codes of a page: the keys of the token tile w, the columns w, w + 4, ..
     auto load = [&](int page) {
@@ -190,7 +190,7 @@ cache_attn_rows_kernel(CacheAttnArgs a) {
             const u32x4 (*cur)[2][64] = buf[i & 1];
             const int t0 = start(i);
             if (live && t0 <= st.wp1 && (t0 + 63 > st.far || t0 < a.S))
-                page_step<D, RT, 1, 2, 2, TREE>(
+                page_step<D, RT, 1, 2, 2, false>(
                     a, st, t0, lane_value(pages.ks, i), lane_value(pages.vs, i), a.W, a.S, lane,
                     [&](int t, int j, int p) { return cur[t * KL + j][p][lane]; },
                     [&](int y, int p) { return cur[4 * KL + y][p][lane]; }, [] {}, [](int) {});
@@ -200,7 +200,7 @@ cache_attn_rows_kernel(CacheAttnArgs a) {
     }
 #pragma unroll
     for (int x = 0; x < RT; ++x) st.l[x] = row_sum(st.l[x]);
-    if (live) close_rows<D, RT, TREE>(a, st, k, wr0, ROWS, lane);
+    if (live) close_rows<D, RT, false>(a, st, k, wr0, ROWS, lane);
 }
 
 // Joins a row's chunks.  D / 4 lanes hold a row; the kThreads / (D / 4) groups of a
@@ -275,7 +275,10 @@ void launch(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
     const dim3 g(static_cast<unsigned>(wgs)), t(kThreads);
     {
         TraceScope _t(TREE ? "cache_tree_attn" : "cache_attn", s);
-        if (p.wr == 4) hipLaunchKernelGGL((cache_attn_rows_kernel<D, TREE>), g, t, 0, s, a);
+        if (p.wr == 4) {
+            if constexpr (TREE) launch_tree_rows(a, g, s);
+            else hipLaunchKernelGGL((cache_attn_rows_kernel<D>), g, t, 0, s, a);
+        }
         else if (p.wide) launch_wide<D, TREE>(a, g, s);
         else if (p.rt == 2) hipLaunchKernelGGL((cache_attn_kernel<D, 2, 4, TREE>), g, t, 0, s, a);
         else hipLaunchKernelGGL((cache_attn_kernel<D, 1, 4, TREE>), g, t, 0, s, a);
@@ -330,9 +333,10 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
         // rounds of them (512, 768, 1024, 1536, 2048: 255, 236, 224, 211, 211 us for 8
         // contexts of up to 128K x 8 heads), each tile one more than its share at most.
         const int64_t aim = (p.wr == 4 ? kRowsResident(d) : p.rt == 1 ? 1536 : 768) / Hkv;
-        p.items = int32_t(std::max(p.wr == 4 ? aim : aim - e, e));
+        p.even = tree && p.wr == 4;
+        p.items = int32_t(std::max(p.wr == 4 ? aim : aim - e, p.even ? 1 : e));
         const int64_t most = p.wr == 4 ? 2 * int64_t(p.items) : p.items + e;
-        p.slots = int32_t(std::min(most, e * ((width + kMinChunk - 1) / kMinChunk)));
+        p.slots = int32_t(p.even ? p.items + e : std::min(most, e * ((width + kMinChunk - 1) / kMinChunk)));
         while (e * ((width >> p.unit) + 1) > INT32_MAX) ++p.unit;
         return p;
     }
