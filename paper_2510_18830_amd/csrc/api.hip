@@ -1247,7 +1247,7 @@ static size_t carve_cache_fork(const msparse_cache* c, int32_t sequences, char* 
     Carve w{base};
     a->cap = int32_t(std::min(int64_t(sequences) * c->width, int64_t(c->pages)));
     a->need = w.take<int32_t>(size_t(sequences));
-    a->list = w.take<int32_t>(size_t(1) + a->cap);
+    a->list = w.take<int32_t>(std::max(size_t(1) + a->cap, size_t(c->pages)));   // (or a copy of the counts)
     return w.off;
 }
 

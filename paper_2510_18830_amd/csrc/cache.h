@@ -146,8 +146,8 @@ struct ForkArgs {
     int32_t N;
     // workspace
     int32_t* need;          // [N]: pages asked for, then those asked for before
-    int32_t* list;          // [1 + N width at most, or pages]: their number, the free pages
-    int32_t cap;            // of the list
+    int32_t* list;          // the number of free pages found, and they; or a copy of refs
+    int32_t cap;            // pages that the list has room for
 };
 hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s);
 

@@ -276,6 +276,37 @@ __global__ void __launch_bounds__(kListThreads) fork_list_kernel(ForkArgs a) {
     if (tid == 0) a.list[0] = found;
 }
 
+// One page to another: thread t of `threads`.
+__device__ __forceinline__ void copy_page(const CacheView& c, int of, int to, int t, int threads) {
+    const int64_t bytes = int64_t(c.Hkv) * kPage * c.d, part = bytes / 16;
+    const u32x4* k0 = reinterpret_cast<const u32x4*>(c.k + of * bytes);
+    const u32x4* v0 = reinterpret_cast<const u32x4*>(c.v + of * bytes);
+    u32x4* k1 = reinterpret_cast<u32x4*>(c.k + to * bytes);
+    u32x4* v1 = reinterpret_cast<u32x4*>(c.v + to * bytes);
+    int64_t x = t;
+    for (; x + 3 * int64_t(threads) < part; x += 4 * int64_t(threads)) {
+        u32x4 k[4], v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            k[j] = k0[x + j * threads];
+            v[j] = v0[x + j * threads];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            k1[x + j * threads] = k[j];
+            v1[x + j * threads] = v[j];
+        }
+    }
+    for (; x < part; x += threads) {
+        k1[x] = k0[x];
+        v1[x] = v0[x];
+    }
+    for (int h = t; h < c.Hkv; h += threads) {
+        c.ks[int64_t(to) * c.Hkv + h] = c.ks[int64_t(of) * c.Hkv + h];
+        c.vs[int64_t(to) * c.Hkv + h] = c.vs[int64_t(of) * c.Hkv + h];
+    }
+}
+
 // A row's pages, and a share of the copy of its last one.
 constexpr int kCopyShares = 4;
 __global__ void __launch_bounds__(kThreads) fork_fill_kernel(ForkArgs a) {
@@ -294,21 +325,7 @@ __global__ void __launch_bounds__(kThreads) fork_fill_kernel(ForkArgs a) {
         const bool leads = block_sum(before, red) == 0;
         if (of >= 0 && !leads) copy = first < found ? a.list[1 + first] : -2;
     }
-    if (copy >= 0) {
-        const int64_t bytes = int64_t(a.c.Hkv) * kPage * a.c.d, part = bytes / 16;
-        const u32x4* k0 = reinterpret_cast<const u32x4*>(a.c.k + of * bytes);
-        const u32x4* v0 = reinterpret_cast<const u32x4*>(a.c.v + of * bytes);
-        u32x4* k1 = reinterpret_cast<u32x4*>(a.c.k + copy * bytes);
-        u32x4* v1 = reinterpret_cast<u32x4*>(a.c.v + copy * bytes);
-        for (int64_t x = share * kThreads + tid; x < part; x += kCopyShares * kThreads) {
-            k1[x] = k0[x];
-            v1[x] = v0[x];
-        }
-        for (int h = share * kThreads + tid; h < a.c.Hkv; h += kCopyShares * kThreads) {
-            a.c.ks[int64_t(copy) * a.c.Hkv + h] = a.c.ks[int64_t(of) * a.c.Hkv + h];
-            a.c.vs[int64_t(copy) * a.c.Hkv + h] = a.c.vs[int64_t(of) * a.c.Hkv + h];
-        }
-    }
+    if (copy >= 0) copy_page(a.c, of, copy, share * kThreads + tid, kCopyShares * kThreads);
     if (share != 0) return;
     int rank = first, asked = 0;
     for (int i0 = 0; i0 < a.c.width; i0 += kThreads) {
@@ -330,6 +347,132 @@ __global__ void __launch_bounds__(kThreads) fork_fill_kernel(ForkArgs a) {
     }
 }
 
+// All of it in one launch: every workgroup makes up the same counts in LDS from refs, sources and
+// table, finds its own row's pages there by their order, and writes its row, its share of the new
+// counts and its copy.  What rows ask for follows from their lengths alone but for a first taker's
+// pages behind its tokens, which are counted on the way.  A call is bound by its chains of reads and
+// by launches: 9.5 us against 14 for 8 to 32 sequences with 16 entries each, 18.8 against 22.6 for
+// 64 with 1024 from 8, 22.0 against 22.3 for 256 from 64 with 64 and a pool of 8000 pages.  Beyond
+// that the work that every workgroup repeats costs more: 27 us against 19 for 128 with 128, 68
+// against 39 for 1024 with 64.
+struct SmallFork {   // where each lies, in words; bytes: of all, -1: more than LDS is given
+    int32_t first, takers, full, held, room, gaps, given, bytes;
+};
+constexpr int kSmallThreads = 512, kSmallBytes = 64 * 1024;
+constexpr int64_t kSmallRows = 256, kSmallEntries = 8192;
+__host__ __device__ inline SmallFork small_fork(int64_t pages, int64_t B, int64_t width) {
+    SmallFork f{};
+    int64_t at = pages;
+    for (int32_t* x : {&f.first, &f.takers, &f.full, &f.held, &f.room, &f.gaps}) {
+        *x = int32_t(at < kSmallBytes ? at : 0);
+        at += B;
+    }
+    f.given = int32_t(at < kSmallBytes ? at : 0);
+    at += width;
+    f.bytes = at * 4 <= kSmallBytes - 256 ? int32_t(at * 4) : -1;
+    return f;
+}
+
+__global__ void __launch_bounds__(kSmallThreads) fork_small_kernel(ForkArgs a, SmallFork f) {
+    extern __shared__ int32_t lds[];
+    __shared__ int red[kSmallThreads / 64];
+    int32_t *count = lds, *first = lds + f.first, *takers = lds + f.takers, *full = lds + f.full, *held = lds + f.held,
+            *room = lds + f.room, *gaps = lds + f.gaps, *given = lds + f.given;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x;
+    for (int p = tid; p < a.c.pages; p += kSmallThreads) count[p] = a.refs[p];
+    for (int s = tid; s < a.c.B; s += kSmallThreads) {
+        first[s] = INT32_MAX;
+        takers[s] = gaps[s] = 0;
+    }
+    __syncthreads();
+    for (int m = tid; m < a.N; m += kSmallThreads) {
+        const int s = a.src[m];
+        if (uint32_t(s) < uint32_t(a.c.B)) {
+            atomicMin(first + s, m);
+            atomicAdd(takers + s, 1);
+        }
+    }
+    __syncthreads();
+    for (int s = tid; s < a.c.B; s += kSmallThreads) {   // what the first taker keeps
+        const Want w = takers[s] ? want_of(a, first[s]) : Want{};
+        full[s] = w.full;
+        held[s] = w.held;
+        room[s] = w.room;
+    }
+    __syncthreads();
+    for (int s = wave; s < a.c.B; s += kSmallThreads / 64) {
+        const int t = takers[s], fu = full[s], he = held[s], ro = room[s];
+        for (int i = lane; i < a.c.width; i += 64) {
+            const int p = cache_page(a.c, s, i);
+            const int change = !t ? -1 : i < fu ? t - 1 : i < ro ? 0 : -1;
+            if (p >= 0 && change) atomicAdd(count + p, change);
+            if (p < 0 && i >= he && i < ro) atomicAdd(gaps + s, 1);
+        }
+    }
+    __syncthreads();
+    // what the rows ask for: this one, those before it, all
+    auto asks = [&](int m) {
+        const Want w = want_of(a, m);
+        if (w.s >= 0 && first[w.s] == m) return gaps[w.s];
+        const bool copy = w.s >= 0 && w.held > w.full && cache_page(a.c, w.s, w.full) >= 0;
+        return w.room - w.held + copy;
+    };
+    int before = 0, all = 0;
+    for (int m = tid; m < a.N; m += kSmallThreads) {
+        const int x = asks(m);
+        all += x;
+        if (m < n) before += x;
+    }
+    before = block_sum(before, red);
+    all = block_sum(all, red);
+    const int asked = asks(n);
+    // the free pages in order: this row's, and a share of the new counts
+    const int64_t c0 = int64_t(a.c.pages) * n / a.N, c1 = int64_t(a.c.pages) * (n + 1) / a.N;
+    int found = 0;
+    constexpr int E = 8;
+    for (int p0 = 0; p0 < a.c.pages; p0 += E * kSmallThreads) {
+        int c[E], mine = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + E * tid + e;
+            c[e] = p < a.c.pages ? count[p] : 1;
+            mine += c[e] == 0;
+        }
+        int here, at = found + block_before(mine, red, here);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + E * tid + e;
+            if (p >= c0 && p < c1) a.refs_out[p] = c[e] == 0 && at < all ? 1 : c[e];
+            if (c[e] == 0) {
+                if (at >= before && at < before + asked) given[at - before] = p;
+                ++at;
+            }
+        }
+        found += here;
+    }
+    __syncthreads();
+    const int got = min(max(found - before, 0), asked);
+    const Want w = want_of(a, n);
+    const bool leads = w.s >= 0 && first[w.s] == n;
+    int rank = 0;
+    for (int i0 = 0; i0 < a.c.width; i0 += kSmallThreads) {
+        const int i = i0 + tid;
+        const int p = i < w.room && w.s >= 0 ? cache_page(a.c, w.s, i) : -1;
+        const bool keeps = p >= 0 && (leads || i < w.full);
+        const bool ask = i < w.room && !keeps && (p >= 0 || i >= w.held);
+        int here;
+        const int at = rank + block_before(ask, red, here);
+        if (i < a.c.width) a.table_out[int64_t(n) * a.c.width + i] = keeps ? p : ask && at < got ? given[at] : -1;
+        rank += here;
+    }
+    const int of = w.s >= 0 && !leads && w.held > w.full ? cache_page(a.c, w.s, w.full) : -1;
+    if (of >= 0 && got > 0) copy_page(a.c, of, given[0], tid, kSmallThreads);   // (what such a row asks for first)
+    if (tid == 0) {
+        a.missing[n] = asked - got;
+        a.lens_out[n] = of >= 0 && got == 0 ? w.full * kPage : w.len;
+    }
+}
+
 }  // namespace
 
 hipError_t launch_cache_keep(const KeepArgs& a, hipStream_t s) {
@@ -342,9 +485,20 @@ hipError_t launch_cache_keep(const KeepArgs& a, hipStream_t s) {
 
 hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s) {
     TraceScope _t("cache_fork", s);
-    const dim3 t(kThreads);
-    if (a.refs != a.refs_out)
-        hipLaunchKernelGGL(fork_refs_kernel, dim3(unsigned((int64_t(a.c.pages) + kThreads - 1) / kThreads)), t, 0, s, a);
+    const dim3 t(kThreads), by_pages(unsigned((int64_t(a.c.pages) + kThreads - 1) / kThreads));
+    const SmallFork f = small_fork(a.c.pages, a.c.B, a.c.width);
+    if (f.bytes > 0 && a.N <= kSmallRows && int64_t(a.c.B) * a.c.width <= kSmallEntries) {
+        ForkArgs b = a;
+        if (a.refs == a.refs_out) {   // (the counts are read by all while they are written)
+            b.refs_out = a.list;
+            hipLaunchKernelGGL(fork_refs_kernel, by_pages, t, 0, s, b);
+            b.refs = a.list;
+            b.refs_out = a.refs_out;
+        }
+        hipLaunchKernelGGL(fork_small_kernel, dim3(unsigned(a.N)), dim3(kSmallThreads), f.bytes, s, b, f);
+        return hipGetLastError();
+    }
+    if (a.refs != a.refs_out) hipLaunchKernelGGL(fork_refs_kernel, by_pages, t, 0, s, a);
     hipLaunchKernelGGL(fork_rows_kernel, dim3(unsigned(int64_t(a.c.B) + a.N)), t, 0, s, a);
     hipLaunchKernelGGL(fork_list_kernel, dim3(1), dim3(kListThreads), 0, s, a);
     hipLaunchKernelGGL(fork_fill_kernel, dim3(unsigned(int64_t(a.N) * kCopyShares)), t, 0, s, a);

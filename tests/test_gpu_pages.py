@@ -197,6 +197,21 @@ def test_fork_matches_oracle(gpu, B, N, width, pages, Hkv, d, top, spare, in_pla
     _fork(gpu, cache, table, lens, refs, src, room, in_place)
 
 
+@pytest.mark.parametrize("B,N,width,pages,top,spare", [
+    (3, 5, 40, 25000, 2500, 2), (30, 40, 1300, 9000, 14000, 4), (2, 1100, 4, 3000, 250, 1), (200, 300, 12, 21000, 700, 1),
+    (1, 1024, 2, 2100, 128, 1), (40, 33, 800, 12000, 15000, 9), (8, 256, 1024, 14000, 15000, 9), (1000, 256, 8, 9000, 450, 1),
+])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_fork_of_large_pools_and_tables(gpu, B, N, width, pages, top, spare, in_place):
+    """Either side of what one workgroup's memory holds."""
+    print(f"fork B{B} N{N} width{width} pages{pages}", flush=True)
+    table, lens, refs, src, rng = _some(B * N, B, N, width, pages, top, spare)
+    cache = _pool(B, pages, 1, 64, gpu)
+    room = [int(x) for x in rng.integers(-3, 64 * width + 50, N)]
+    for want in (None, room):
+        _fork(gpu, cache, table, lens, refs, src, want, in_place)
+
+
 def test_fork_runs_out_of_pages(gpu):
     """Fewer free pages than are asked for: the first rows get theirs, the others' entries stay -1, a row whose last page
     could not be copied ends with its full pages."""
