@@ -351,15 +351,15 @@ __global__ void __launch_bounds__(kThreads) fork_fill_kernel(ForkArgs a) {
 // table, finds its own row's pages there by their order, and writes its row, its share of the new
 // counts and its copy.  What rows ask for follows from their lengths alone but for a first taker's
 // pages behind its tokens, which are counted on the way.  A call is bound by its chains of reads and
-// by launches: 9.5 us against 14 for 8 to 32 sequences with 16 entries each, 18.8 against 22.6 for
-// 64 with 1024 from 8, 22.0 against 22.3 for 256 from 64 with 64 and a pool of 8000 pages.  Beyond
-// that the work that every workgroup repeats costs more: 27 us against 19 for 128 with 128, 68
-// against 39 for 1024 with 64.
+// by launches: 9.9 us against 14 for 8 sequences with 16 entries each, 15.8 against 20.2 for 256
+// from 64 with 24 and 4000 pages, 19.9 against 22.6 for 64 from 8 with 1024 and 10000 pages.
+// Beyond that the work that every workgroup repeats costs more: 29 us against 19 for 128 with 128
+// and 19000 pages, 62 against 39 for 1024 from 64.  (1024 threads: 11.3, 16.4 and 18.0 us.)
 struct SmallFork {   // where each lies, in words; bytes: of all, -1: more than LDS is given
     int32_t first, takers, full, held, room, gaps, given, bytes;
 };
-constexpr int kSmallThreads = 512, kSmallBytes = 64 * 1024;
-constexpr int64_t kSmallRows = 256, kSmallEntries = 8192;
+constexpr int kSmallThreads = 512, kSmallBytes = 80 * 1024;   // two workgroups a CU
+constexpr int64_t kSmallRows = 256, kSmallReads = 20000;   // rows; words that each workgroup reads
 __host__ __device__ inline SmallFork small_fork(int64_t pages, int64_t B, int64_t width) {
     SmallFork f{};
     int64_t at = pages;
@@ -378,8 +378,21 @@ __global__ void __launch_bounds__(kSmallThreads) fork_small_kernel(ForkArgs a, S
     __shared__ int red[kSmallThreads / 64];
     int32_t *count = lds, *first = lds + f.first, *takers = lds + f.takers, *full = lds + f.full, *held = lds + f.held,
             *room = lds + f.room, *gaps = lds + f.gaps, *given = lds + f.given;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x;
-    for (int p = tid; p < a.c.pages; p += kSmallThreads) count[p] = a.refs[p];
+    const int tid = threadIdx.x, n = blockIdx.x;
+    constexpr int E = 8;   // loads in flight
+    for (int p0 = tid; p0 < a.c.pages; p0 += E * kSmallThreads) {
+        int c[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + e * kSmallThreads;
+            c[e] = p < a.c.pages ? a.refs[p] : 0;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + e * kSmallThreads;
+            if (p < a.c.pages) count[p] = c[e];
+        }
+    }
     for (int s = tid; s < a.c.B; s += kSmallThreads) {
         first[s] = INT32_MAX;
         takers[s] = gaps[s] = 0;
@@ -400,13 +413,23 @@ __global__ void __launch_bounds__(kSmallThreads) fork_small_kernel(ForkArgs a, S
         room[s] = w.room;
     }
     __syncthreads();
-    for (int s = wave; s < a.c.B; s += kSmallThreads / 64) {
-        const int t = takers[s], fu = full[s], he = held[s], ro = room[s];
-        for (int i = lane; i < a.c.width; i += 64) {
-            const int p = cache_page(a.c, s, i);
-            const int change = !t ? -1 : i < fu ? t - 1 : i < ro ? 0 : -1;
-            if (p >= 0 && change) atomicAdd(count + p, change);
-            if (p < 0 && i >= he && i < ro) atomicAdd(gaps + s, 1);
+    const int entries = a.c.B * a.c.width;
+    for (int x0 = tid; x0 < entries; x0 += E * kSmallThreads) {
+        int p[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int x = x0 + e * kSmallThreads;
+            p[e] = x < entries ? a.c.table[x] : -1;
+            p[e] = uint32_t(p[e]) < uint32_t(a.c.pages) ? p[e] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int x = x0 + e * kSmallThreads;
+            if (x >= entries) break;
+            const int s = x / a.c.width, i = x - s * a.c.width, t = takers[s];
+            const int change = !t ? -1 : i < full[s] ? t - 1 : i < room[s] ? 0 : -1;
+            if (p[e] >= 0 && change) atomicAdd(count + p[e], change);
+            if (p[e] < 0 && i >= held[s] && i < room[s]) atomicAdd(gaps + s, 1);
         }
     }
     __syncthreads();
@@ -429,7 +452,6 @@ __global__ void __launch_bounds__(kSmallThreads) fork_small_kernel(ForkArgs a, S
     // the free pages in order: this row's, and a share of the new counts
     const int64_t c0 = int64_t(a.c.pages) * n / a.N, c1 = int64_t(a.c.pages) * (n + 1) / a.N;
     int found = 0;
-    constexpr int E = 8;
     for (int p0 = 0; p0 < a.c.pages; p0 += E * kSmallThreads) {
         int c[E], mine = 0;
 #pragma unroll
@@ -487,7 +509,7 @@ hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s) {
     TraceScope _t("cache_fork", s);
     const dim3 t(kThreads), by_pages(unsigned((int64_t(a.c.pages) + kThreads - 1) / kThreads));
     const SmallFork f = small_fork(a.c.pages, a.c.B, a.c.width);
-    if (f.bytes > 0 && a.N <= kSmallRows && int64_t(a.c.B) * a.c.width <= kSmallEntries) {
+    if (f.bytes > 0 && a.N <= kSmallRows && int64_t(a.c.B) * a.c.width + a.c.pages <= kSmallReads) {
         ForkArgs b = a;
         if (a.refs == a.refs_out) {   // (the counts are read by all while they are written)
             b.refs_out = a.list;
