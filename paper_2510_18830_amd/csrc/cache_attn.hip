@@ -337,7 +337,7 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
         p.items = int32_t(std::max(p.wr == 4 ? aim : aim - e, p.even ? 1 : e));
         const int64_t most = p.wr == 4 ? 2 * int64_t(p.items) : p.items + e;
         p.slots = int32_t(p.even ? p.items + e : std::min(most, e * ((width + kMinChunk - 1) / kMinChunk)));
-        while (e * ((width >> p.unit) + 1) > INT32_MAX) ++p.unit;
+        while (e * ((width >> p.unit) + 1) > INT32_MAX / (p.even ? 2 : 1)) ++p.unit;   // (even: a run's end past all)
         return p;
     }
     // Many tiles fill the card by themselves; every wave's search for its chunk among

@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kListThreads) fork_list_kernel(ForkArgs a) {
         const int n = n0 + tid, x = n < a.N ? a.need[n] : 0;
         int all;
         const int before = block_before(x, red, all);
-        if (n < a.N) a.need[n] = int32_t(min(total + before, int64_t(INT32_MAX)));
+        if (n < a.N) a.need[n] = int32_t(min(total + before, int64_t(1) << 30));   // (no pool has as many pages)
         total += all;
     }
     const int most = int(min(total, int64_t(a.cap)));

@@ -212,6 +212,21 @@ def test_fork_of_large_pools_and_tables(gpu, B, N, width, pages, top, spare, in_
         _fork(gpu, cache, table, lens, refs, src, want, in_place)
 
 
+def test_fork_asks_for_2e31_pages(gpu):
+    """More places than 32 bits count: the first rows get what there is, the others nothing."""
+    pages, width, N = 50, 32800, 65536
+    cache = _pool(1, pages, 1, 64, gpu)
+    table = torch.full((1, width), -1, dtype=I32, device=gpu)
+    zero = torch.zeros(1, dtype=I32, device=gpu)
+    room = torch.full((N,), 64 * width, dtype=I32, device=gpu)
+    got, lens, refs, missing = ms.cache_fork(cache, table, zero, torch.zeros(pages, dtype=I32, device=gpu),
+                                             torch.full((N,), -1, dtype=I32, device=gpu), room=room)
+    assert got[0, :pages].tolist() == list(range(pages)) and (got[0, pages:] == -1).all()
+    assert all((part == -1).all() for part in got[1:].split(4096))
+    assert (refs == 1).all() and (lens == 0).all()
+    assert missing[0] == width - pages and (missing[1:] == width).all()
+
+
 def test_fork_runs_out_of_pages(gpu):
     """Fewer free pages than are asked for: the first rows get theirs, the others' entries stay -1, a row whose last page
     could not be copied ends with its full pages."""

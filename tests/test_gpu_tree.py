@@ -85,7 +85,7 @@ def _masks(parents, contexts, counts, W, S):
     return np.stack([x[0] for x in both]), np.stack([x[1] for x in both])
 
 
-def _run(gpu, Hq, Hkv, d, T, contexts, counts, W, S, kind="tree", seed=1, qmul=1.0):
+def _run(gpu, Hq, Hkv, d, T, contexts, counts, W, S, kind="tree", seed=1, qmul=1.0, width=0):
     B = len(contexts)
     print(f"tree Hq{Hq} Hkv{Hkv} d{d} T{T} {contexts} {counts} W{W} S{S} {kind}", flush=True)
     parents = _parents(seed, B, T, kind)
@@ -95,10 +95,14 @@ def _run(gpu, Hq, Hkv, d, T, contexts, counts, W, S, kind="tree", seed=1, qmul=1
                               sinks=S)
     assert np.array_equal(gat.cpu().numpy(), at) and np.array_equal(gseen.cpu().numpy(), OT.words(sees))
     cache, table, L = _filled(T + d, contexts, T, Hkv, d, gpu, counts)
+    narrow = table
+    if width:
+        table = torch.full((B, width), -1, dtype=I32, device=gpu)
+        table[:, :narrow.shape[1]] = narrow
     q = _randn(seed, (B, Hq, T, d), gpu, qmul)
     out, lse = ms.cache_tree_attn(cache, table, L, q, gseen, positions=gat if W else None, counts=cnt, window=W, sinks=S)
     torch.cuda.synchronize()
-    _check(q, out, lse, cache, table, L, sees, at, counts, W, S)
+    _check(q, out, lse, cache, narrow, L, sees, at, counts, W, S)
     again = ms.cache_tree_attn(cache, table, L, q, gseen, positions=gat, counts=cnt, window=W, sinks=S)
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
     return out, lse
@@ -150,6 +154,69 @@ def test_tree_attn_many_sequences(gpu, B, Hq, Hkv, d, T):
     contexts = [int(x) for x in rng.integers(0, 300, B)]
     counts = [int(x) for x in rng.integers(0, T + 1, B)]
     _run(gpu, Hq, Hkv, d, T, contexts, counts, 0, 0)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,T,contexts,width", [
+    (4, 1, 64, 4, [1500, 700], 0), (4, 1, 64, 4, [600] * 130, 0), (4, 2, 128, 5, [5000, 90, 2500], 0),
+    (16, 4, 128, 8, [3000, 90, 1500], 0), (8, 1, 64, 4, [4000, 1, 64], 0), (1, 1, 64, 12, [3, 1200], 150),
+])
+@pytest.mark.parametrize("W,S", [(0, 0), (900, 70)])
+def test_few_rows_over_several_chunks(gpu, Hq, Hkv, d, T, contexts, width, W, S):
+    rng = np.random.default_rng(T)
+    _run(gpu, Hq, Hkv, d, T, contexts, [int(x) for x in rng.integers(1, T + 1, len(contexts))], W, S, width=width)
+
+
+@pytest.mark.parametrize("d,Hq,T", [(64, 8, 64), (128, 4, 100)])
+def test_many_tiles_of_rows(gpu, d, Hq, T):
+    """From 512 tiles of 128 rows on, each walks its pages by itself, or, where the table is wide, one of several chunks."""
+    rng = np.random.default_rng(T)
+    contexts = [int(x) for x in rng.integers(0, 100, 128)]
+    counts = [int(x) for x in rng.integers(0, T + 1, 128)]
+    _run(gpu, Hq, 1, d, T, contexts, counts, 0, 0, width=7)
+    contexts[77], contexts[90] = 4190, 4030
+    _run(gpu, Hq, 1, d, T, contexts, counts, 0, 0, width=150)
+
+
+def test_the_widest_table(gpu):
+    """100 tiles in a table of 2^24 pages, which are dealt out by twos."""
+    _run(gpu, 64, 1, 64, 200, [1500], None, 0, 0, width=2 ** 24)
+
+
+def test_all_trees_empty(gpu):
+    """No node anywhere; nodes of the last sequence alone."""
+    for counts in ([0, 0, 0, 0], [0, 0, 0, 40], [40, 0, 0, 0]):
+        _run(gpu, 8, 2, 64, 40, [300, 1000, 0, 700], counts, 0, 0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_missing_pages_positions_and_strides_of_many_rows(gpu, d):
+    Hq, Hkv, T, contexts = 12, 2, 50, [500, 130, 64]
+    cache, table, L = _filled(8, contexts, T, Hkv, d, gpu, None)
+    table[0, 1], table[0, 8], table[2, 1] = 10 ** 6, -1, -5
+    q = _randn(1, (3, T, Hq, d), gpu).transpose(1, 2)
+    at, sees = _masks(_parents(2, 3, T), contexts, None, 0, 0)
+    seen = _dev(OT.words(sees), gpu)
+    out = torch.empty((3, T, Hq, d), dtype=BF, device=gpu).transpose(1, 2)
+    got, lse = ms.cache_tree_attn(cache, table, L, q, seen, scale=0.2, out=out)
+    torch.cuda.synchronize()
+    assert got is out
+    _check(q, out, lse, cache, table, L, sees, at, None, 0, 0, 0.2)
+    for odd in ([0, 50, 51], [-3, 7, 1]):
+        n = torch.tensor(odd, dtype=I32, device=gpu)
+        out, lse = ms.cache_tree_attn(cache, table, n, q, seen)
+        torch.cuda.synchronize()
+        _check(q, out, lse, cache, table, n.clamp(min=0), sees, at, None, 0, 0)
+    far = torch.tensor([2 ** 31 - 1, 64 * table.shape[1] + 60, 2 ** 30], dtype=I32, device=gpu)
+    out, lse = ms.cache_tree_attn(cache, table, far, q, seen, positions=far[:, None].expand(3, T).contiguous(), window=40)
+    torch.cuda.synchronize()
+    assert torch.isneginf(lse).all() and (out == 0).all()
+    rng = np.random.default_rng(d)   # positions in any order, some outside the nodes' places
+    at = np.stack([rng.integers(n - 30, n + T + 30, T) for n in contexts])
+    at[:, :2] = 2 ** 31 - 1, -2 ** 31
+    for W, S in ((1, 0), (50, 3), (70, 200)):
+        out, lse = ms.cache_tree_attn(cache, table, L, q, seen, positions=_dev(at, gpu), window=W, sinks=S)
+        torch.cuda.synchronize()
+        _check(q, out, lse, cache, table, L, sees, at, None, W, S)
 
 
 @pytest.mark.parametrize("d,T", [(64, 1), (128, 5), (64, 40), (128, 70)])
