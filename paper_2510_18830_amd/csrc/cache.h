@@ -152,7 +152,7 @@ struct ForkArgs {
 hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s);
 
 // a tree's rows in tiles of 128, a workgroup of 256 threads for each place of the grid
-void launch_tree_rows(const CacheAttnArgs& a, dim3 grid, hipStream_t s);
+void launch_tree_rows(const CacheAttnArgs& a, int rows, dim3 grid, hipStream_t s);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 
 }  // namespace msparse

@@ -276,7 +276,7 @@ void launch(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
     {
         TraceScope _t(TREE ? "cache_tree_attn" : "cache_attn", s);
         if (p.wr == 4) {
-            if constexpr (TREE) launch_tree_rows(a, g, s);
+            if constexpr (TREE) launch_tree_rows(a, p.rows, g, s);
             else hipLaunchKernelGGL((cache_attn_rows_kernel<D>), g, t, 0, s, a);
         }
         else if (p.wide) launch_wide<D, TREE>(a, g, s);
@@ -306,8 +306,9 @@ CacheAttnPlan cache_attn_plan(int64_t B, int64_t Hq, int64_t Hkv, int64_t T, int
     // 5 to 9 tokens 146-150 -> 112-116; 16 of up to 8K, 32 over 8, head dim 64, 9 to 16
     // tokens 46-49 -> 39-40; 4 of up to 8K, 16 over 2, 5 to 8 tokens 17.5-18.7 -> 17.9-19.4;
     // 64 of up to 2K, 32 over 4, head dim 64, 6 to 8 tokens 24.4 -> 29.6)
+    // Trees take 64 at most in tiles of their own (as above 93-95 us, in tiles of 128 102-104).
     p.wr = rows <= 32 ? 1 : 4;
-    p.rows = 16 * p.rt * p.wr;
+    p.rows = tree && p.wr == 4 && rows <= 64 ? 64 : 16 * p.rt * p.wr;
     p.tiles = int32_t((rows + p.rows - 1) / p.rows);
     // the most pages that a tile sees: the window of its tokens (of a tree's nodes: of any), the sinks' (what a plan
     // needs grows with them, so that one without a window has room for all)

@@ -7,17 +7,24 @@
 // ancestors, which descend, and writes its words from the last to the first as it passes them: no
 // word is held or read back.  Bound by latency: the walk's LDS reads, one after the other.
 //
-// ---- Attention.  The T G rows of a KV head (row r: node r / G, head r % G of the group) are cut
-// into tiles of 128, 32 a wave, that walk the pages they see together:
+// 64 trees of 16 nodes: 3.4 us.
+//
+// ---- Attention.  The T G rows of a KV head (row r: node r / G, head r % G of the group) are cut into tiles of 128, 32
+// a wave, that walk the pages they see together; up to 64 rows, two waves share 32, and each takes half of every page's
+// tokens:
 //   S^T = K Q^T      (32x32x16 bf16: A = 32 tokens, B = the queries)
-//   online softmax   (a lane owns a row and half of the page's tokens)
+//   online softmax   (a lane owns a row and half of the tokens)
 //   O^T += V^T P^T   (A = 32 columns, B = P from the S^T registers)
-// The codes of a page are converted once for the four waves, to bf16 operands in LDS.  (Products of 8 bits,
-// which would take keys as they lie, with the queries split into two e4m3 parts, are exact, but their sums
-// are not: the matrix cores keep 12 bits below the largest of 64 products, which put lse off by 1e-3.)
-// A page's K scale enters the logits' factor, its V scale the conversion.
-#include <type_traits>
-
+// Codes go to LDS as they lie in memory, some pages ahead and past the registers, and every wave converts its operands to
+// bf16 between the products.  A page's K scale enters the logits' factor, its V scale the conversion.  (Products of 8
+// bits, which would take keys as they lie, with the queries split into two e4m3 parts, are exact, but their sums are not:
+// the matrix cores keep 12 bits below the largest of 64 products, which put lse off by 1e-3.)
+//
+// Few rows are bound by the cache's bytes and each step's chain, many by the issue of instructions (a product takes 16 of
+// its 32 cycles of it) and by power, which lowers the clock.  Contexts of up to 16K, 32 of them, 28 over 4 heads, with the
+// join: 8 nodes 93 us, 16 126, 32 206 (0.70 PFLOP/s; a plain matrix product of bf16 reaches 1.37).  Codes converted once for the
+// four waves to bf16 in LDS, twice its bytes: 102, 128 and 213 us; 64 rows a wave, which halves LDS's bytes and the
+// conversions, one wave a SIMD: 132, 142 and 243.
 #include "cache_walk.h"
 #include "tiles.h"
 #include "trace.h"
@@ -71,19 +78,20 @@ constexpr float kSlack = 8.f;   // log2 units that a row's maximum may rise by b
 // A wave's 32 rows; lane (half h, i) owns row i and half h of the contractions.
 template <int D>
 struct TreeRows {
-    u32x4 q[D / 16];     // the query, columns 16 s + 8 h ..
+    u32x4 q[D / 16];     // the query: step 2 c + e takes columns 32 c + 16 h + 8 e ..
     f32x16 o[D / 32];
     float m, l;          // the whole number that the weights are relative to; their sum, of this lane's tokens
     float limit;         // logits beyond it raise m
 };
 constexpr float kNone = -0x1.fffffep127f;   // m of a row without a token yet: finite, so that a masked logit weighs 0
+constexpr int kDepth = 4;   // pages of keys, and of values, in LDS
 
 template <int D>
 __device__ __forceinline__ void open_tree_rows(const CacheAttnArgs& a, TreeRows<D>& st, const Walk& k, int wr0, int lane) {
     const int G = a.Hq / a.c.Hkv, R = a.T * G, r = min(wr0 + (lane & 31), R - 1);
-    const uint16_t* qp = a.q + k.b * a.qs[0] + (k.hk * G + r % G) * a.qs[1] + (r / G) * a.qs[2] + 8 * (lane >> 5);
+    const uint16_t* qp = a.q + k.b * a.qs[0] + (k.hk * G + r % G) * a.qs[1] + (r / G) * a.qs[2] + 16 * (lane >> 5);
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) st.q[s] = *reinterpret_cast<const u32x4*>(qp + 16 * s);
+    for (int s = 0; s < D / 16; ++s) st.q[s] = *reinterpret_cast<const u32x4*>(qp + 32 * (s >> 1) + 8 * (s & 1));
 #pragma unroll
     for (int x = 0; x < D / 32; ++x) st.o[x] = f32x16{};
     st.m = kNone;
@@ -131,17 +139,29 @@ __device__ __forceinline__ uint64_t row_sees(const CacheAttnArgs& a, int r, int 
     return (bits & ~context) | (context & (~below64(max(pos - a.W + 1, 0) - j) | below64(min(a.S - 1, pos) + 1 - j)));
 }
 
-// Where a page lies in LDS, as bf16.  Keys: a token's row of D columns, values: a column's row of 64 tokens, each row
-// 16 bytes apart from the next, which puts the 16 rows that an LDS cycle serves into distinct banks.
+// Where the codes of a page lie in LDS: as in memory, rows of a token's D columns (keys) or a column's 64 tokens (values),
+// but for the order of a row's 16-byte pieces, which puts those that 16 lanes read in one LDS cycle into distinct banks.
+// Which piece of row `row` stands in place c, and where piece c stands: both c ^ this.
 template <int D>
-struct TreePage {
-    static constexpr int kKeyRow = 2 * D + 16, kValueRow = 2 * kPage + 16;
-    static constexpr int kKeys = kPage * kKeyRow, kValues = D * kValueRow;   // bytes
-};
+__device__ __forceinline__ int key_order(int row) {
+    return D == 128 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2);
+}
+__device__ __forceinline__ int value_order(int row) { return (row >> 2) & 3; }
+// Which token a row of the S^T tiles stands for: those of half h's accumulators are 16 tokens in a row from 16 h on,
+// eight for each step of the second product, whose 16-byte pieces of a column they are.
+__device__ __forceinline__ int token_of(int i) { return 4 * (i & 4) + ((i >> 1) & 12) + (i & 3); }
 
-// Which token a row of the S^T tiles stands for: those of a lane's accumulators, eight by eight, are eight
-// tokens in a row, the B operand of the second product.
-__device__ __forceinline__ int token_of(int i) { return (i & 16) + 2 * (i & 4) + ((i & 8) >> 1) + (i & 3); }
+// 16 bytes a lane from `base` + its offset to LDS, lane after lane from `to` on; no wait.
+__device__ __forceinline__ void fetch16(const uint8_t* base, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to))
+                 : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void wait_fetched() {   // all but the last N
+    asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory");
+}
 
 // A page's V scale: the power of two enters the values as they are converted, the mantissa (1, where an
 // append wrote the page) the weights' exponent, as its logarithm, and leaves their sum again.
@@ -153,60 +173,86 @@ __device__ __forceinline__ ValueScale value_scale(float x) {
     return ValueScale{__uint_as_float(__float_as_uint(x) & 0x7f800000u), fast_log2(m), 1.f / m};
 }
 
-// What a wave carries from one half of a page to the next: the logits of 32 tokens, and the weights of the
-// 32 before them, whose product with the values is still to come.
+// What a wave carries from one step of 32 tokens to the next: the weights of the 32 before them, whose product with the
+// values is still to come.
 struct TreeHalf {
     u32x4 p[2];
 };
+// A lane's logits of 32 tokens, and the largest of them.
+struct TreeLogits {
+    f32x16 s;
+    float top;
+};
+__device__ __forceinline__ float largest(const f32x16& s) {
+    float top = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+    return top;
+}
 
-// The 32 tokens in `cur` become weights, while the matrix cores form the logits of the next 32 (keys at kb) and the
-// product of the last ones (values at vb): each MFMA is followed by vector work that it covers.
+// The 32 tokens in `cur` become weights, while the matrix cores form the logits of the next 32 (codes of keys at kb + kat),
+// then the product of the last ones (codes of values at vb, times `power`): each MFMA is followed by vector work that it
+// covers.
 template <int D>
-__device__ __forceinline__ void tree_half(TreeRows<D>& st, const f32x16& cur, f32x16& next, TreeHalf& w, const uint8_t* kb,
-                                          const uint8_t* vb, int vhalf, float fac, ValueScale vs) {
-    constexpr int KS = D / 16, NB = D / 32;
-    u32x4 kop[KS / 2], vop[NB];   // the next operands of either product
-    auto read_k = [&](int s) { kop[s % (KS / 2)] = *reinterpret_cast<const u32x4*>(kb + 32 * s); };
-    auto read_v = [&](int x) {
-        vop[x % NB] = *reinterpret_cast<const u32x4*>(vb + 64 * vhalf + 32 * (x / NB) + 32 * TreePage<D>::kValueRow * (x % NB));
+__device__ __forceinline__ void tree_half(TreeRows<D>& st, TreeLogits& cur, TreeHalf& w, const uint8_t* kb, int kat,
+                                          const uint8_t* vb, float fac, ValueScale vs, float power) {
+    constexpr int KS = D / 16;
+    u32x4 kraw[2], vraw[2], kop[2], vop[2];   // codes of two steps each; operands
+    auto read_k = [&](int c) { kraw[c & 1] = *reinterpret_cast<const u32x4*>(kb + (kat ^ (32 * c))); };
+    auto read_v = [&](int c) { vraw[c & 1] = *reinterpret_cast<const u32x4*>(vb + 32 * kPage * c); };
+    auto convert_k = [&](int x) {
+        const u32x4& r = kraw[(x >> 1) & 1];
+        kop[x & 1] = x & 1 ? codes_to_bf16(r.z, r.w) : codes_to_bf16(r.x, r.y);
     };
-#pragma unroll
-    for (int s = 0; s < KS / 2; ++s) read_k(s);
-#pragma unroll
-    for (int x = 0; x < NB; ++x) read_v(x);
+    auto convert_v = [&](int x) {
+        const u32x4& r = vraw[(x >> 1) & 1];
+        vop[x & 1] = x & 1 ? codes_to_bf16(r.z, r.w, power) : codes_to_bf16(r.x, r.y, power);
+    };
+    read_k(0);
+    read_k(1);
     const float shift = vs.shift - st.m;
     const u32x4 last[2] = {w.p[0], w.p[1]};
     float l[2] = {0.f, 0.f};
-    auto weights = [&](int r0, int n) {   // pairs r0, r0 + 2, .. below r0 + n
-#pragma unroll
-        for (int r = r0; r < r0 + n && r < 16; r += 2) {
-            const float x = fast_exp2(__builtin_fmaf(cur[r], fac, shift));
-            const float y = fast_exp2(__builtin_fmaf(cur[r + 1], fac, shift));
-            uint32_t xy = pack_bf16x2(x, y);
-            l[0] += x;
-            l[1] += y;
-            asm volatile("" : "+v"(xy), "+v"(l[0]), "+v"(l[1]));   // here, beside the products, and not where they are used
-            w.p[r >> 3][(r & 7) >> 1] = xy;
-        }
+    auto weights = [&](int y) {   // of a pair of tokens
+        const float a = fast_exp2(__builtin_fmaf(cur.s[2 * y], fac, shift));
+        const float b = fast_exp2(__builtin_fmaf(cur.s[2 * y + 1], fac, shift));
+        uint32_t ab = pack_bf16x2(a, b);
+        l[0] += a;
+        l[1] += b;
+        asm volatile("" : "+v"(ab), "+v"(l[0]), "+v"(l[1]));   // here, beside the products, and not where they are used
+        w.p[y >> 2][y & 3] = ab;
     };
-    // weights before the first product, and beside each pair of products
-    constexpr int kAhead = 4, kEach = D == 128 ? 2 : 4;
-    static_assert(KS == 2 * NB, "a step for each k-step of the logits and each product with values");
+    // Pairs before the logits' products and beside them; the rest beside the first half of the values'.
+    constexpr int kPairs = 8, kAhead = 1, kLogits = KS * 5 / 8;
+    int y = 0;
+    for (; y < kAhead; ++y) weights(y);
+    convert_k(0);
+    f32x16 next;
     __builtin_amdgcn_sched_barrier(0);
-    weights(0, kAhead);
-    int r = kAhead;
 #pragma unroll
     for (int x = 0; x < KS; ++x) {
-        next = mfma32(kop[x % (KS / 2)], st.q[x], x ? next : f32x16{});
+        next = mfma32(kop[x & 1], st.q[x], x ? next : f32x16{});
         __builtin_amdgcn_sched_barrier(0);
-        st.o[x % NB] = mfma32(vop[x % NB], last[x / NB], st.o[x % NB]);
+        if (x + 1 < KS) convert_k(x + 1);
+        const int goal = kAhead + kLogits * (x + 1) / KS;
+#pragma unroll
+        for (; y < goal; ++y) weights(y);
+        if ((x & 1) == 0 && x / 2 + 2 < KS / 2) read_k(x / 2 + 2);
+        if (x >= KS - 2) read_v(x - (KS - 2));
         __builtin_amdgcn_sched_barrier(0);
-        if (x < KS / 2) {
-            read_k(x + KS / 2);
-            read_v(x + NB);
-        }
-        weights(r, kEach);
-        r += kEach;
+    }
+    convert_v(0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+        st.o[x >> 1] = mfma32(vop[x & 1], last[x & 1], st.o[x >> 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (x + 1 < KS) convert_v(x + 1);
+        const int goal = kAhead + kLogits + (kPairs - kAhead - kLogits) * (x + 1) / (KS / 2);
+#pragma unroll
+        for (; y < goal && y < kPairs; ++y) weights(y);
+        if ((x & 1) == 0 && x / 2 + 2 < KS / 2) read_v(x / 2 + 2);
+        if (x == KS - 1) cur = TreeLogits{next, largest(next)};
         __builtin_amdgcn_sched_barrier(0);
     }
     st.l = __builtin_fmaf(l[0] + l[1], vs.back, st.l);
@@ -214,39 +260,42 @@ __device__ __forceinline__ void tree_half(TreeRows<D>& st, const f32x16& cur, f3
 
 // The logits of the first 32 tokens.
 template <int D>
-__device__ __forceinline__ void tree_first(const TreeRows<D>& st, f32x16& next, const uint8_t* kb) {
-    next = f32x16{};
+__device__ __forceinline__ TreeLogits tree_first(const TreeRows<D>& st, const uint8_t* kb, int kat) {
+    f32x16 s{};
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) next = mfma32(*reinterpret_cast<const u32x4*>(kb + 32 * s), st.q[s], next);
+    for (int c = 0; c < D / 32; ++c) {
+        const u32x4 raw = *reinterpret_cast<const u32x4*>(kb + (kat ^ (32 * c)));
+        s = mfma32(codes_to_bf16(raw.x, raw.y), st.q[2 * c], s);
+        s = mfma32(codes_to_bf16(raw.z, raw.w), st.q[2 * c + 1], s);
+    }
+    return TreeLogits{s, largest(s)};
 }
 
 // The product of the weights that are left with their values.
 template <int D>
-__device__ __forceinline__ void tree_flush(TreeRows<D>& st, TreeHalf& w, const uint8_t* vb, int vhalf) {
+__device__ __forceinline__ void tree_flush(TreeRows<D>& st, const TreeHalf& w, const uint8_t* vb, float power) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int b = 0; b < D / 32; ++b)
-            st.o[b] = mfma32(*reinterpret_cast<const u32x4*>(vb + 64 * vhalf + 32 * g + 32 * TreePage<D>::kValueRow * b), w.p[g], st.o[b]);
-    w.p[0] = w.p[1] = u32x4{};
+    for (int b = 0; b < D / 32; ++b) {
+        const u32x4 raw = *reinterpret_cast<const u32x4*>(vb + 32 * kPage * b);
+        st.o[b] = mfma32(codes_to_bf16(raw.x, raw.y, power), w.p[0], st.o[b]);
+        st.o[b] = mfma32(codes_to_bf16(raw.z, raw.w, power), w.p[1], st.o[b]);
+    }
 }
 
 // The logits of 32 tokens before they become weights: masks, and the running maximum, which moves only where
 // it has to (the weights stay below 2^(kSlack + 1)).  It is a whole number, so that what moves by it moves by a
 // power of two: the weights that wait for their product do exactly.
 template <int D, class Sees>
-__device__ __forceinline__ void tree_top(TreeRows<D>& st, f32x16& s, TreeHalf& w, bool part, Sees mask, float fac) {
+__device__ __forceinline__ void tree_top(TreeRows<D>& st, TreeLogits& cur, TreeHalf& w, bool part, Sees mask, float fac) {
     if (part) {
         const uint32_t sees = mask();
         keep_branch();
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-            if (!((sees >> (16 * (r >> 3) + (r & 7))) & 1)) s[r] = -INFINITY;
+            if (!((sees >> r) & 1)) cur.s[r] = -INFINITY;
+        cur.top = largest(cur.s);
     }
-    float top = s[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
-    top *= fac;
+    float top = cur.top * fac;
     if (__any(top > st.limit)) {
         top = half_swap_max(top);
         const float m = top > st.limit ? __builtin_ceilf(top) : st.m;
@@ -258,8 +307,8 @@ __device__ __forceinline__ void tree_top(TreeRows<D>& st, f32x16& s, TreeHalf& w
         for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int j = 0; j < 4; ++j) w.p[g][j] = pack_bf16x2(bf16_lo(w.p[g][j]) * alpha, bf16_hi(w.p[g][j]) * alpha);
+        st.limit = top > st.limit ? m + kSlack : st.limit;
         st.m = m;
-        st.limit = m + kSlack;
     }
 }
 
@@ -314,13 +363,19 @@ __device__ __forceinline__ void close_tree_rows(const CacheAttnArgs& a, TreeRows
 // in several; a tile that lies in one run writes its results, one that is cut leaves a part in slot (workgroup + tile)
 // for each, which are neighbours for the join.  Tiles without pages go with the place where they lie.  Pages are counted
 // in units of 2^unit, a tile's rounded up, which keeps their sum below 2^31.
+// A second tile in a run costs a second start, some pages' time: where runs up to that much longer can each keep to
+// one tile, a tile's units are rounded up to whole runs (2 x 60 nodes of 32 over 8 heads at 2000: 29.0 -> 23.8 us, 16 x 16
+// at 8192, head dim 64: 40.7 -> 37).
+constexpr int kStart = 3;   // pages
 struct Share {
     int32_t item, total, each, lo, hi;   // the workgroup; units: all, of a run, of this one
     int32_t e, at;                       // the next tile and its first unit
     int32_t last;                        // the last workgroup that has a run
+    int32_t whole;                       // a tile takes a multiple of so many
 };
-__device__ __forceinline__ int tile_units(const CacheAttnArgs& a, const PageList& l) {
-    return int((uint32_t(l.count) + (1u << a.unit) - 1) >> a.unit);
+__device__ __forceinline__ int tile_units(const CacheAttnArgs& a, const PageList& l, int whole) {
+    const int n = int((uint32_t(l.count) + (1u << a.unit) - 1) >> a.unit);
+    return whole == 1 ? n : (n + whole - 1) / whole * whole;
 }
 __device__ __forceinline__ PageList pages_of_tile(const CacheAttnArgs& a, int e, int rows) {
     const int b = e / a.tiles;
@@ -328,19 +383,28 @@ __device__ __forceinline__ PageList pages_of_tile(const CacheAttnArgs& a, int e,
 }
 __device__ __forceinline__ bool open_share(const CacheAttnArgs& a, int rows, int lane, Share& s) {
     const int E = a.c.B * a.tiles;
-    auto units = [&](int e) { return e < E ? tile_units(a, pages_of_tile(a, e, rows)) : 0; };
+    auto units = [&](int e, int whole) { return e < E ? tile_units(a, pages_of_tile(a, e, rows), whole) : 0; };
     int sum = 0;
-    for (int e = lane; e < E; e += 64) sum += units(e);
+    for (int e = lane; e < E; e += 64) sum += units(e, 1);
     s.item = blockIdx.x / a.c.Hkv;
     s.total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
     s.each = max((s.total + a.items - 1) / a.items, kMinChunk);
+    s.whole = 1;
+    if (E <= 64)
+        for (int each = s.each; each <= s.each + kStart; ++each) {
+            const int runs = __builtin_amdgcn_readlane(wave_scan((sum + each - 1) / each), 63);
+            if (runs > a.items) continue;
+            s.total = runs * each;
+            s.each = s.whole = each;
+            break;
+        }
     s.last = max(s.total - 1, 0) / s.each;
     if (s.item > s.last) return false;
     s.lo = s.item * s.each;
     s.hi = min(s.lo + s.each, s.total);
     s.at = 0;
     for (int e0 = 0; e0 < E; e0 += 64) {   // the first tile that ends behind lo, or lies there without pages
-        const int n = units(e0 + lane), end = s.at + wave_scan(n);
+        const int n = units(e0 + lane, s.whole), end = s.at + wave_scan(n);
         const uint64_t here = __ballot(e0 + lane < E && (end > s.lo || (n == 0 && end >= s.lo)));
         if (here) {
             const int l = __builtin_ctzll(here);
@@ -358,7 +422,7 @@ __device__ __forceinline__ bool next_tile(const CacheAttnArgs& a, int rows, Shar
     k.b = s.e / a.tiles;
     k.tr = tile_rows<true>(a, k.b, __builtin_amdgcn_readfirstlane(length_of(a, k.b)), s.e % a.tiles, rows);
     k.pl = tile_pages(a, k.tr);
-    const int n = tile_units(a, k.pl), end = s.at + n;
+    const int n = tile_units(a, k.pl, s.whole), end = s.at + n;
     const int first = min(s.at, max(s.total - 1, 0)) / s.each, last = n > 0 ? (end - 1) / s.each : first;
     k.ch = Chunk{s.e, first + s.e, last - first + 1, s.item - first, 0};
     k.c0 = int(min(int64_t(max(s.lo - s.at, 0)) << a.unit, int64_t(k.pl.count)));
@@ -372,197 +436,213 @@ __device__ __forceinline__ bool next_tile(const CacheAttnArgs& a, int rows, Shar
     return true;
 }
 
-// A tile's rows over the pages [k.c0, k.c1) of its list.
-constexpr int kTreeRows = 128;
+// The two token halves of a tile's rows: the waves of the second leave theirs in `mem`, those of the first add them.
 template <int D>
-__device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k, uint8_t (*kb)[TreePage<D>::kKeys],
-                                          uint8_t (*vb)[TreePage<D>::kValues]) {
-    constexpr int NV = D / 64;   // 16-byte pieces of a page's keys, and of its values, per thread
+__device__ __forceinline__ void merge_halves(TreeRows<D>& st, bool second, float* mem, int lane) {
+    constexpr int N = D / 32;
+    float* at = mem + lane;
+    if (second) {
+#pragma unroll
+        for (int b = 0; b < N; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) at[(16 * b + r) * 64] = st.o[b][r];
+        at[16 * N * 64] = st.m;
+        at[16 * N * 64 + 64] = st.l;
+    }
+    __syncthreads();
+    if (second) return;
+    const float m2 = at[16 * N * 64], m = fmaxf(st.m, m2), f1 = fast_exp2(st.m - m), f2 = fast_exp2(m2 - m);
+    st.l = st.l * f1 + at[16 * N * 64 + 64] * f2;
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st.o[b][r] = st.o[b][r] * f1 + at[(16 * b + r) * 64] * f2;
+    st.m = m;
+}
+
+// A tile's rows over the pages [k.c0, k.c1) of its list, 32 a wave.  SPLIT: of up to 64 rows; two waves share 32, each takes
+// half of every page's tokens.
+constexpr int tree_rows(bool split) { return split ? 64 : 128; }
+template <int D>
+struct TreeMemory {
+    uint8_t k[kDepth][kPage * D], v[kDepth][kPage * D];
+};
+template <int D, bool SPLIT>
+__device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k, TreeMemory<D>& mem) {
+    constexpr int NF = D / 64;          // pieces of 16 bytes of a page's keys, and of its values, per thread
+    constexpr int kBytes = kPage * D;   // of either
     const int tid = threadIdx.x, lane = tid & 63;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // (the two workgroups of a CU start from either half of its SIMDs, so that tiles of up to 64 rows, which two waves
-    // take, use them all)
-    const int wr0 = k.tr.r0 + 32 * ((w + 2 * (blockIdx.x / 256 & 1)) & 3);
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), th = SPLIT ? w >> 1 : 0;
+    // (the two workgroups of a CU start from either half of its SIMDs, so that tiles of few rows use them all)
+    const int wr0 = k.tr.r0 + 32 * (SPLIT ? w & 1 : (w + 2 * (blockIdx.x / 256 & 1)) & 3);
     const bool live = wr0 < a.T * (a.Hq / a.c.Hkv);
     TreeRows<D> st;
     open_tree_rows(a, st, k, wr0, lane);
-    // this lane's operands: a token's columns from 8 h on, a column's tokens from 8 h on
-    const int kat = token_of(lane & 31) * TreePage<D>::kKeyRow + 16 * (lane >> 5);
-    const int vat = (lane & 31) * TreePage<D>::kValueRow + 16 * (lane >> 5);
+    // this lane's operands: of a token the pieces h, 2 + h, .., of a column the piece of its half of this wave's tokens
+    const int i32 = lane & 31, h = lane >> 5, tok = token_of(i32) + 32 * th;
+    const int kat = tok * D + 16 * (h ^ key_order<D>(tok)), vat = i32 * kPage + 16 * ((2 * th + h) ^ value_order(i32));
+    const int kat1 = kat + 32 * D, vat1 = vat ^ 32;   // of the page's second half
+    // what this thread fetches: bytes 16 tid .. of every 4096 of a page
+    const int kf = 16 * tid / D, vf = tid / 4, piece = (tid & 3) ^ value_order(vf);
+    const uint32_t from_k = kf * D + 16 * ((tid % (D / 16)) ^ key_order<D>(kf)), from_v = kPage * vf + 16 * piece;
+    const uint32_t lds_k = lds_addr(mem.k) + 1024 * w, lds_v = lds_addr(mem.v) + 1024 * w;
     // what all rows see in full ends before the first node; what none sees lies before `far`
     const int base = k.tr.base, len = k.tr.len, far = base - a.W;
     auto in_part = [&](int t0) { return partly(t0, base - 1, len - 1, a.W, a.S); };
-    u32x4 raw_k[2][NV], raw_v[2][NV];   // codes of two pages on their way, the even and the odd one
-    auto load = [&](u32x4* raw, const uint8_t* codes, int page) {
-        const uint8_t* p = codes + (int64_t(max(page, 0)) * a.c.Hkv + k.hk) * (kPage * D);
-#pragma unroll
-        for (int n = 0; n < NV; ++n) raw[n] = *reinterpret_cast<const u32x4*>(p + 16 * (tid + kThreads * n));
-    };
-    auto convert_keys = [&](u32x4* raw, int buf) {
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int x = tid + kThreads * n;
-            u32x4* to = reinterpret_cast<u32x4*>(kb[buf] + x / (D / 16) * TreePage<D>::kKeyRow + 32 * (x % (D / 16)));
-            to[0] = codes_to_bf16(raw[n].x, raw[n].y);
-            to[1] = codes_to_bf16(raw[n].z, raw[n].w);
-        }
-    };
-    // (Codes of tokens that no row sees may stand for anything, NaN among it, which a weight of 0 would not
-    // remove: they are cleared.)
-    auto convert_values = [&](u32x4* raw, int buf, int t0, float power) {
-        if (in_part(t0)) {
-            keep_branch();
-            const int lim = min(a.S, len);
-            const int x0 = t0 + 16 * (opaque(tid) & 3);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t keep = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int x = x0 + 4 * j + e;
-                    if (x < len && (x > far || x < lim)) keep |= 0xffu << (8 * e);
-                }
-#pragma unroll
-                for (int n = 0; n < NV; ++n) raw[n][j] &= keep;
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            u32x4* to = reinterpret_cast<u32x4*>(vb[buf] + (tid + kThreads * n) / 4 * TreePage<D>::kValueRow + 32 * (tid & 3));
-            to[0] = codes_to_bf16(raw[n].x, raw[n].y, power);
-            to[1] = codes_to_bf16(raw[n].z, raw[n].w, power);
-        }
-    };
-    // Halves of pages: 2 i and 2 i + 1 are those of page i.  While half x becomes weights, the logits of half x + 1
-    // and the product of half x - 1 with its values are formed.  Interval i, from barrier to barrier, takes the
-    // halves 2 i + 1 and 2 i + 2: it reads the keys of page i + 1 and the values of page i, converts the keys of page
-    // i + 2 and the values of page i + 1, and asks for the codes that the one after the next converts.
     const int n = k.c1 - k.c0;
     if (n > 0) {
-        constexpr int kLooks = 60;   // pages looked up at a time, and the four after them
+        constexpr int kLooks = 64 - kDepth;   // pages looked up at a time, and those after them
         Pages pages;
         ValueScale scales;
+        uint32_t off_lo, off_hi;   // where a page's codes lie
         int x0 = 0;
         auto look = [&](int x) {
             x0 = x;
             pages = look_up(a, k, k.c0 + x, 1, lane);
             scales = value_scale(pages.vs);
+            const uint64_t off = (uint64_t(max(pages.page, 0)) * a.c.Hkv + k.hk) * kBytes;
+            off_lo = uint32_t(off);
+            off_hi = uint32_t(off >> 32);
         };
         look(0);
-        auto page = [&](int i) { return page_at(pages, i - x0); };
-        auto start = [&](int i) { return page_start(page(i), k.pl.page(k.c0 + i)); };
-        // (the factor stays above 0, as a masked logit times 0 would be NaN)
-        auto factor = [&](int i) { return lane_value(pages.ks, i - x0); };
-        auto scale_of = [&](int i) {
-            return ValueScale{0.f, lane_value(scales.shift, i - x0), lane_value(scales.back, i - x0)};
+        // (past the last page as many, of 16 bytes of the pool's first page, so that a step's wait counts the same)
+        auto fetch = [&](const uint8_t* codes, uint32_t from, uint32_t to, int i, int slot) {
+            const uint64_t off = uint32_t(__builtin_amdgcn_readlane(off_lo, i - x0)) |
+                                 uint64_t(uint32_t(__builtin_amdgcn_readlane(off_hi, i - x0))) << 32;
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+                fetch16(codes + off + 4096 * j, i < n ? from : 0, to + kBytes * slot + 4096 * j);
         };
-        auto load_k = [&](int i) {
-            if (i < n) load(raw_k[i & 1], a.c.k, page(i));
-        };
-        auto load_v = [&](int i) {
-            if (i < n) load(raw_v[i & 1], a.c.v, page(i));
-        };
-        auto values = [&](int i) { convert_values(raw_v[i & 1], i & 1, start(i), lane_value(scales.power, i - x0)); };
-        load_k(0);
-        load_v(0);
-        load_k(1);
-        load_v(1);
         __syncthreads();   // the tile before has been read
-        convert_keys(raw_k[0], 0);
-        load_k(2);
-        values(0);
-        load_v(2);
-        if (n > 1) convert_keys(raw_k[1], 1);
-        load_k(3);
+        // Step i: the weights of page i, the logits of the tokens after them and the product of those before with their
+        // values.  It reads the keys of pages i (SPLIT: no more) and i + 1 and the values of pages i - 1 and i (SPLIT: not
+        // yet), and asks for the keys of page i + kAheadK and the values of page i + kDepth - 2.
+        constexpr int kAheadK = SPLIT ? kDepth : kDepth - 1;
+        constexpr int kLeft = (SPLIT ? kDepth - 2 : kDepth - 3) * 2 * NF;   // fetches behind those that a step needs
+#pragma unroll
+        for (int i = 0; i < kAheadK; ++i) {
+            fetch(a.c.k, from_k, lds_k, i, i);
+            const int v = i + kDepth - 2 - kAheadK;
+            if (v >= 0) fetch(a.c.v, from_v, lds_v, v, v);
+        }
+#pragma unroll
+        for (int j = 0; j < NF; ++j)   // (the first weights, which are 0, meet no values yet)
+            *reinterpret_cast<u32x4*>(mem.v[kDepth - 1] + 16 * tid + 4096 * j) = u32x4{};
+        wait_fetched<SPLIT ? kLeft : kLeft + 2 * NF>();
         __syncthreads();
-        // P: whether i is odd
-        auto interval = [&](auto P, int i) {
-            __syncthreads();
-            // Of two waves that could issue the older one does: of the two workgroups of a CU the first took 316 us and
-            // the second, then alone, 409 (8 contexts of up to 64K x 8 heads).  The second leads every other page: 372
-            // and 382.
-            if (blockIdx.x & 256) __builtin_amdgcn_s_setprio(P);
-            if (i - x0 >= kLooks) look(i);
-            if (i + 2 < n) convert_keys(raw_k[P], P);
-            if (i + 4 < n) load(raw_k[P], a.c.k, page(i + 4));
-            if (i + 1 < n) convert_values(raw_v[P ^ 1], P ^ 1, start(i + 1), lane_value(scales.power, i + 1 - x0));
-            if (i + 3 < n) load(raw_v[P ^ 1], a.c.v, page(i + 3));
-        };
-        constexpr std::integral_constant<int, 0> kEven{};
-        constexpr std::integral_constant<int, 1> kOdd{};
-        if (!live) {
-            for (int i = 0; i < n; i += 2) {
-                interval(kEven, i);
-                if (i + 1 < n) interval(kOdd, i + 1);
-            }
-            return;
-        }
-        f32x16 s0, s1;
+        TreeLogits cur = tree_first(st, mem.k[0], kat);
         TreeHalf left{};   // (no weights yet: 0)
-        // what this lane's row sees of half `half` of page i (asked for where some row does not see all)
-        auto seen = [&](int i, int half) {
-            return [=, &a, &k] {
-                const int t0 = start(i) + 32 * half;
-                const int l = opaque(lane);
-                return uint32_t(row_sees(a, wr0 + (l & 31), t0, k) >> (8 * (l >> 5)));
-            };
+        int kslot = 0, vslot = kDepth - 1;   // of page i's keys, page i - 1's values
+        auto after = [](int slot) { return slot == kDepth - 1 ? 0 : slot + 1; };
+        auto before = [](int slot) { return slot == 0 ? kDepth - 1 : slot - 1; };
+        float power = 1.f;   // of page i - 1
+        auto start_of = [&](int i) {
+            return __builtin_amdgcn_readfirstlane(page_start(page_at(pages, i - x0), k.pl.page(k.c0 + i)));
         };
-        bool part = in_part(start(0));
-        float fac = factor(0);
-        ValueScale vs = scale_of(0);
-        tree_first<D>(st, s0, kb[0] + kat);
-        tree_top<D>(st, s0, left, part, seen(0, 0), fac);
-        tree_half<D>(st, s0, s1, left, kb[0] + kat + 32 * TreePage<D>::kKeyRow, vb[0] + vat, 0, fac, vs);
-        auto step = [&](auto P, int i) {
-            const uint8_t *kn = kb[P ^ 1] + kat, *vn = vb[P] + vat, *kn2 = kn + 32 * TreePage<D>::kKeyRow;
-            interval(P, i);
-            tree_top<D>(st, s1, left, part, seen(i, 1), fac);
-            tree_half<D>(st, s1, s0, left, kn, vn, 0, fac, vs);
-            part = in_part(start(i + 1));
-            fac = factor(i + 1);
-            vs = scale_of(i + 1);
-            tree_top<D>(st, s0, left, part, seen(i + 1, 0), fac);
-            tree_half<D>(st, s0, s1, left, kn2, vn, 1, fac, vs);
+        // The values at `slot`, of a page that begins at t0, are there: codes of tokens that no row sees may stand for
+        // anything, NaN among it, which a weight of 0 would not remove; each thread clears those that it has fetched.
+        auto enter = [&](int slot, int t0) {
+            wait_fetched<kLeft>();
+            if (t0 >= 0 && in_part(t0)) {
+                keep_branch();
+                const int lim = min(a.S, len), x0 = t0 + 16 * (opaque(tid) & 3 ^ value_order(opaque(tid) / 4));
+                u32x4 keep;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    keep[j] = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int x = x0 + 4 * j + e;
+                        if (x < len && (x > far || x < lim)) keep[j] |= 0xffu << (8 * e);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < NF; ++j) *reinterpret_cast<u32x4*>(mem.v[slot] + 16 * tid + 4096 * j) &= keep;
+            }
+            __syncthreads();
         };
-        int i = 0;
-        for (; i + 2 < n; i += 2) {
-            step(kEven, i);
-            step(kOdd, i + 1);
+        int start0 = -1;   // of page i - 1
+        for (int i = 0; i < n; ++i) {
+            if (i - x0 >= kLooks) look(i);
+            const int start = start_of(i);
+            if constexpr (SPLIT) enter(vslot, start0);
+            else enter(after(vslot), start);
+            // Of two waves that could issue the older one does: of a CU's workgroups the second then lags behind the first
+            // and works alone in the end.  It leads every other page (128 rows, contexts of 16K: 131 -> 127 us).
+            if (blockIdx.x & 256) {
+                if (i & 1) __builtin_amdgcn_s_setprio(1);
+                else __builtin_amdgcn_s_setprio(0);
+            }
+            fetch(a.c.k, from_k, lds_k, i + kAheadK, SPLIT ? kslot : before(kslot));
+            fetch(a.c.v, from_v, lds_v, i + kDepth - 2, before(vslot));
+            const float now = lane_value(scales.power, i - x0);
+            if (live) {
+                // (the factor stays above 0, as a masked logit times 0 would be NaN)
+                const float fac = lane_value(pages.ks, i - x0);
+                const ValueScale vs{0.f, lane_value(scales.shift, i - x0), lane_value(scales.back, i - x0)};
+                const bool part = in_part(start);
+                // what this lane's row sees of its tokens of half x of the page (asked for where some row does not see all)
+                auto seen = [&](int x) {
+                    return [=, &a, &k] {
+                        const int l = opaque(lane);
+                        return uint32_t(row_sees(a, wr0 + (l & 31), start + 32 * x, k) >> (16 * (l >> 5)));
+                    };
+                };
+                tree_top(st, cur, left, part, seen(th), fac);
+                if constexpr (SPLIT) {   // (the last step's logits are of no page, for nothing)
+                    tree_half(st, cur, left, mem.k[after(kslot)], kat, mem.v[vslot] + vat, fac, vs, power);
+                } else {
+                    tree_half(st, cur, left, mem.k[kslot], kat1, mem.v[vslot] + vat1, fac, vs, power);
+                    tree_top(st, cur, left, part, seen(1), fac);
+                    tree_half(st, cur, left, mem.k[after(kslot)], kat, mem.v[after(vslot)] + vat, fac, vs, now);
+                }
+            }
+            power = now;
+            start0 = start;
+            kslot = after(kslot);
+            vslot = after(vslot);
         }
-        if (i + 1 < n) step(kEven, i++);
-        const uint8_t* vn = vb[i & 1] + vat;
-        if (i & 1) interval(kOdd, i);
-        else interval(kEven, i);
-        tree_top<D>(st, s1, left, part, seen(i, 1), fac);
-        tree_half<D>(st, s1, s0, left, kb[0] + kat, vn, 0, fac, vs);   // (logits of no page, for nothing)
-        tree_flush<D>(st, left, vn, 1);
+        if constexpr (SPLIT) enter(vslot, start0);
+        if (live) tree_flush(st, left, mem.v[vslot] + (SPLIT ? vat : vat1), power);
+        wait_fetched<0>();
+        if constexpr (SPLIT) {
+            __syncthreads();
+            merge_halves(st, th, reinterpret_cast<float*>(&mem) + (w & 1) * (sizeof(TreeMemory<D>) / 8), lane);
+        }
     }
-    if (live) close_tree_rows(a, st, k, wr0, kTreeRows, lane);
+    if (live && th == 0) close_tree_rows(a, st, k, wr0, tree_rows(SPLIT), lane);
 }
 
-template <int D>
+template <int D, bool SPLIT>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3)))
 tree_rows_kernel(CacheAttnArgs a) {
-    __shared__ __attribute__((aligned(16))) uint8_t kb[2][TreePage<D>::kKeys], vb[2][TreePage<D>::kValues];
+    __shared__ __attribute__((aligned(16))) TreeMemory<D> mem;
+    constexpr int kRows = tree_rows(SPLIT);
     const int lane = threadIdx.x & 63;
     Walk k;
     Share share;
     if (a.items > 0) {
-        if (!open_share(a, kTreeRows, lane, share) || !next_tile(a, kTreeRows, share, k)) return;
-    } else if (!open_walk<false, true>(a, kTreeRows, lane, k)) {
+        if (!open_share(a, kRows, lane, share) || !next_tile(a, kRows, share, k)) return;
+    } else if (!open_walk<false, true>(a, kRows, lane, k)) {
         return;
     }
     do {
         make_uniform(k);
-        tree_tile<D>(a, k, kb, vb);
-    } while (a.items > 0 && next_tile(a, kTreeRows, share, k));
+        tree_tile<D, SPLIT>(a, k, mem);
+    } while (a.items > 0 && next_tile(a, kRows, share, k));
 }
 
 }  // namespace
 
-void launch_tree_rows(const CacheAttnArgs& a, dim3 grid, hipStream_t s) {
-    if (a.c.d == 128) hipLaunchKernelGGL(tree_rows_kernel<128>, grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL(tree_rows_kernel<64>, grid, dim3(kThreads), 0, s, a);
+void launch_tree_rows(const CacheAttnArgs& a, int rows, dim3 grid, hipStream_t s) {
+    const dim3 t(kThreads);
+    if (rows == tree_rows(true)) {
+        if (a.c.d == 128) hipLaunchKernelGGL((tree_rows_kernel<128, true>), grid, t, 0, s, a);
+        else hipLaunchKernelGGL((tree_rows_kernel<64, true>), grid, t, 0, s, a);
+    } else {
+        if (a.c.d == 128) hipLaunchKernelGGL((tree_rows_kernel<128, false>), grid, t, 0, s, a);
+        else hipLaunchKernelGGL((tree_rows_kernel<64, false>), grid, t, 0, s, a);
+    }
 }
 
 hipError_t launch_tree_mask(const TreeMaskArgs& a, hipStream_t s) {
