@@ -351,15 +351,18 @@ __global__ void __launch_bounds__(kThreads) fork_fill_kernel(ForkArgs a) {
 // table, finds its own row's pages there by their order, and writes its row, its share of the new
 // counts and its copy.  What rows ask for follows from their lengths alone but for a first taker's
 // pages behind its tokens, which are counted on the way.  A call is bound by its chains of reads and
-// by launches: 9.9 us against 14 for 8 sequences with 16 entries each, 15.8 against 20.2 for 256
-// from 64 with 24 and 4000 pages, 19.9 against 22.6 for 64 from 8 with 1024 and 10000 pages.
-// Beyond that the work that every workgroup repeats costs more: 29 us against 19 for 128 with 128
-// and 19000 pages, 62 against 39 for 1024 from 64.  (1024 threads: 11.3, 16.4 and 18.0 us.)
+// by launches: 9.9 us against 14 for 8 sequences with 16 entries each, 15.9 against 20.1 for 256
+// from 64 with 24 and 4000 pages, 17.9 against 22.1 for 64 from 8 with 1024 and 10000 pages, 22.0
+// against 22.2 for 256 from 64 with 133 and 9800.  Beyond that the work that every workgroup
+// repeats costs more: 24 us against 18 for 128 with 128 and 19000 pages, 62 against 39 for 1024
+// from 64.  Many words are read by 1024 threads (the third of these 19.8 us with 512), few by 512
+// (the first 11.3 with 1024).
 struct SmallFork {   // where each lies, in words; bytes: of all, -1: more than LDS is given
     int32_t first, takers, full, held, room, gaps, given, bytes;
 };
-constexpr int kSmallThreads = 512, kSmallBytes = 80 * 1024;   // two workgroups a CU
+constexpr int kSmallBytes = 80 * 1024;   // two workgroups a CU
 constexpr int64_t kSmallRows = 256, kSmallReads = 20000;   // rows; words that each workgroup reads
+constexpr int64_t kSmallFew = 6000;   // of them, that 512 threads read
 __host__ __device__ inline SmallFork small_fork(int64_t pages, int64_t B, int64_t width) {
     SmallFork f{};
     int64_t at = pages;
@@ -373,6 +376,7 @@ __host__ __device__ inline SmallFork small_fork(int64_t pages, int64_t B, int64_
     return f;
 }
 
+template <int kSmallThreads>
 __global__ void __launch_bounds__(kSmallThreads) fork_small_kernel(ForkArgs a, SmallFork f) {
     extern __shared__ int32_t lds[];
     __shared__ int red[kSmallThreads / 64];
@@ -509,7 +513,8 @@ hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s) {
     TraceScope _t("cache_fork", s);
     const dim3 t(kThreads), by_pages(unsigned((int64_t(a.c.pages) + kThreads - 1) / kThreads));
     const SmallFork f = small_fork(a.c.pages, a.c.B, a.c.width);
-    if (f.bytes > 0 && a.N <= kSmallRows && int64_t(a.c.B) * a.c.width + a.c.pages <= kSmallReads) {
+    const int64_t reads = int64_t(a.c.B) * a.c.width + a.c.pages;
+    if (f.bytes > 0 && a.N <= kSmallRows && reads <= kSmallReads) {
         ForkArgs b = a;
         if (a.refs == a.refs_out) {   // (the counts are read by all while they are written)
             b.refs_out = a.list;
@@ -517,7 +522,8 @@ hipError_t launch_cache_fork(const ForkArgs& a, hipStream_t s) {
             b.refs = a.list;
             b.refs_out = a.refs_out;
         }
-        hipLaunchKernelGGL(fork_small_kernel, dim3(unsigned(a.N)), dim3(kSmallThreads), f.bytes, s, b, f);
+        if (reads > kSmallFew) hipLaunchKernelGGL(fork_small_kernel<1024>, dim3(unsigned(a.N)), dim3(1024), f.bytes, s, b, f);
+        else hipLaunchKernelGGL(fork_small_kernel<512>, dim3(unsigned(a.N)), dim3(512), f.bytes, s, b, f);
         return hipGetLastError();
     }
     if (a.refs != a.refs_out) hipLaunchKernelGGL(fork_refs_kernel, by_pages, t, 0, s, a);

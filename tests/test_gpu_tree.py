@@ -140,6 +140,7 @@ def test_tree_attn_matches_oracle(gpu, Hq, Hkv, d, T, contexts, counts, W, S, ki
 
 @pytest.mark.parametrize("Hq,Hkv,d,T,contexts", [
     (4, 1, 64, 3, [20011, 1, 640, 0, 9000]), (28, 4, 128, 12, [8000, 100, 3001]), (8, 2, 128, 40, [5000, 2500]),
+    (28, 4, 128, 8, [4000, 100, 3001]), (8, 2, 64, 16, [9000, 640, 0, 77]), (8, 1, 128, 300, [2000, 1]),
 ])
 def test_tree_attn_long_and_ragged(gpu, Hq, Hkv, d, T, contexts):
     """Many chunks of one context beside short ones."""
