@@ -16,5 +16,10 @@ states:
   attn.py      masked attention forward (out, lse), its gradients
                (Eq. softmax_gradient, Eq. attention_backward) and the
                log-sum-exp merge of partial results (Algorithm 2)
+Beside the paper's path:
+  window.py    attention with a window and sinks, its gradients and error bounds
+  cache.py     the paged cache's codes and scales, append, attention over it
+  tree.py      rotation on several axes, drafted trees' masks and attention
+  pages.py     moves of tokens and of sequences among the cache's pages
 """
 from . import bf16, estimate, index, attn  # noqa: F401

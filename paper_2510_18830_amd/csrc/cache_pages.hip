@@ -16,7 +16,8 @@ constexpr int kThreads = 256;
 // has written.  A workgroup owns the keys or the values of one head of a sequence and takes its
 // pages in turn: it reads the moved tokens' codes into LDS, finds the page's scale (its own, or what
 // tokens from other pages need) and writes them, older tokens too where the scale has grown.
-// Bound by latency: lengths, path, table, scales, codes, one after the other.
+// Bound by latency: lengths, path, table, scales, codes, one after the other, for each page: 16 nodes
+// of 64 sequences, 8 heads of 128, 7.8 us; 200 of 7, 2 heads of 64 (four pages a workgroup), 11.7.
 template <int D>
 __global__ void __launch_bounds__(kThreads) cache_keep_kernel(KeepArgs a) {
     constexpr int kRow = D + 16;
@@ -307,7 +308,8 @@ __device__ __forceinline__ void copy_page(const CacheView& c, int of, int to, in
     }
 }
 
-// A row's pages, and a share of the copy of its last one.
+// A row's pages, and a share of the copy of its last one (1, 2, 4 and 8 of them: 44.9, 41.8, 38.0 and
+// 39.4 us a call for 1024 rows).
 constexpr int kCopyShares = 4;
 __global__ void __launch_bounds__(kThreads) fork_fill_kernel(ForkArgs a) {
     __shared__ int red[kThreads / 64];
