@@ -178,7 +178,8 @@ def test_rotate_in_a_graph_and_on_a_stream(gpu):
 # ---------------------------------------------------------------- the cache
 @pytest.mark.parametrize("B,Hq,Hkv,d,T,lens,counts,axes", [
     (1, 4, 1, 64, 1, [63], None, 1), (3, 4, 2, 128, 70, [0, 30, 64], [70, 0, 33], 3), (2, 6, 2, 64, 130, [5, 100], None, 2),
-    (2, 28, 4, 128, 16, [60, 1000], None, 4),
+    (2, 28, 4, 128, 16, [60, 1000], None, 4), (1, 14, 1, 64, 4200, [17], None, 2), (66, 6, 3, 64, 64, list(range(66)), None, 1),
+    (2, 24, 24, 64, 2050, [1, 64], [2050, 700], 3), (1, 26, 2, 128, 4097, [0], None, 3),
 ])
 def test_append_at_positions(gpu, B, Hq, Hkv, d, T, lens, counts, axes):
     """The cache's values are those of keys rotated by rotate in fp32 and appended without a rotation, up to the fp32
