@@ -22,7 +22,7 @@
 //
 // Few rows are bound by the cache's bytes and each step's chain, many by the issue of instructions (a product takes 16 of
 // its 32 cycles of it) and by power, which lowers the clock.  Contexts of up to 16K, 32 of them, 28 over 4 heads, with the
-// join: 8 nodes 93 us, 16 126, 32 206 (0.70 PFLOP/s; a plain matrix product of bf16 reaches 1.37).  Codes converted once for the
+// join: 8 nodes 88 us, 16 124, 32 205 (0.70 PFLOP/s; a plain matrix product of bf16 reaches 1.37).  Codes converted once for the
 // four waves to bf16 in LDS, twice its bytes: 102, 128 and 213 us; 64 rows a wave, which halves LDS's bytes and the
 // conversions, one wave a SIMD: 132, 142 and 243.
 #include "cache_walk.h"
@@ -363,19 +363,22 @@ __device__ __forceinline__ void close_tree_rows(const CacheAttnArgs& a, TreeRows
 // in several; a tile that lies in one run writes its results, one that is cut leaves a part in slot (workgroup + tile)
 // for each, which are neighbours for the join.  Tiles without pages go with the place where they lie.  Pages are counted
 // in units of 2^unit, a tile's rounded up, which keeps their sum below 2^31.
-// A second tile in a run costs a second start, some pages' time: where runs up to that much longer can each keep to
-// one tile, a tile's units are rounded up to whole runs (2 x 60 nodes of 32 over 8 heads at 2000: 29.0 -> 23.8 us, 16 x 16
-// at 8192, head dim 64: 40.7 -> 37).
-constexpr int kStart = 3;   // pages
+// A second tile in a run costs a second start, about four pages' time (9 us).  Where runs can each keep to one tile at
+// that price, a tile's units are rounded up to whole runs (2 x 60 nodes of 32 over 8 heads at 2000: 29.0 -> 23.8 us, 16 x
+// 16 at 8192, head dim 64: 40.7 -> 37); else every tile counts as so many pages more, before its first, that a run with
+// two of them takes fewer (8 x 128 at 8192, 32 over 8 heads 131 -> 123 us, 32 x 16 at 16384, 28 over 4 127 -> 124).
+constexpr int kStart = 4;
 struct Share {
     int32_t item, total, each, lo, hi;   // the workgroup; units: all, of a run, of this one
     int32_t e, at;                       // the next tile and its first unit
     int32_t last;                        // the last workgroup that has a run
-    int32_t whole;                       // a tile takes a multiple of so many
+    int32_t whole, start;                // a tile takes a multiple of so many units; so many of them are its start
 };
-__device__ __forceinline__ int tile_units(const CacheAttnArgs& a, const PageList& l, int whole) {
-    const int n = int((uint32_t(l.count) + (1u << a.unit) - 1) >> a.unit);
-    return whole == 1 ? n : (n + whole - 1) / whole * whole;
+__device__ __forceinline__ int page_units(const CacheAttnArgs& a, const PageList& l) {
+    return int((uint32_t(l.count) + (1u << a.unit) - 1) >> a.unit);
+}
+__device__ __forceinline__ int tile_units(int n, const Share& s) {
+    return n == 0 ? 0 : s.whole == 1 ? n + s.start : (n + s.whole - 1) / s.whole * s.whole;
 }
 __device__ __forceinline__ PageList pages_of_tile(const CacheAttnArgs& a, int e, int rows) {
     const int b = e / a.tiles;
@@ -383,19 +386,26 @@ __device__ __forceinline__ PageList pages_of_tile(const CacheAttnArgs& a, int e,
 }
 __device__ __forceinline__ bool open_share(const CacheAttnArgs& a, int rows, int lane, Share& s) {
     const int E = a.c.B * a.tiles;
-    auto units = [&](int e, int whole) { return e < E ? tile_units(a, pages_of_tile(a, e, rows), whole) : 0; };
-    int sum = 0;
-    for (int e = lane; e < E; e += 64) sum += units(e, 1);
+    auto units = [&](int e) { return e < E ? page_units(a, pages_of_tile(a, e, rows)) : 0; };
+    int sum = 0, some = 0;
+    for (int e = lane; e < E; e += 64) {
+        const int n = units(e);
+        sum += n;
+        some += n > 0;
+    }
     s.item = blockIdx.x / a.c.Hkv;
-    s.total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
-    s.each = max((s.total + a.items - 1) / a.items, kMinChunk);
+    s.start = a.unit == 0 ? kStart : 0;
     s.whole = 1;
+    const int pages = __builtin_amdgcn_readlane(wave_scan(sum), 63);
+    s.total = pages + s.start * __builtin_amdgcn_readlane(wave_scan(some), 63);
+    s.each = max((s.total + a.items - 1) / a.items, kMinChunk);
     if (E <= 64)
-        for (int each = s.each; each <= s.each + kStart; ++each) {
+        for (int each = max((pages + a.items - 1) / a.items, kMinChunk); each <= s.each; ++each) {
             const int runs = __builtin_amdgcn_readlane(wave_scan((sum + each - 1) / each), 63);
             if (runs > a.items) continue;
             s.total = runs * each;
             s.each = s.whole = each;
+            s.start = 0;
             break;
         }
     s.last = max(s.total - 1, 0) / s.each;
@@ -404,7 +414,7 @@ __device__ __forceinline__ bool open_share(const CacheAttnArgs& a, int rows, int
     s.hi = min(s.lo + s.each, s.total);
     s.at = 0;
     for (int e0 = 0; e0 < E; e0 += 64) {   // the first tile that ends behind lo, or lies there without pages
-        const int n = units(e0 + lane, s.whole), end = s.at + wave_scan(n);
+        const int n = tile_units(units(e0 + lane), s), end = s.at + wave_scan(n);
         const uint64_t here = __ballot(e0 + lane < E && (end > s.lo || (n == 0 && end >= s.lo)));
         if (here) {
             const int l = __builtin_ctzll(here);
@@ -417,16 +427,17 @@ __device__ __forceinline__ bool open_share(const CacheAttnArgs& a, int rows, int
     return false;
 }
 __device__ __forceinline__ bool next_tile(const CacheAttnArgs& a, int rows, Share& s, Walk& k) {
-    if (s.e >= a.c.B * a.tiles || !(s.at < s.hi || (s.at == s.total && s.item == s.last))) return false;
+    if (s.e >= a.c.B * a.tiles) return false;
     k.hk = blockIdx.x % a.c.Hkv;
     k.b = s.e / a.tiles;
     k.tr = tile_rows<true>(a, k.b, __builtin_amdgcn_readfirstlane(length_of(a, k.b)), s.e % a.tiles, rows);
     k.pl = tile_pages(a, k.tr);
-    const int n = tile_units(a, k.pl, s.whole), end = s.at + n;
-    const int first = min(s.at, max(s.total - 1, 0)) / s.each, last = n > 0 ? (end - 1) / s.each : first;
+    const int n = tile_units(page_units(a, k.pl), s), end = s.at + n, from = n > 0 ? s.at + s.start : s.at;   // its first page
+    if (!(from < s.hi || (from == s.total && s.item == s.last))) return false;
+    const int first = min(from, max(s.total - 1, 0)) / s.each, last = n > 0 ? (end - 1) / s.each : first;
     k.ch = Chunk{s.e, first + s.e, last - first + 1, s.item - first, 0};
-    k.c0 = int(min(int64_t(max(s.lo - s.at, 0)) << a.unit, int64_t(k.pl.count)));
-    k.c1 = int(min(int64_t(min(s.hi, end) - s.at) << a.unit, int64_t(k.pl.count)));
+    k.c0 = int(min(int64_t(max(s.lo - from, 0)) << a.unit, int64_t(k.pl.count)));
+    k.c1 = int(min(int64_t(min(s.hi, end) - from) << a.unit, int64_t(k.pl.count)));
     if (k.hk == 0 && k.ch.index == 0 && threadIdx.x == 0) {
         a.info[2 * s.e] = k.ch.first;
         a.info[2 * s.e + 1] = k.ch.count;
