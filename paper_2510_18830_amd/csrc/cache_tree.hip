@@ -99,13 +99,6 @@ __device__ __forceinline__ void open_tree_rows(const CacheAttnArgs& a, TreeRows<
     st.l = 0.f;
 }
 
-// A value that the compiler does not know to be the same every time: what a rare branch computes from it is not
-// computed ahead of the loop and held in registers.
-__device__ __forceinline__ int opaque(int x) {
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
 // A workgroup's walk in scalar registers (clamps and ballots left it in vector ones).
 __device__ __forceinline__ void make_uniform(Walk& k) {
     for (int32_t* x : {&k.b, &k.c0, &k.c1, &k.tr.r0, &k.tr.len, &k.tr.base, &k.pl.sinks, &k.pl.lo, &k.ch.first, &k.ch.count,

@@ -180,8 +180,15 @@ struct CacheRows {
     int pos[RT];
     int wp0, wp1;   // positions of the first and last row; below 0: rows before the sequence, which see nothing
     int far;        // the last position that the window of no row reaches
-    int node[RT];   // TREE: the row's node of the call, -1: a row behind the sequence's nodes, which sees nothing
+    int b, r0;      // TREE: the sequence, the first row
 };
+
+// A value that the compiler does not know to be the same every time: what a rare branch computes from it is not
+// computed ahead of the loop and held in registers.
+__device__ __forceinline__ int opaque(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
 
 // rows from wr0 on (past the last: that one again) of R = T G
 template <int D, int RT, bool TREE>
@@ -192,15 +199,7 @@ __device__ __forceinline__ void open_rows(const CacheAttnArgs& a, CacheRows<D, R
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int r = min(wr0 + 16 * x + m, R - 1);
-        if constexpr (TREE) {
-            const int t = r / G, at = b * a.T + t;
-            const bool live = t < len - tr.base;
-            st.node[x] = live ? at : -1;
-            // (without a window the position says nothing but that the row is behind the context)
-            st.pos[x] = live ? max(min(a.at ? a.at[at] : tr.base, len - 1), tr.base) : -1;
-        } else {
-            st.pos[x] = max(len - a.T + r / G, -1);   // (a row before the sequence: no difference to a key overflows)
-        }
+        if constexpr (!TREE) st.pos[x] = max(len - a.T + r / G, -1);   // (a row before the sequence: no difference to a key overflows)
         const uint16_t* qp = a.q + b * a.qs[0] + (hk * G + r % G) * a.qs[1] + (r / G) * a.qs[2];
 #pragma unroll
         for (int s = 0; s < CacheRows<D, RT>::KS; ++s)
@@ -214,6 +213,8 @@ __device__ __forceinline__ void open_rows(const CacheAttnArgs& a, CacheRows<D, R
         st.wp0 = tr.base - 1;
         st.wp1 = len - 1;
         st.far = tr.base - a.W;
+        st.b = b;
+        st.r0 = wr0;
         return;
     }
     st.wp0 = len - a.T + min(wr0, R - 1) / G;
@@ -221,12 +222,14 @@ __device__ __forceinline__ void open_rows(const CacheAttnArgs& a, CacheRows<D, R
     st.far = max(st.wp0, 0) - a.W;
 }
 
-// Which of the 16 tokens from slot j on node `node`, at position pos, sees: of the context, which ends
-// at `base`, what its position does, of the nodes behind it (up to slot len) those of its bits.
+// Which of the 16 tokens from slot j on row r of sequence b's tree sees: of the context, which ends at `base`, what its
+// position does (without a window that says nothing but that the row is behind it), of the nodes behind it (up to slot
+// len) those of its bits.  A row behind the nodes sees nothing.
 __device__ __forceinline__ uint32_t below(int n) { return n >= 16 ? 0xffffu : (1u << max(n, 0)) - 1; }
-__device__ __forceinline__ uint32_t node_sees(const CacheAttnArgs& a, int node, int pos, int j, int base, int len, int W,
-                                              int S) {
-    if (node < 0) return 0;
+__device__ __forceinline__ uint32_t node_sees(const CacheAttnArgs& a, int b, int r, int j, int base, int len, int W, int S) {
+    const int t = r / (a.Hq / a.c.Hkv), node = b * a.T + t;
+    if (t >= len - base) return 0;
+    const int pos = max(min(a.at ? a.at[node] : base, len - 1), base);
     uint32_t bits = 0;
     if (j < len && j + 15 >= base) {
         const int u = j - base, w = u >> 5;   // (u > -16: the word before the first is empty)
@@ -330,15 +333,15 @@ __device__ __forceinline__ void page_step(const CacheAttnArgs& a, CacheRows<D, R
         keep_branch();
 #pragma unroll
         for (int x = 0; x < RT; ++x) {
-            const int lim = min(S - 1, st.pos[x]);
             if constexpr (TREE) {
-                const uint32_t sees =
-                    node_sees(a, st.node[x], st.pos[x], t0 + 16 * g4, st.wp0 + 1, st.wp1 + 1, W, S);
+                const int l = opaque(lane);
+                const uint32_t sees = node_sees(a, st.b, st.r0 + 16 * x + (l & 15), t0 + 16 * (l >> 4), st.wp0 + 1, st.wp1 + 1, W, S);
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (!((sees >> e) & 1)) s[x][e >> 2][e & 3] = -INFINITY;
                 continue;
             }
+            const int lim = min(S - 1, st.pos[x]);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -425,7 +428,7 @@ __device__ __forceinline__ void close_rows(const CacheAttnArgs& a, CacheRows<D, 
     for (int x = 0; x < RT; ++x) {
         const int r = wr0 + 16 * x + m;
         if (r >= R) continue;
-        if (TREE && st.node[x] < 0) {   // (pages without a mask have been added to it too)
+        if (TREE && r / G >= k.tr.len - k.tr.base) {   // (pages without a mask have been added to it too)
             st.mx[x] = -INFINITY;
             st.l[x] = 0.f;
 #pragma unroll
