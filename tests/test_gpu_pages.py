@@ -199,7 +199,8 @@ def test_fork_matches_oracle(gpu, B, N, width, pages, Hkv, d, top, spare, in_pla
 
 @pytest.mark.parametrize("B,N,width,pages,top,spare", [
     (3, 5, 40, 25000, 2500, 2), (30, 40, 1300, 9000, 14000, 4), (2, 1100, 4, 3000, 250, 1), (200, 300, 12, 21000, 700, 1),
-    (1, 1024, 2, 2100, 128, 1), (40, 33, 800, 12000, 15000, 9), (8, 256, 1024, 14000, 15000, 9), (1000, 256, 8, 9000, 450, 1),
+    (1, 1024, 2, 2100, 128, 1), (40, 33, 800, 12000, 15000, 9), (8, 256, 1024, 14000, 15000, 9), (1000, 256, 8, 9000, 450, 1), (1400, 256, 6, 11000, 350, 1),
+    (4000, 200, 2, 9000, 100, 0), (8, 256, 1024, 9000, 15000, 9), (8, 257, 1024, 9000, 15000, 9),
 ])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_fork_of_large_pools_and_tables(gpu, B, N, width, pages, top, spare, in_place):

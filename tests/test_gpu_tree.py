@@ -306,11 +306,33 @@ def test_nan_queries_stay_in_their_rows(gpu):
     assert torch.equal(out[0][keep], want[0][keep]) and torch.equal(lse[0][keep], wl[0][keep])
 
 
+@pytest.mark.parametrize("d,T", [(64, 3), (128, 6), (64, 14), (128, 12), (64, 60), (128, 45)])
+@pytest.mark.parametrize("W,S", [(100, 3), (65, 0), (200, 130)])
+def test_nan_outside_the_window_and_behind_the_nodes(gpu, d, T, W, S):
+    """Codes that no row sees may be NaN: those before every row's window and behind the sinks, nodes behind the counts."""
+    Hq, Hkv, contexts, counts = 8, 2, [500, 300, 64], [T, max(T - 2, 1), T]
+    cache, table, L = _filled(13, contexts, T, Hkv, d, gpu, None)
+    q = _randn(1, (3, Hq, T, d), gpu)
+    cnt = _dev(np.array(counts), gpu)
+    total = _dev(np.array(contexts) + np.array(counts), gpu)
+    at, seen = ms.tree_mask(_dev(_parents(5, 3, T), gpu), _dev(np.array(contexts), gpu), counts=cnt, window=W, sinks=S)
+    want = ms.cache_tree_attn(cache, table, total, q, seen, positions=at, counts=cnt, window=W, sinks=S)
+    assert want[0].isfinite().all()
+    for b, n in enumerate(contexts):
+        for j in list(range(S, n - W + 1)) + list(range(n + counts[b], n + T)):
+            page = int(table[b, j // 64])
+            cache.k.view(torch.uint8)[page, :, j % 64] = 0x7f
+            cache.v.view(torch.uint8)[page, :, :, j % 64] = 0xff
+    got = ms.cache_tree_attn(cache, table, total, q, seen, positions=at, counts=cnt, window=W, sinks=S)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("d", [64, 128])
-def test_magnitudes_of_queries_and_scales(gpu, d):
+@pytest.mark.parametrize("T", [24, 7, 70])
+def test_magnitudes_of_queries_and_scales(gpu, T, d):
     """Queries of one large and many small columns, tiny and huge ones, and page scales that are no powers of two and far
     apart."""
-    Hq, Hkv, T, contexts = 4, 2, 24, [500]
+    Hq, Hkv, contexts = 4, 2, [500]
     cache, table, L = _filled(10, contexts, T, Hkv, d, gpu, None)
     g = torch.Generator().manual_seed(3)
     cache.k_scale.copy_(cache.k_scale.cpu() * (1 + torch.rand(cache.k_scale.shape, generator=g)))
