@@ -5,9 +5,8 @@
 // context's last token).  Its position is lens + the number of its ancestors; it sees itself and
 // those ancestors that the window or the sinks leave visible.  A thread walks one node's
 // ancestors, which descend, and writes its words from the last to the first as it passes them: no
-// word is held or read back.  Bound by latency: the walk's LDS reads, one after the other.
-//
-// 64 trees of 16 nodes: 3.4 us.
+// word is held or read back.  Bound by latency: the walk's LDS reads, one after the other (64 trees
+// of 16 nodes 3.4 us).
 //
 // ---- Attention.  The T G rows of a KV head (row r: node r / G, head r % G of the group) are cut into tiles of 128, 32
 // a wave, that walk the pages they see together; up to 64 rows, two waves share 32, and each takes half of every page's
@@ -22,9 +21,9 @@
 //
 // Few rows are bound by the cache's bytes and each step's chain, many by the issue of instructions (a product takes 16 of
 // its 32 cycles of it) and by power, which lowers the clock.  Contexts of up to 16K, 32 of them, 28 over 4 heads, with the
-// join: 8 nodes 88 us, 16 124, 32 205 (0.70 PFLOP/s; a plain matrix product of bf16 reaches 1.37).  Codes converted once for the
-// four waves to bf16 in LDS, twice its bytes: 102, 128 and 213 us; 64 rows a wave, which halves LDS's bytes and the
-// conversions, one wave a SIMD: 132, 142 and 243.
+// join: 8 nodes 88 us, 16 124, 32 205 (0.70 PFLOP/s; a plain matrix product of bf16 reaches 1.37).  Codes converted once
+// for the four waves to bf16 in LDS, twice its bytes: 102, 128 and 213 us; 64 rows a wave, which halves LDS's bytes and
+// the conversions, one wave a SIMD: 132, 142 and 243.
 #include "cache_walk.h"
 #include "tiles.h"
 #include "trace.h"
@@ -84,7 +83,7 @@ struct TreeRows {
     float limit;         // logits beyond it raise m
 };
 constexpr float kNone = -0x1.fffffep127f;   // m of a row without a token yet: finite, so that a masked logit weighs 0
-constexpr int kDepth = 4;   // pages of keys, and of values, in LDS
+constexpr int kDepth = 4;   // pages of keys, and of values, in LDS (5 and 6: the same times)
 
 template <int D>
 __device__ __forceinline__ void open_tree_rows(const CacheAttnArgs& a, TreeRows<D>& st, const Walk& k, int wr0, int lane) {
@@ -425,7 +424,8 @@ __device__ __forceinline__ bool next_tile(const CacheAttnArgs& a, int rows, Shar
     k.b = s.e / a.tiles;
     k.tr = tile_rows<true>(a, k.b, __builtin_amdgcn_readfirstlane(length_of(a, k.b)), s.e % a.tiles, rows);
     k.pl = tile_pages(a, k.tr);
-    const int n = tile_units(page_units(a, k.pl), s), end = s.at + n, from = n > 0 ? s.at + s.start : s.at;   // its first page
+    const int n = tile_units(page_units(a, k.pl), s), end = s.at + n;
+    const int from = n > 0 ? s.at + s.start : s.at;   // its first page
     if (!(from < s.hi || (from == s.total && s.item == s.last))) return false;
     const int first = min(from, max(s.total - 1, 0)) / s.each, last = n > 0 ? (end - 1) / s.each : first;
     k.ch = Chunk{s.e, first + s.e, last - first + 1, s.item - first, 0};

@@ -199,7 +199,8 @@ __device__ __forceinline__ void open_rows(const CacheAttnArgs& a, CacheRows<D, R
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int r = min(wr0 + 16 * x + m, R - 1);
-        if constexpr (!TREE) st.pos[x] = max(len - a.T + r / G, -1);   // (a row before the sequence: no difference to a key overflows)
+        // (a row before the sequence: no difference to a key overflows)
+        if constexpr (!TREE) st.pos[x] = max(len - a.T + r / G, -1);
         const uint16_t* qp = a.q + b * a.qs[0] + (hk * G + r % G) * a.qs[1] + (r / G) * a.qs[2];
 #pragma unroll
         for (int s = 0; s < CacheRows<D, RT>::KS; ++s)
@@ -288,7 +289,8 @@ __device__ __forceinline__ u32x4 operand(const u32x4* x, int p) {
 // see in full: it clears the codes of the tokens that no row sees.
 template <int D, int RT, int TS, int YS, int PARTS, bool TREE, class Key, class Value, class Done, class Clear>
 __device__ __forceinline__ void page_step(const CacheAttnArgs& a, CacheRows<D, RT>& st, int t0, float kscale,
-                                          float vscale, int W, int S, int lane, Key key, Value value, Done keys_done, Clear clear) {
+                                          float vscale, int W, int S, int lane, Key key, Value value, Done keys_done,
+                                          Clear clear) {
     constexpr int KL = CacheRows<D, RT>::KL, ND = CacheRows<D, RT>::ND;
     const int g4 = lane >> 4;
     const bool part = partly(t0, st.wp0, st.wp1, W, S);
@@ -335,7 +337,8 @@ __device__ __forceinline__ void page_step(const CacheAttnArgs& a, CacheRows<D, R
         for (int x = 0; x < RT; ++x) {
             if constexpr (TREE) {
                 const int l = opaque(lane);
-                const uint32_t sees = node_sees(a, st.b, st.r0 + 16 * x + (l & 15), t0 + 16 * (l >> 4), st.wp0 + 1, st.wp1 + 1, W, S);
+                const uint32_t sees = node_sees(a, st.b, st.r0 + 16 * x + (l & 15), t0 + 16 * (l >> 4), st.wp0 + 1,
+                                                st.wp1 + 1, W, S);
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (!((sees >> e) & 1)) s[x][e >> 2][e & 3] = -INFINITY;
