@@ -12,19 +12,27 @@ constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------- tokens
 // Slot L0 + i takes what slot L0 + path[i] holds (L0: the context's length).  A path ascends, so a
-// target's source lies at or behind it, and pages done in ascending order read what no earlier one
-// has written.  A workgroup owns the keys or the values of one head of a sequence and takes its
-// pages in turn: it reads the moved tokens' codes into LDS, finds the page's scale (its own, or what
-// tokens from other pages need) and writes them, older tokens too where the scale has grown.
-// Bound by latency: lengths, path, table, scales, codes, one after the other, for each page: 16 nodes
-// of 64 sequences, 8 heads of 128, 7.8 us; 200 of 7, 2 heads of 64 (four pages a workgroup), 11.7.
+// target's source lies at or behind it, and runs of kKeepPages pages done in ascending order read what
+// no earlier one has written.  A workgroup owns the keys or the values of one head of a sequence: it
+// looks up where the tokens of a run lie (a thread a slot), reads their codes into LDS, finds each
+// page's scale (its own, or what tokens from other pages need) and writes them, older tokens too
+// where the scale has grown.
+// Bound by latency, lengths, path, table, scales, codes, one after the other for each run, and with many
+// tokens by V's bytes, one by one of their columns.  Pages one by one, by two, by four (us): 64 sequences,
+// 8 heads of 128, 5 tokens kept of 16 8.4, 7.5, 7.8; 256 of them 19.8, 17.3, 23.2 (fewer fit a CU); 32 with
+// 128 of 256 43.5, 40.3, 37.8; 7, 2 heads of 64, 100 of 200 20.2, 17.8, 16.4.
+constexpr int kKeepPages = 2, kRun = kKeepPages * kPage;   // pages of a run, their slots
+constexpr int kFlight = 4;   // a thread's loads in flight
 template <int D>
 __global__ void __launch_bounds__(kThreads) cache_keep_kernel(KeepArgs a) {
     constexpr int kRow = D + 16;
-    __shared__ __attribute__((aligned(16))) uint8_t tok[kPage * kRow];   // the moved tokens' codes, [slot][column]
-    __shared__ int from[kPage], slot_of[kPage];   // where a slot's token lies: page (-1: it stays) and slot in it
-    __shared__ float was_of[kPage];  // and its scale there
-    __shared__ float red[kThreads / 64];
+    __shared__ __attribute__((aligned(16))) uint8_t tok[kRun * kRow];   // the moved tokens' codes, [slot][column]
+    __shared__ int from[kRun];      // the page where a slot's token lies, -1: it stays
+    __shared__ int slot_of[kRun];   // its slot there
+    __shared__ float was_of[kRun];  // and its scale there
+    __shared__ int page_of[kKeepPages], others[kKeepPages];
+    __shared__ float scale_of[kKeepPages];
+    __shared__ uint32_t top_of[kKeepPages];             // the largest value from other pages
     const int tid = threadIdx.x;
     const bool value = blockIdx.x & 1;
     const int hk = (blockIdx.x >> 1) % a.c.Hkv, b = (blockIdx.x >> 1) / a.c.Hkv;
@@ -35,97 +43,118 @@ __global__ void __launch_bounds__(kThreads) cache_keep_kernel(KeepArgs a) {
     uint8_t* codes = value ? a.c.v : a.c.k;
     float* scales = value ? a.c.vs : a.c.ks;
     auto base = [&](int page) { return codes + (int64_t(page) * a.c.Hkv + hk) * (kPage * D); };
-    for (int lp = first / kPage; lp <= (first + kept - 1) / kPage; ++lp) {
-        const int page = cache_page(a.c, b, lp);
-        if (page < 0) continue;
-        const int s0 = max(first - lp * kPage, 0), s1 = min(first + kept - lp * kPage, kPage);   // slots that take a token
-        float* scale = scales + int64_t(page) * a.c.Hkv + hk;
-        const float was = *scale;
-        if (tid < kPage) {
-            int f = -1;
-            if (tid >= s0 && tid < s1) {
-                const int i = lp * kPage + tid - first, u = a.path[int64_t(b) * a.T + i];
-                if (u > i && u < nodes) {
-                    const int slot = first + u, p = cache_page(a.c, b, slot / kPage);
-                    f = p;
-                    slot_of[tid] = slot % kPage;
-                }
-            }
+    auto largest = [&](uint32_t w, float sc) {
+        const float x[4] = {__builtin_amdgcn_cvt_f32_fp8(w, 0), __builtin_amdgcn_cvt_f32_fp8(w, 1),
+                            __builtin_amdgcn_cvt_f32_fp8(w, 2), __builtin_amdgcn_cvt_f32_fp8(w, 3)};
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, finite_abs(x[j] * sc));
+        return top;
+    };
+    for (int lp0 = first / kPage; lp0 <= (first + kept - 1) / kPage; lp0 += kKeepPages) {
+        // the run's slots that take a token
+        const int c0 = max(first - lp0 * kPage, 0), c1 = min(first + kept - lp0 * kPage, kRun);
+        if (tid < kRun) {
+            const int i = min(max(lp0 * kPage + tid - first, 0), kept - 1), u = a.path[int64_t(b) * a.T + i];
+            const int page = tid / kPage < (c1 + kPage - 1) / kPage ? cache_page(a.c, b, lp0 + tid / kPage) : -1;
+            const bool takes = page >= 0 && tid >= c0 && tid < c1 && u > i && u < nodes;
+            const int slot = takes ? first + u : 0, p = cache_page(a.c, b, slot / kPage), f = takes ? p : -1;
+            const float was = scales[int64_t(max(page, 0)) * a.c.Hkv + hk];
+            const float there = scales[int64_t(max(f, 0)) * a.c.Hkv + hk];
+            const bool moves = f >= 0 && f != page;
             from[tid] = f;
-            was_of[tid] = f < 0 || f == page ? was : scales[int64_t(f) * a.c.Hkv + hk];
+            slot_of[tid] = slot % kPage;
+            was_of[tid] = moves ? there : was;
+            const bool some = __any(moves);   // (a wave is a page)
+            if (tid % kPage == 0) {
+                page_of[tid / kPage] = page;
+                others[tid / kPage] = some;
+                scale_of[tid / kPage] = was;
+                top_of[tid / kPage] = 0;
+            }
         }
         __syncthreads();
-        // the moved tokens' codes; the largest value among those of other pages
-        float top = 0.f;
-        const int n = s1 - s0;
-        auto largest = [&](uint32_t w, float sc) {
-            const float x[4] = {__builtin_amdgcn_cvt_f32_fp8(w, 0), __builtin_amdgcn_cvt_f32_fp8(w, 1),
-                                __builtin_amdgcn_cvt_f32_fp8(w, 2), __builtin_amdgcn_cvt_f32_fp8(w, 3)};
+        // the moved tokens' codes; the largest value among those of other pages, for each page
+        float top[kKeepPages] = {};
+        auto note = [&](float x, int c) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, finite_abs(x[j] * sc));
+            for (int g = 0; g < kKeepPages; ++g) top[g] = fmaxf(top[g], c / kPage == g ? x : 0.f);
         };
         if (!value) {
-            for (int x = tid; x < n * (D / 16); x += kThreads) {
-                const int s = s0 + x / (D / 16), c = x % (D / 16), f = from[s];
+            constexpr int C = D / 16;   // pieces of a token
+            for (int x = c0 * C + tid; x < c1 * C; x += kThreads) {
+                const int c = x / C, y = x % C, f = from[c];
+                const u32x4 w = *reinterpret_cast<const u32x4*>(base(max(f, 0)) + slot_of[c] * D + 16 * y);
                 if (f < 0) continue;
-                const u32x4 w = *reinterpret_cast<const u32x4*>(base(f) + slot_of[s] * D + 16 * c);
-                *reinterpret_cast<u32x4*>(tok + s * kRow + 16 * c) = w;
-                if (f != page)
+                *reinterpret_cast<u32x4*>(tok + c * kRow + 16 * y) = w;
+                if (f != page_of[c / kPage])
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) largest(w[j], was_of[s]);
+                    for (int j = 0; j < 4; ++j) note(largest(w[j], was_of[c]), c);
             }
         } else {
-            for (int x = tid; x < n * D; x += kThreads) {
-                const int s = s0 + x / D, row = x % D, f = from[s];
-                if (f < 0) continue;
-                const uint8_t w = base(f)[row * kPage + slot_of[s]];
-                tok[s * kRow + row] = w;
-                if (f != page) top = fmaxf(top, finite_abs(__builtin_amdgcn_cvt_f32_fp8(w, 0) * was_of[s]));
-            }
-        }
-        top = wave_max(top);
-        if ((tid & 63) == 0) red[tid >> 6] = top;
-        bool other = false;
-        for (int s = s0; s < s1; ++s) other |= from[s] >= 0 && from[s] != page;
-        __syncthreads();   // also: every read of this page is done
-        top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-        const float now = other ? fmaxf(was, code_scale(top)) : was;
-        const bool grown = now > was;
-        // every word that holds a slot of a moved token, or, where the scale has grown, an older one
-        auto moved = [&](int s, uint32_t held, uint8_t own) -> uint32_t {   // the code of slot s
-            if (s >= s1) return held;
-            const int f = s < s0 ? -1 : from[s];
-            const uint32_t code = f < 0 ? held : own;
-            const float sc = f < 0 ? was : was_of[s];
-            return sc == now ? code : rescale4(code, sc / now) & 0xffu;
-        };
-        if (!value) {
-            const int r0 = grown ? 0 : s0;
-            for (int x = tid; x < (s1 - r0) * (D / 4); x += kThreads) {
-                const int s = r0 + x / (D / 4), c = x % (D / 4);
-                const int f = s < s0 ? -1 : from[s];
-                if (f < 0 && !grown) continue;
-                uint32_t* at = reinterpret_cast<uint32_t*>(base(page) + s * D) + c;
-                const uint32_t w = f < 0 ? *at : *reinterpret_cast<const uint32_t*>(tok + s * kRow + 4 * c);
-                const float sc = f < 0 ? was : was_of[s];
-                *at = sc == now ? w : rescale4(w, sc / now);
-            }
-        } else {
-            const int w0 = grown ? 0 : s0 / 4, w1 = (s1 + 3) / 4;
-            for (int x = tid; x < D * (w1 - w0); x += kThreads) {
-                const int row = x / (w1 - w0), w = w0 + x % (w1 - w0);
-                uint32_t* at = reinterpret_cast<uint32_t*>(base(page) + row * kPage) + w;
-                const uint32_t held = *at;
-                uint32_t r = 0;
+            for (int x0 = c0 * D + tid; x0 < c1 * D; x0 += kFlight * kThreads) {
+                uint8_t w[kFlight];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int s = 4 * w + e;
-                    r |= moved(s, (held >> (8 * e)) & 0xffu, tok[s * kRow + row]) << (8 * e);
+                for (int e = 0; e < kFlight; ++e) {   // (of a token that stays, any byte)
+                    const int x = min(x0 + e * kThreads, c1 * D - 1), c = x / D;
+                    w[e] = base(max(from[c], 0))[x % D * kPage + slot_of[c]];
                 }
-                *at = r;
+#pragma unroll
+                for (int e = 0; e < kFlight; ++e) {
+                    const int x = x0 + e * kThreads, c = x / D;
+                    if (x >= c1 * D || from[c] < 0) continue;
+                    tok[c * kRow + x % D] = w[e];
+                    if (from[c] != page_of[c / kPage])
+                        note(finite_abs(__builtin_amdgcn_cvt_f32_fp8(w[e], 0) * was_of[c]), c);
+                }
             }
         }
-        if (grown && tid == 0) *scale = now;
+#pragma unroll
+        for (int g = 0; g < kKeepPages; ++g)
+            if (others[g]) {
+                const float most = wave_max(top[g]);
+                if (tid % 64 == 0) atomicMax(top_of + g, __float_as_uint(most));
+            }
+        __syncthreads();   // also: every read of these pages is done
+        for (int g = 0; g < kKeepPages; ++g) {
+            const int page = page_of[g];
+            const int s0 = max(c0 - g * kPage, 0), s1 = min(c1 - g * kPage, kPage);   // slots that take a token
+            if (page < 0 || s0 >= s1) continue;
+            const int at0 = g * kPage;   // of the page's slots in the run
+            const float was = scale_of[g];
+            const float now = others[g] ? fmaxf(was, code_scale(__uint_as_float(top_of[g]))) : was;
+            const bool grown = now > was;
+            if (!value) {   // every word of a moved token, or, where the scale has grown, an older one
+                const int r0 = grown ? 0 : s0;
+                for (int x = tid; x < (s1 - r0) * (D / 4); x += kThreads) {
+                    const int s = r0 + x / (D / 4), c = x % (D / 4);
+                    const int f = s < s0 ? -1 : from[at0 + s];
+                    if (f < 0 && !grown) continue;
+                    uint32_t* at = reinterpret_cast<uint32_t*>(base(page) + s * D) + c;
+                    const uint32_t w = f < 0 ? *at : *reinterpret_cast<const uint32_t*>(tok + (at0 + s) * kRow + 4 * c);
+                    const float sc = f < 0 ? was : was_of[at0 + s];
+                    *at = sc == now ? w : rescale4(w, sc / now);
+                }
+            } else {   // a thread a row: every word that holds a slot of one
+                const int w0 = grown ? 0 : s0 / 4, w1 = (s1 + 3) / 4;
+                for (int w = w0 + tid / D; w < w1; w += kThreads / D) {
+                    const int row = tid % D;
+                    uint32_t* at = reinterpret_cast<uint32_t*>(base(page) + row * kPage) + w;
+                    const uint32_t held = *at;
+                    uint32_t r = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int s = 4 * w + e, f = s < s0 || s >= s1 ? -1 : from[at0 + s];
+                        uint32_t code = f < 0 ? (held >> (8 * e)) & 0xffu : tok[(at0 + s) * kRow + row];
+                        const float sc = f < 0 ? was : was_of[at0 + s];
+                        if (s < s1 && sc != now) code = rescale4(code, sc / now) & 0xffu;   // (the same for a wave)
+                        r |= code << (8 * e);
+                    }
+                    *at = r;
+                }
+            }
+            if (grown && tid == 0) scales[int64_t(page) * a.c.Hkv + hk] = now;
+        }
         __syncthreads();   // LDS is read
     }
 }
