@@ -143,9 +143,10 @@ __device__ __forceinline__ int value_order(int row) { return (row >> 2) & 3; }
 // eight for each step of the second product, whose 16-byte pieces of a column they are.
 __device__ __forceinline__ int token_of(int i) { return 4 * (i & 4) + ((i >> 1) & 12) + (i & 3); }
 
-// 16 bytes a lane from `base` + its offset to LDS, lane after lane from `to` on; no wait.
+// 16 bytes a lane from `base` + its offset to LDS, lane after lane from `to` on; no wait (but the wait state that M0
+// needs between its write and the load).
 __device__ __forceinline__ void fetch16(const uint8_t* base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                  :
                  : "v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(to))
                  : "memory", "m0");

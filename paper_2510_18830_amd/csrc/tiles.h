@@ -105,9 +105,10 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
 // `src`; lane l's bytes land at LDS byte address `lds` + 16 l (`lds` uniform
 // across the wave).  Written as inline assembly so that the compiler adds no
 // waits of its own before LDS reads of other buffers; the consumer waits with
-// wait_vmem() and publishes the tile with a barrier.
+// wait_vmem() and publishes the tile with a barrier.  One wait state has to lie between
+// a scalar write of M0 and the load that reads it.
 __device__ __forceinline__ void dma16(const void* src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off"
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                  :
                  : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory", "m0");
