@@ -195,18 +195,19 @@ __device__ __forceinline__ int block_sum(int x, int* red) {
     return r;
 }
 // sum over the threads before this one; `all`: over all
-__device__ __forceinline__ int block_before(int x, int* red, int& all) {
-    int inc = x;
+template <class N>
+__device__ __forceinline__ N block_before(N x, N* red, N& all) {
+    N inc = x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(inc, o);
+        const N y = __shfl_up(inc, o);
         if (lane >= o) inc += y;
     }
     __syncthreads();
     if (lane == 63) red[wave] = inc;
     __syncthreads();
-    int before = 0;
+    N before = 0;
     all = 0;
     for (int w = 0; w < int(blockDim.x) / 64; ++w) {
         if (w < wave) before += red[w];
@@ -274,12 +275,13 @@ __global__ void __launch_bounds__(kThreads) fork_rows_kernel(ForkArgs a) {
 constexpr int kListThreads = 1024;
 __global__ void __launch_bounds__(kListThreads) fork_list_kernel(ForkArgs a) {
     __shared__ int red[kListThreads / 64];
+    __shared__ int64_t red64[kListThreads / 64];
     const int tid = threadIdx.x;
-    int64_t total = 0;
+    int64_t total = 0;   // (a row may ask for kMaxWidth pages, so 128 of them for 2^31)
     for (int n0 = 0; n0 < a.N; n0 += kListThreads) {
-        const int n = n0 + tid, x = n < a.N ? a.need[n] : 0;
-        int all;
-        const int before = block_before(x, red, all);
+        const int n = n0 + tid;
+        int64_t all;
+        const int64_t before = block_before(int64_t(n < a.N ? a.need[n] : 0), red64, all);
         if (n < a.N) a.need[n] = int32_t(min(total + before, int64_t(1) << 30));   // (no pool has as many pages)
         total += all;
     }
@@ -363,7 +365,7 @@ __global__ void __launch_bounds__(kThreads) fork_fill_kernel(ForkArgs a) {
         const int i = i0 + tid;
         const bool ask = i < a.c.width && row[i] == kAsked;
         int all;
-        const int at = rank + block_before(ask, red, all);
+        const int at = rank + block_before(int(ask), red, all);
         if (ask) {
             const int p = at < found ? a.list[1 + at] : -1;
             row[i] = p;
@@ -518,7 +520,7 @@ __global__ void __launch_bounds__(kSmallThreads) fork_small_kernel(ForkArgs a, S
         const bool keeps = p >= 0 && (leads || i < w.full);
         const bool ask = i < w.room && !keeps && (p >= 0 || i >= w.held);
         int here;
-        const int at = rank + block_before(ask, red, here);
+        const int at = rank + block_before(int(ask), red, here);
         if (i < a.c.width) a.table_out[int64_t(n) * a.c.width + i] = keeps ? p : ask && at < got ? given[at] : -1;
         rank += here;
     }

@@ -228,6 +228,29 @@ def test_fork_asks_for_2e31_pages(gpu):
     assert missing[0] == width - pages and (missing[1:] == width).all()
 
 
+def test_fork_rows_that_ask_for_2e24_pages_each(gpu):
+    """128 rows of the widest table ask for 2^31 pages, more than 32 bits count in one pass over the rows: the first row gets
+    what there is, the others nothing."""
+    pages, width, N = 50, 2 ** 24, 131
+    print(f"fork N{N} width{width}", flush=True)
+    cache = _pool(1, pages, 1, 64, gpu)
+    table = torch.full((1, width), -1, dtype=I32, device=gpu)
+    table[0, :2] = torch.tensor([7, 3], dtype=I32)
+    refs = torch.zeros(pages, dtype=I32, device=gpu)
+    refs[[3, 7]] = 1
+    lens = torch.tensor([128], dtype=I32, device=gpu)
+    src = torch.full((N,), -1, dtype=I32, device=gpu)
+    src[-1] = 0
+    room = torch.full((N,), 64 * width, dtype=I32, device=gpu)
+    got, lens, refs, missing = ms.cache_fork(cache, table, lens, refs, src, room=room)
+    free = [p for p in range(pages) if p not in (3, 7)]
+    assert got[0, :pages - 2].tolist() == free and all((part == -1).all() for part in got[0, pages - 2:].split(1 << 22))
+    assert all((row == -1).all() for row in got[1:-1])
+    assert got[-1, :2].tolist() == [7, 3] and (got[-1, 2:] == -1).all()
+    assert (refs == 1).all() and lens.tolist() == [0] * (N - 1) + [128]
+    assert missing.tolist() == [width - pages + 2] + [width] * (N - 2) + [width - 2]
+
+
 def test_fork_runs_out_of_pages(gpu):
     """Fewer free pages than are asked for: the first rows get theirs, the others' entries stay -1, a row whose last page
     could not be copied ends with its full pages."""
