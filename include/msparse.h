@@ -618,9 +618,9 @@ MSPARSE_API msparse_status msparse_cache_keep(const msparse_cache* cache, int32_
  * Free pages (those given back among them) are allotted in the order of n and of the places,
  * the lowest page first.  A place for which none is left, and one of tokens that had no page,
  * holds -1; where that is the page to be copied, the sequence ends with its full pages.
- * Outputs: refs_out int32 [pages] (may be refs), table_out int32 [sequences, width] and
- * lens_out int32 [sequences] (neither may share memory with the inputs), missing int32
- * [sequences]: pages that were asked for and not there.
+ * Outputs: refs_out int32 [pages] (may be refs), table_out int32 [sequences, width], lens_out int32
+ * [sequences] and missing int32 [sequences]: pages that were asked for and not there.  They and the
+ * workspace share no memory with the inputs (but refs_out with refs) nor with each other.
  * Equal calls give equal tables.  A call that only frees continues nothing: src = -1. */
 MSPARSE_API size_t msparse_cache_fork_workspace(const msparse_cache* cache, int32_t sequences);
 MSPARSE_API msparse_status msparse_cache_fork(const msparse_cache* cache, int32_t sequences, const int32_t* src,

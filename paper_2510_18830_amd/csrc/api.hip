@@ -1251,6 +1251,36 @@ static size_t carve_cache_fork(const msparse_cache* c, int32_t sequences, char* 
     return w.off;
 }
 
+// What a fork writes shares no memory with what it reads (some workgroups read while others write), nor with each other;
+// the counts alone may be updated in their place.
+static msparse_status check_fork_memory(const msparse_cache* c, int32_t sequences, const int32_t* src,
+                                        const int32_t* room, const int32_t* refs, const int32_t* refs_out,
+                                        const int32_t* table_out, const int32_t* lens_out, const int32_t* missing,
+                                        const void* ws, size_t ws_bytes) {
+    struct Range {
+        const char* name;
+        const void* at;
+        uint64_t bytes;
+    };
+    const uint64_t old = uint64_t(c->batch), n = uint64_t(sequences), width = uint64_t(c->width);
+    const Range written[] = {{"refs_out", refs_out, 4 * uint64_t(c->pages)}, {"page_table_out", table_out, 4 * n * width},
+                             {"lens_out", lens_out, 4 * n}, {"missing", missing, 4 * n}, {"workspace", ws, ws_bytes}};
+    const Range read[] = {{"refs", refs, 4 * uint64_t(c->pages)}, {"page_table", c->page_table, 4 * old * width},
+                          {"lens", c->lens, 4 * old}, {"src", src, 4 * n}, {"room", room, room ? 4 * n : 0}};
+    auto share = [](const Range& x, const Range& y) {
+        const uint64_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+        return a < b + y.bytes && b < a + x.bytes;
+    };
+    for (const Range& w : written) {
+        for (const Range& r : read)
+            if (share(w, r) && !(&w == written && &r == read && refs == refs_out))   // (the counts in their place)
+                return fail(MSPARSE_ERR_INVALID, "%s and %s share memory", w.name, r.name);
+        for (const Range* x = written; x < &w; ++x)
+            if (share(w, *x)) return fail(MSPARSE_ERR_INVALID, "%s and %s share memory", w.name, x->name);
+    }
+    return MSPARSE_OK;
+}
+
 size_t msparse_cache_fork_workspace(const msparse_cache* cache, int32_t sequences) {
     if (check_fork(cache, sequences)) return 0;
     ForkArgs a{};
@@ -1267,12 +1297,12 @@ msparse_status msparse_cache_fork(const msparse_cache* cache, int32_t sequences,
         return fail(MSPARSE_ERR_INVALID, "fork array is NULL");
     if (odd_words({src, room, refs, refs_out, table_out, lens_out, missing}))
         return fail(MSPARSE_ERR_INVALID, "fork array not 4-byte aligned");
-    if (table_out == cache->page_table || lens_out == cache->lens)
-        return fail(MSPARSE_ERR_INVALID, "the new table or lens in the old ones' place");
     if (misaligned({ws})) return fail(MSPARSE_ERR_INVALID, "workspace is not 16-byte aligned");
     ForkArgs a{};
     const size_t need = carve_cache_fork(cache, sequences, static_cast<char*>(ws), &a);
     if (!ws || ws_bytes < need) return fail(MSPARSE_ERR_WORKSPACE, "cache fork workspace %zu < %zu bytes", ws_bytes, need);
+    if ((st = check_fork_memory(cache, sequences, src, room, refs, refs_out, table_out, lens_out, missing, ws, need)))
+        return st;
     a.c = cache_view(cache);
     a.refs = refs;
     a.src = src;

@@ -160,6 +160,30 @@ def test_fork_refuses():
         assert fork(c=_cache(**change)) == status, (change, _message())
 
 
+def test_fork_refuses_shared_memory():
+    """What a call writes shares no word with what it reads or else writes, but refs_out with refs."""
+    L, n = ms.lib(), 3
+    c = _cache(page_table=1 << 16, lens=2 << 16)
+    need = L.msparse_cache_fork_workspace(c, n)
+    at = dict(src=3 << 16, room=4 << 16, refs=5 << 16, refs_out=6 << 16, table=7 << 16, lens=8 << 16, missing=9 << 16, ws=10 << 16)
+    words = dict(src=n, room=n, refs=10, refs_out=10, table=4 * n, lens=n, missing=n, ws=need // 4, page_table=8, old_lens=2)
+    everything = dict(at, page_table=1 << 16, old_lens=2 << 16)
+    names = dict(refs_out="refs_out", table="page_table_out", lens="lens_out", missing="missing", ws="workspace")
+    for out, name in names.items():
+        for other in everything:
+            if other == out:
+                continue
+            for off in (0, 4 * words[other] - 4, 4 - 4 * words[out]):   # the same, its last word, this one's last word
+                if (out, other, off) in (("refs_out", "refs", 0),) or (out == "ws" and off % 16):
+                    continue
+                args = dict(at, **{out: everything[other] + off})
+                assert L.msparse_cache_fork(c, n, *(_p(x) for x in args.values()), need, None) == -1, (out, other, off)
+                assert name in _message() and "share memory" in _message(), (out, other, off, _message())
+    for other in ("src", "room", "lens", "missing"):   # counts in their place, and another array there too
+        args = dict(at, refs=at["refs_out"], **{other: at["refs_out"]})
+        assert L.msparse_cache_fork(c, n, *(_p(x) for x in args.values()), need, None) == -1 and "share" in _message(), other
+
+
 def test_binding_refuses_host_tensors_shapes_and_types():
     bf = torch.bfloat16
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
