@@ -612,9 +612,13 @@ MSPARSE_API msparse_status msparse_cache_keep(const msparse_cache* cache, int32_
  * as the width goes (room NULL: its tokens alone):
  *   - full pages are shared;
  *   - the page that holds the last tokens but is not full, and pages without tokens, stay
- *     with the first n that continues the sequence; the others get a copy of the one and
- *     new pages for the rest, so that no page is shared that a sequence appends to;
+ *     with the first n that continues the sequence, whoever else holds them; the others get
+ *     a copy of the one and new pages for the rest;
  *   - entries that no new sequence keeps are given back.
+ * So the pages that a sequence appends to are its own, if that of the last tokens and those
+ * behind it had one holder (refs 1) before the call.  Where another table, or another row,
+ * holds them as well, the first n shares them with it, and an append to either changes what
+ * both hold: let a second n continue the sequence then, whose copy is its own.
  * Free pages (those given back among them) are allotted in the order of n and of the places,
  * the lowest page first.  A place for which none is left, and one of tokens that had no page,
  * holds -1; where that is the page to be copied, the sequence ends with its full pages.

@@ -263,6 +263,22 @@ def test_fork_runs_out_of_pages(gpu):
             assert got[1].tolist() == [100, 100, 100, 100, 64] and got[3].tolist() == [0, 0, 0, 0, 1]
 
 
+def test_fork_of_a_partly_filled_page_that_another_table_holds(gpu):
+    """The first that continues the sequence shares it as before; the second one's copy is its own, and an append to that
+    leaves the held page as it was."""
+    Hkv, d = 2, 64
+    cache = _pool(4, 6, Hkv, d, gpu, nan=False)
+    got = _fork(gpu, cache, np.array([[4, 2, -1]], np.int32), [100], np.array([0, 0, 2, 0, 2, 0]), [0, 0], [100, 110])
+    assert got[0].tolist() == [[4, 2, -1], [4, 0, -1]] and got[2].tolist() == [1, 0, 2, 0, 3, 0]
+    before = _host(cache)
+    g = torch.Generator().manual_seed(0)
+    k = (torch.randn((1, Hkv, 10, d), generator=g) * 1000).to(BF).to(gpu)
+    ms.cache_append(cache, _dev(got[0][1:], gpu), _dev(np.array([100]), gpu), k, k)
+    after = _host(cache)
+    for x, y in zip(before, after):
+        assert not np.array_equal(x[0], y[0]) and np.array_equal(x[1:], y[1:])
+
+
 def test_fork_frees_and_reuses(gpu):
     """Sequences that nothing continues give their pages back, and the same call allots them again; all freed at the end;
     entries and lengths out of range."""

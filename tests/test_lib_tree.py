@@ -269,3 +269,6 @@ def test_oracle_fork_by_hand():
     assert got[0].tolist() == [[4, 2, 6, 5], [4, 7, -1, -1], [1, 3, -1, -1], [-1] * 4]
     assert got[1].tolist() == [100, 100, 128, 0] and got[3].tolist() == [0, 0, 2, 1]
     assert got[2].tolist() == [1, 1, 2, 1, 2, 1, 1, 1] and got[4] == [(2, 7)]
+    # pages that another table holds too: the partly filled one stays with the first, the second one's copy is its own
+    got = OP.fork(np.array([[4, 2, -1]]), [100], np.array([0, 0, 2, 0, 2, 0]), [0, 0], None, 6)
+    assert got[0].tolist() == [[4, 2, -1], [4, 0, -1]] and got[2].tolist() == [1, 0, 2, 0, 3, 0] and got[4] == [(2, 0)]
