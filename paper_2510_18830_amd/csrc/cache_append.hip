@@ -127,16 +127,7 @@ cache_append_kernel(AppendArgs a) {
                 if (mine[u]) {
                     if (AT || a.freq) {
                         const int at = (x0 + u * kThreads) / QC * H2 + 8 * c;
-                        float x1[8], x2[8];
-                        unpack8(l[u], x1);
-                        unpack8(r[u], x2);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) rotate(x1[j], x2[j], cosv[at + j], sinv[at + j]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            l[u][j] = pack_bf16x2(x1[2 * j], x1[2 * j + 1]);
-                            r[u][j] = pack_bf16x2(x2[2 * j], x2[2 * j + 1]);
-                        }
+                        rotate8<AT>(l[u], r[u], cosv + at, sinv + at);
                     }
                     uint16_t* w = dst + (share + shares * k) * a.qos[1] + to[u];
                     __builtin_nontemporal_store(l[u], reinterpret_cast<u32x4*>(w));
@@ -196,7 +187,13 @@ cache_append_kernel(AppendArgs a) {
                 const f32x4 cs = *reinterpret_cast<const f32x4*>(cosv + t * H2 + 4 * c);
                 const f32x4 sn = *reinterpret_cast<const f32x4*>(sinv + t * H2 + 4 * c);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) rotate(kx[n][j], kx[n][4 + j], cs[j], sn[j]);
+                for (int j = 0; j < 4; ++j) {
+                    float x1 = kx[n][j], x2 = kx[n][4 + j];
+                    rotate(x1, x2, cs[j], sn[j]);
+                    if (AT && stays(sn[j])) continue;
+                    kx[n][j] = x1;
+                    kx[n][4 + j] = x2;
+                }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {

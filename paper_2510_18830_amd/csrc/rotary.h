@@ -69,10 +69,32 @@ __device__ __forceinline__ void unpack8(const u32x4& w, float* x) {
     }
 }
 
-// of pair i of token `t` of the call
+// In the place of a pair's sine: the pair stays as it is, bit for bit.  (The angle 0 would do for finite values only:
+// an infinity or a NaN of one column times the sine 0 makes the other one NaN, and -0 + 0 is +0.)
+constexpr float kStays = 2.f;
+__device__ __forceinline__ bool stays(float s) { return fabsf(s) == kStays; }
+
+// Eight pairs of bf16, rounded once.  AXES: some may stay.
+template <bool AXES>
+__device__ __forceinline__ void rotate8(u32x4& w1, u32x4& w2, const float* c, const float* s) {
+    float x1[8], x2[8];
+    unpack8(w1, x1);
+    unpack8(w2, x2);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) rotate(x1[j], x2[j], c[j], s[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t r1 = pack_bf16x2(x1[2 * j], x1[2 * j + 1]), r2 = pack_bf16x2(x2[2 * j], x2[2 * j + 1]);
+        const uint32_t keep = !AXES ? 0 : (stays(s[2 * j]) ? 0xffffu : 0) | (stays(s[2 * j + 1]) ? 0xffff0000u : 0);
+        w1[j] = (w1[j] & keep) | (r1 & ~keep);
+        w2[j] = (w2[j] & keep) | (r2 & ~keep);
+    }
+}
+
+// of pair i of token `t` of the call; the sine is kStays where it has no axis
 __device__ __forceinline__ Turn turn_at(const Positions& p, int i, int64_t t) {
     const int axis = p.axis ? p.axis[i] : 0;
-    if (uint32_t(axis) >= uint32_t(p.axes)) return Turn{1.0, 0.0};
+    if (uint32_t(axis) >= uint32_t(p.axes)) return Turn{1.0, double(kStays)};
     return turn_by(double(p.at[axis * p.tokens + t]), p.freq[i]);
 }
 

@@ -28,41 +28,36 @@ struct Row8<uint16_t> {
     __device__ __forceinline__ void load(const uint16_t* p) {
         w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
     }
-    __device__ __forceinline__ void get(float* x) const { unpack8(w, x); }
-    __device__ __forceinline__ void put(const float* x) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
-    }
     __device__ __forceinline__ void store(uint16_t* p) const {
         __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
     }
 };
 template <>
 struct Row8<float> {
-    f32x4 lo, hi;
+    f32x4 w[2];
     __device__ __forceinline__ void load(const float* p) {
-        lo = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
-        hi = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + 4));
-    }
-    __device__ __forceinline__ void get(float* x) const {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x[j] = lo[j];
-            x[4 + j] = hi[j];
-        }
-    }
-    __device__ __forceinline__ void put(const float* x) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            lo[j] = x[j];
-            hi[j] = x[4 + j];
-        }
+        w[0] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+        w[1] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + 4));
     }
     __device__ __forceinline__ void store(float* p) const {
-        __builtin_nontemporal_store(lo, reinterpret_cast<f32x4*>(p));
-        __builtin_nontemporal_store(hi, reinterpret_cast<f32x4*>(p + 4));
+        __builtin_nontemporal_store(w[0], reinterpret_cast<f32x4*>(p));
+        __builtin_nontemporal_store(w[1], reinterpret_cast<f32x4*>(p + 4));
     }
 };
+__device__ __forceinline__ void turn(Row8<uint16_t>& r1, Row8<uint16_t>& r2, const float* c, const float* s) {
+    rotate8<true>(r1.w, r2.w, c, s);
+}
+__device__ __forceinline__ void turn(Row8<float>& r1, Row8<float>& r2, const float* c, const float* s) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float x1 = r1.w[j >> 2][j & 3], x2 = r2.w[j >> 2][j & 3];
+        rotate(x1, x2, c[j], s[j]);
+        if (!stays(s[j])) {
+            r1.w[j >> 2][j & 3] = x1;
+            r2.w[j >> 2][j & 3] = x2;
+        }
+    }
+}
 
 template <int D, class T>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(RotateArgs a) {
@@ -106,13 +101,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(RotateArgs a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (!to[u]) continue;
-            float x1[8], x2[8];
-            r1[u].get(x1);
-            r2[u].get(x2);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) rotate(x1[j], x2[j], cosv[at[u] + j], sinv[at[u] + j]);
-            r1[u].put(x1);
-            r2[u].put(x2);
+            turn(r1[u], r2[u], cosv + at[u], sinv + at[u]);
             r1[u].store(to[u]);
             r2[u].store(to[u] + H2);
         }

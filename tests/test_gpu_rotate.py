@@ -86,6 +86,39 @@ def test_rotate_a_part_of_the_columns_and_far_positions(gpu):
     assert torch.equal(qo[..., left], q[..., left])
 
 
+def _any_bits(seed, shape, gpu, dtype):
+    """Any bit patterns: infinities, NaNs of both kinds, zeros of both signs, subnormal values."""
+    g = torch.Generator().manual_seed(seed)
+    n, whole = (16, torch.int16) if dtype == BF else (32, torch.int32)
+    x = torch.randint(-2 ** (n - 1), 2 ** (n - 1), shape, generator=g, dtype=torch.int64)
+    some = torch.tensor([0, -2 ** (n - 1), 0x7f80, 0x7fc0, 0x7f81, -0x80, 1], dtype=torch.int64)
+    some[2:6] <<= n - 16   # the infinities, a quiet and a signalling NaN
+    pick = torch.randint(0, 20, shape, generator=g)
+    x = torch.where(pick < 7, some[pick.clamp(max=6)], x)
+    return x.to(whole).view(dtype).to(gpu)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_pairs_outside_the_axes_keep_their_bits(gpu, d, dtype, inverse):
+    N, axes = 130, 2
+    whole = torch.int16 if dtype == BF else torch.int32
+    g = torch.Generator().manual_seed(d)
+    axis = torch.randint(-2, 4, (d // 2,), generator=g, dtype=torch.int32)
+    left = torch.cat([(axis < 0) | (axis >= axes)] * 2).to(gpu)
+    q, k = (torch.where(left, _any_bits(i, (2, h, N, d), gpu, dtype).view(whole),
+                        _randn(i, (2, h, N, d), gpu, dtype).view(whole)).view(dtype) for i, h in ((1, 3), (2, 1)))
+    pos, freq = _positions(3, axes, 2, N, 70000, gpu), _freq(d, gpu)
+    got = ms.rotate(q, k, pos, freq, axis=axis.to(gpu), inverse=inverse)
+    for y, x in zip(got, (q, k)):
+        assert torch.equal(y[..., left].view(whole), x[..., left].view(whole))
+        z = torch.where(left, torch.zeros_like(x), x)
+        _check(torch.where(left, torch.zeros_like(y), y), z, pos.cpu().numpy(), freq.cpu().numpy(), axis.numpy(), inverse)
+    same = ms.rotate(q, k, pos, freq, axis=torch.full_like(axis, axes).to(gpu), inverse=inverse, q_out=q.clone())
+    assert torch.equal(same[0].view(whole), q.view(whole)) and torch.equal(same[1].view(whole), k.view(whole))
+
+
 def test_rotate_strides_in_place_and_one_axis(gpu):
     B, Hq, Hkv, N, d = 2, 4, 2, 70, 64
     q, k = _randn(1, (B, N, Hq, d), gpu).transpose(1, 2), _randn(2, (B, Hkv, N, d + 16), gpu)[..., :d]
@@ -238,3 +271,32 @@ def test_append_at_one_axis_is_append(gpu):
     assert torch.equal(c0.v.view(torch.uint8), c1.v.view(torch.uint8)) and torch.equal(c0.v_scale, c1.v_scale)
     assert torch.equal(c0.k_scale, c1.k_scale)
     assert (c0.k.view(torch.uint8) != c1.k.view(torch.uint8)).float().mean() <= 1e-3
+
+
+@pytest.mark.parametrize("d,T", [(64, 5), (128, 100)])
+def test_append_leaves_pairs_outside_the_axes(gpu, d, T):
+    """Queries keep their bits there; of keys an element that is not finite has the code NaN, and its partner its own."""
+    Hq, Hkv = 4, 2
+    axis = (torch.arange(d // 2, dtype=torch.int32) % 3 - 1).to(gpu)
+    left = torch.cat([axis < 0] * 2)
+    q = torch.where(left, _any_bits(1, (1, Hq, T, d), gpu, BF).view(torch.int16), _randn(1, (1, Hq, T, d), gpu).view(torch.int16))
+    k = _randn(2, (1, Hkv, T, d), gpu)
+    k[0, 0, 1::7, 0], k[0, 1, ::5, d // 2 + 3], k[0, 1, 3, 6] = float("inf"), float("nan"), -float("inf")
+    odd = torch.where(left, ~k.isfinite(), False)
+    assert odd.any() and k[..., ~left].isfinite().all()
+    pages = (T + 63) // 64
+    table = torch.arange(pages, dtype=torch.int32, device=gpu)[None]
+    pos, freq = _positions(3, 2, 1, T, 70000, gpu), _freq(d, gpu)
+    lens = torch.zeros(1, dtype=torch.int32, device=gpu)
+    both = []
+    for keys in (k, torch.where(odd, torch.zeros_like(k), k)):
+        c = ms.make_cache(pages, Hkv, d, gpu)
+        for t in (c.k, c.v, c.k_scale, c.v_scale):
+            t.view(torch.uint8).zero_()
+        got = ms.cache_append(c, table, lens, keys, keys, q=q.view(BF), inv_freq=freq, positions=pos, axis=axis)
+        assert torch.equal(got[..., left].view(torch.int16), q[..., left])
+        code = c.k.view(torch.uint8).permute(1, 0, 2, 3).reshape(1, Hkv, -1, d)[:, :, :T]
+        both.append((code, c.k_scale))
+    (code, scale), (want, wanted) = both
+    assert torch.equal(scale, wanted)
+    assert (code[odd] & 127 == 127).all() and torch.equal(code[~odd], want[~odd])
