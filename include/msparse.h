@@ -579,7 +579,9 @@ MSPARSE_API msparse_status msparse_tree_mask(int32_t batch, int32_t tokens, cons
  * msparse_window_fwd at positions[b, t] sees, and the nodes u < counts[b] of its bits of seen
  * (any, not only a tree's), where they have a page.  positions is read with a window only (NULL without; values outside
  * the nodes' places count as the nearest of them).  A row behind the counts, or without a
- * key, gets out = 0 and lse = -inf.  All else as msparse_cache_attn. */
+ * key, gets out = 0 and lse = -inf.  All else as msparse_cache_attn: codes of tokens that no row
+ * of the call sees (pruned nodes among them) may hold anything, and so may the scales of pages
+ * that hold none but such. */
 MSPARSE_API size_t msparse_cache_tree_attn_workspace(const msparse_cache* cache, int32_t heads_q, int32_t tokens);
 MSPARSE_API msparse_status msparse_cache_tree_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens,
                                                    int32_t window, int32_t sinks, float scale,

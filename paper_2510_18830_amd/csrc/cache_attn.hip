@@ -84,8 +84,8 @@ __global__ void __launch_bounds__(64 * WAVES)
                 [&] {
                     if (i + 1 < n) load_k(next);
                 },
-                [&](int t0) {
-                    const u32x4 keep = seen_bytes(t0, st.wp1, st.far, a.S, lane);
+                [&](int t0, uint32_t seen) {
+                    const u32x4 keep = TREE ? bytes_of(seen) : seen_bytes(t0, st.wp1, st.far, a.S, lane);
 #pragma unroll
                     for (int y = 0; y < ND; ++y) vr[y] &= keep;
                 });
@@ -193,7 +193,7 @@ cache_attn_rows_kernel(CacheAttnArgs a) {
                 page_step<D, RT, 1, 2, 2, false>(
                     a, st, t0, lane_value(pages.ks, i), lane_value(pages.vs, i), a.W, a.S, lane,
                     [&](int t, int j, int p) { return cur[t * KL + j][p][lane]; },
-                    [&](int y, int p) { return cur[4 * KL + y][p][lane]; }, [] {}, [](int) {});
+                    [&](int y, int p) { return cur[4 * KL + y][p][lane]; }, [] {}, [](int, uint32_t) {});
             __builtin_amdgcn_sched_barrier(0);
             __syncthreads();
         }

@@ -112,23 +112,82 @@ __device__ __forceinline__ int node_of(const CacheAttnArgs& a, const Walk& k, in
     return r < a.T * G && t < k.tr.len - k.tr.base ? k.b * a.T + t : -1;
 }
 __device__ __forceinline__ uint64_t below64(int n) { return n >= 64 ? ~0ull : (uint64_t(1) << max(n, 0)) - 1; }
-// Which of the 64 tokens from slot j on row r sees: of the context what its position does (without a window
-// that says nothing but that the row is behind it), of the nodes those of its bits.
-__device__ __forceinline__ uint64_t row_sees(const CacheAttnArgs& a, int r, int j, const Walk& k) {
-    const int node = node_of(a, k, r), base = k.tr.base, len = k.tr.len;
-    if (node < 0) return 0;
+// Which of the 64 tokens from slot j on a row at position pos (of the nodes' places) sees: of the context what its
+// position does (without a window all of it), of the nodes those of its bits, word(x) for x >= 0.
+template <class Word>
+__device__ __forceinline__ uint64_t tokens_seen(const CacheAttnArgs& a, const Walk& k, int pos, int j, Word word) {
+    const int base = k.tr.base, len = k.tr.len;
     uint64_t bits = 0;
     if (j < len && j + 63 >= base) {
         const int u = j - base, w = u >> 5;   // (u > -64: the words before the first are empty)
-        const int32_t* row = a.seen + int64_t(node) * a.words;
-        auto word = [&](int x) { return x >= 0 && x < a.words ? uint64_t(uint32_t(row[x])) : 0; };
-        bits = (word(w) | (word(w + 1) << 32)) >> (u & 31);
-        if (u & 31) bits |= word(w + 2) << (64 - (u & 31));
+        auto at = [&](int x) { return x >= 0 && x < a.words ? uint64_t(uint32_t(word(x))) : 0; };
+        bits = (at(w) | (at(w + 1) << 32)) >> (u & 31);
+        if (u & 31) bits |= at(w + 2) << (64 - (u & 31));
         bits &= below64(len - j);
     }
-    const int pos = max(min(a.at ? a.at[node] : base, len - 1), base);
     const uint64_t context = below64(base - j);
     return (bits & ~context) | (context & (~below64(max(pos - a.W + 1, 0) - j) | below64(min(a.S - 1, pos) + 1 - j)));
+}
+__device__ __forceinline__ int position_of(const CacheAttnArgs& a, const Walk& k, int node) {
+    return max(min(a.at ? a.at[node] : k.tr.base, k.tr.len - 1), k.tr.base);
+}
+__device__ __forceinline__ uint64_t row_sees(const CacheAttnArgs& a, int r, int j, const Walk& k) {
+    const int node = node_of(a, k, r);
+    if (node < 0) return 0;
+    const int32_t* row = a.seen + int64_t(node) * a.words;
+    return tokens_seen(a, k, position_of(a, k, node), j, [&](int x) { return row[x]; });
+}
+// What a tile's rows see, all of them together: the nodes' words, and the first of their positions, which sees the most
+// of the context.
+struct TileSeen {
+    uint32_t words[kMaxNodes / 32];
+    int32_t pos;
+};
+__device__ __forceinline__ void clear_seen(TileSeen& s) {
+    if (threadIdx.x < kMaxNodes / 32) s.words[threadIdx.x] = 0;
+    if (threadIdx.x == 0) s.pos = INT32_MAX;
+}
+// A thread's position and the first of its words are asked for at once, and entered with the others when the memory is
+// clear.
+struct SeenItems {
+    const int32_t* words;
+    int32_t nodes, items;   // of the tile; their words
+    uint32_t word[2];
+    int32_t pos;
+};
+template <int N>
+__device__ __forceinline__ void ask_words(const SeenItems& x, int y0, uint32_t (&w)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] = y0 + e * kThreads < x.items ? uint32_t(x.words[y0 + e * kThreads]) : 0;
+}
+template <int N>
+__device__ __forceinline__ void enter_words(const CacheAttnArgs& a, int y0, const uint32_t (&w)[N], TileSeen& s) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (w[e]) atomicOr(s.words + (y0 + e * kThreads) % a.words, w[e]);
+}
+__device__ __forceinline__ SeenItems ask_seen(const CacheAttnArgs& a, const Walk& k, int rows) {
+    const int G = a.Hq / a.c.Hkv, t0 = k.tr.r0 / G, t1 = min((k.tr.r0 + rows - 1) / G, k.tr.len - k.tr.base - 1);
+    const int node = k.b * a.T + t0;
+    SeenItems x{};
+    x.nodes = t1 - t0 + 1;
+    x.items = x.nodes * a.words;
+    x.words = a.seen + int64_t(node) * a.words;
+    ask_words(x, threadIdx.x, x.word);
+    x.pos = int(threadIdx.x) < x.nodes ? position_of(a, k, node + threadIdx.x) : INT32_MAX;
+    return x;
+}
+__device__ __forceinline__ void enter_seen(const CacheAttnArgs& a, const SeenItems& x, TileSeen& s) {
+    enter_words(a, threadIdx.x, x.word, s);
+    if (int(threadIdx.x) < x.nodes) atomicMin(&s.pos, x.pos);
+    for (int y0 = threadIdx.x + 2 * kThreads; y0 < x.items; y0 += 8 * kThreads) {
+        uint32_t w[8];
+        ask_words(x, y0, w);
+        enter_words(a, y0, w, s);
+    }
+}
+__device__ __forceinline__ uint64_t tile_sees(const CacheAttnArgs& a, const Walk& k, int j, const TileSeen& s) {
+    return tokens_seen(a, k, s.pos, j, [&](int x) { return s.words[x]; });
 }
 
 // Where the codes of a page lie in LDS: as in memory, rows of a token's D columns (keys) or a column's 64 tokens (values),
@@ -473,7 +532,7 @@ struct TreeMemory {
     uint8_t k[kDepth][kPage * D], v[kDepth][kPage * D];
 };
 template <int D, bool SPLIT>
-__device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k, TreeMemory<D>& mem) {
+__device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k, TreeMemory<D>& mem, TileSeen& all) {
     constexpr int NF = D / 64;          // pieces of 16 bytes of a page's keys, and of its values, per thread
     constexpr int kBytes = kPage * D;   // of either
     const int tid = threadIdx.x, lane = tid & 63;
@@ -491,8 +550,8 @@ __device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k,
     const int kf = 16 * tid / D, vf = tid / 4, piece = (tid & 3) ^ value_order(vf);
     const uint32_t from_k = kf * D + 16 * ((tid % (D / 16)) ^ key_order<D>(kf)), from_v = kPage * vf + 16 * piece;
     const uint32_t lds_k = lds_addr(mem.k) + 1024 * w, lds_v = lds_addr(mem.v) + 1024 * w;
-    // what all rows see in full ends before the first node; what none sees lies before `far`
-    const int base = k.tr.base, len = k.tr.len, far = base - a.W;
+    // what all rows see in full ends before the first node
+    const int base = k.tr.base, len = k.tr.len;
     auto in_part = [&](int t0) { return partly(t0, base - 1, len - 1, a.W, a.S); };
     const int n = k.c1 - k.c0;
     if (n > 0) {
@@ -501,14 +560,33 @@ __device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k,
         ValueScale scales;
         uint32_t off_lo, off_hi;   // where a page's codes lie
         int x0 = 0;
+        // Which tokens of this lane's page some row sees.  (The scale of a page without one may be anything: 1 in its place.)
+        uint32_t seen_lo, seen_hi;
+        auto mark_pages = [&] {
+            const int start = page_start(pages.page, k.pl.page(k.c0 + x0 + lane));
+            seen_lo = seen_hi = ~0u;
+            if (!__any(in_part(start))) return;
+            keep_branch();
+            if (!in_part(start)) return;
+            const uint64_t sees = tile_sees(a, k, start, all);
+            seen_lo = uint32_t(sees);
+            seen_hi = uint32_t(sees >> 32);
+            if (sees == 0) scales = ValueScale{1.f, 0.f, 1.f};
+        };
         auto look = [&](int x) {
             x0 = x;
             pages = look_up(a, k, k.c0 + x, 1, lane);
             scales = value_scale(pages.vs);
+            if (x > 0) mark_pages();
             const uint64_t off = (uint64_t(max(pages.page, 0)) * a.c.Hkv + k.hk) * kBytes;
             off_lo = uint32_t(off);
             off_hi = uint32_t(off >> 32);
         };
+        clear_seen(all);
+        // (without a window the pages that some row does not see in full are the last)
+        const bool masked = a.at || in_part(kPage * k.pl.page(k.c1 - 1));
+        SeenItems asked{};
+        if (masked) asked = ask_seen(a, k, tree_rows(SPLIT));
         look(0);
         // (past the last page as many, of 16 bytes of the pool's first page, so that a step's wait counts the same)
         auto fetch = [&](const uint8_t* codes, uint32_t from, uint32_t to, int i, int slot) {
@@ -519,6 +597,7 @@ __device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k,
                 fetch16(codes + off + 4096 * j, i < n ? from : 0, to + kBytes * slot + 4096 * j);
         };
         __syncthreads();   // the tile before has been read
+        if (masked) enter_seen(a, asked, all);
         // Step i: the weights of page i, the logits of the tokens after them and the product of those before with their
         // values.  It reads the keys of pages i (SPLIT: no more) and i + 1 and the values of pages i - 1 and i (SPLIT: not
         // yet), and asks for the keys of page i + kAheadK and the values of page i + kDepth - 2.
@@ -536,6 +615,7 @@ __device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k,
         wait_fetched<SPLIT ? kLeft : kLeft + 2 * NF>();
         __syncthreads();
         TreeLogits cur = tree_first(st, mem.k[0], kat);
+        mark_pages();
         TreeHalf left{};   // (no weights yet: 0)
         int kslot = 0, vslot = kDepth - 1;   // of page i's keys, page i - 1's values
         auto after = [](int slot) { return slot == kDepth - 1 ? 0 : slot + 1; };
@@ -544,34 +624,29 @@ __device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k,
         auto start_of = [&](int i) {
             return __builtin_amdgcn_readfirstlane(page_start(page_at(pages, i - x0), k.pl.page(k.c0 + i)));
         };
-        // The values at `slot`, of a page that begins at t0, are there: codes of tokens that no row sees may stand for
+        auto seen_of = [&](int i) {
+            return uint32_t(__builtin_amdgcn_readlane(seen_lo, i - x0)) |
+                   uint64_t(uint32_t(__builtin_amdgcn_readlane(seen_hi, i - x0))) << 32;
+        };
+        // The values at `slot`, of a page of which some row sees these tokens, are there: codes of the others may stand for
         // anything, NaN among it, which a weight of 0 would not remove; each thread clears those that it has fetched.
-        auto enter = [&](int slot, int t0) {
+        auto enter = [&](int slot, uint64_t sees) {
             wait_fetched<kLeft>();
-            if (t0 >= 0 && in_part(t0)) {
+            if (~sees) {
                 keep_branch();
-                const int lim = min(a.S, len), x0 = t0 + 16 * (opaque(tid) & 3 ^ value_order(opaque(tid) / 4));
-                u32x4 keep;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    keep[j] = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int x = x0 + 4 * j + e;
-                        if (x < len && (x > far || x < lim)) keep[j] |= 0xffu << (8 * e);
-                    }
-                }
+                const u32x4 keep = bytes_of(uint32_t(sees >> (16 * (opaque(tid) & 3 ^ value_order(opaque(tid) / 4)))));
 #pragma unroll
                 for (int j = 0; j < NF; ++j) *reinterpret_cast<u32x4*>(mem.v[slot] + 16 * tid + 4096 * j) &= keep;
             }
             __syncthreads();
         };
-        int start0 = -1;   // of page i - 1
+        uint64_t sees0 = ~0ull;   // of page i - 1
         for (int i = 0; i < n; ++i) {
             if (i - x0 >= kLooks) look(i);
             const int start = start_of(i);
-            if constexpr (SPLIT) enter(vslot, start0);
-            else enter(after(vslot), start);
+            const uint64_t sees = seen_of(i);
+            if constexpr (SPLIT) enter(vslot, sees0);
+            else enter(after(vslot), sees);
             // Of two waves that could issue the older one does: of a CU's workgroups the second then lags behind the first
             // and works alone in the end.  It leads every other page (128 rows, contexts of 16K: 131 -> 127 us).
             if (blockIdx.x & 256) {
@@ -603,11 +678,11 @@ __device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Walk& k,
                 }
             }
             power = now;
-            start0 = start;
+            sees0 = sees;
             kslot = after(kslot);
             vslot = after(vslot);
         }
-        if constexpr (SPLIT) enter(vslot, start0);
+        if constexpr (SPLIT) enter(vslot, sees0);
         if (live) tree_flush(st, left, mem.v[vslot] + (SPLIT ? vat : vat1), power);
         wait_fetched<0>();
         if constexpr (SPLIT) {
@@ -622,6 +697,7 @@ template <int D, bool SPLIT>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3, D == 128 ? 2 : 3)))
 tree_rows_kernel(CacheAttnArgs a) {
     __shared__ __attribute__((aligned(16))) TreeMemory<D> mem;
+    __shared__ TileSeen all;
     constexpr int kRows = tree_rows(SPLIT);
     const int lane = threadIdx.x & 63;
     Walk k;
@@ -633,7 +709,7 @@ tree_rows_kernel(CacheAttnArgs a) {
     }
     do {
         make_uniform(k);
-        tree_tile<D, SPLIT>(a, k, mem);
+        tree_tile<D, SPLIT>(a, k, mem, all);
     } while (a.items > 0 && next_tile(a, kRows, share, k));
 }
 

@@ -29,6 +29,21 @@ __device__ __forceinline__ u32x4 codes_to_bf16(uint32_t lo, uint32_t hi, float p
     r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true));
     return r;
 }
+// 16 bits as bytes: 0xff where a bit is set
+__device__ __forceinline__ u32x4 bytes_of(uint32_t bits) {
+    u32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = (((bits >> (4 * j)) & 15) * 0x00204081u & 0x01010101u) * 0xffu;
+    return r;
+}
+// x or-ed over the 16 lanes of a quarter of the wave
+__device__ __forceinline__ uint32_t quarter_or(uint32_t x) {
+    x |= __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, false);   // the lane 1, 2, 4, 8 before, around
+    x |= __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, false);
+    x |= __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, false);
+    x |= __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, false);
+    return x;
+}
 // x combined over the four lanes of a row (l, l ^ 16, l ^ 32, l ^ 48)
 __device__ __forceinline__ float row_max(float x) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -285,8 +300,9 @@ __device__ __forceinline__ u32x4 operand(const u32x4* x, int p) {
 
 // One page, its first token at position t0: key(t, j, p) and value(y, p) give this lane's
 // operands, 16 codes (PARTS 1) or their halves as bf16 (2); keys_done() runs once the
-// keys are used up, and clear(t0) before the values of a page are that some row does not
-// see in full: it clears the codes of the tokens that no row sees.
+// keys are used up, and clear(t0, seen) before the values of a page are that some row does not
+// see in full: it clears the codes of the tokens that no row sees (TREE: this lane's 16 are
+// given as bits; else they follow from t0).
 template <int D, int RT, int TS, int YS, int PARTS, bool TREE, class Key, class Value, class Done, class Clear>
 __device__ __forceinline__ void page_step(const CacheAttnArgs& a, CacheRows<D, RT>& st, int t0, float kscale,
                                           float vscale, int W, int S, int lane, Key key, Value value, Done keys_done,
@@ -333,6 +349,7 @@ __device__ __forceinline__ void page_step(const CacheAttnArgs& a, CacheRows<D, R
     __builtin_amdgcn_sched_barrier(0);
     if (part) {
         keep_branch();
+        uint32_t some = 0;
 #pragma unroll
         for (int x = 0; x < RT; ++x) {
             if constexpr (TREE) {
@@ -342,6 +359,7 @@ __device__ __forceinline__ void page_step(const CacheAttnArgs& a, CacheRows<D, R
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (!((sees >> e) & 1)) s[x][e >> 2][e & 3] = -INFINITY;
+                some |= sees;
                 continue;
             }
             const int lim = min(S - 1, st.pos[x]);
@@ -353,7 +371,11 @@ __device__ __forceinline__ void page_step(const CacheAttnArgs& a, CacheRows<D, R
                     if (!(uint32_t(st.pos[x] - j) < uint32_t(W) || j <= lim)) s[x][t][r] = -INFINITY;
                 }
         }
-        clear(t0);
+        if constexpr (TREE) {
+            some = quarter_or(some);
+            if (!__any(some)) vscale = 0.f;   // (a page that no row sees a token of: its scale may be anything too)
+        }
+        clear(t0, some);
     }
     // ---- softmax
     u32x4 pb[RT][2];

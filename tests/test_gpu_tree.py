@@ -327,6 +327,64 @@ def test_nan_outside_the_window_and_behind_the_nodes(gpu, d, T, W, S):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def _unseen(sees, at, contexts, counts, W, S):
+    """Of each sequence: which of its slots no node sees."""
+    out = []
+    for b, (n, m) in enumerate(zip(contexts, counts)):
+        j = np.arange(n)
+        p = np.clip(at[b, :m], n, n + m - 1)[:, None]
+        context = (p - j < W) | (j < S) if W else np.ones((m, n), bool)
+        out.append(~np.concatenate([context.any(0), sees[b, :m, :m].any(0)]) if m else np.ones(n, bool))
+    return out
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,T,contexts,counts,W,S,late", [
+    (2, 2, 64, 1, [65], None, 1, 0, False), (8, 2, 64, 4, [500, 90, 62], [4, 3, 2], 0, 0, False),
+    (8, 2, 128, 3, [63, 300], None, 0, 0, False), (4, 2, 64, 16, [500, 64], None, 30, 3, True),
+    (2, 2, 128, 30, [500, 200], None, 77, 0, True), (4, 4, 64, 30, [500, 564], [30, 29], 77, 5, True),
+    (8, 2, 64, 14, [200, 513, 40], [14, 12, 1], 0, 0, False), (8, 2, 128, 14, [500, 120], None, 70, 0, True),
+    (8, 2, 64, 45, [130, 500], None, 60, 2, True), (8, 2, 128, 45, [130, 500], [45, 40], 0, 0, False),
+    (2, 2, 64, 200, [70, 500], [200, 190], 0, 0, False), (2, 2, 128, 200, [640, 30], None, 100, 70, True),
+    (1, 1, 64, 1024, [30], None, 0, 0, False), (16, 2, 128, 130, [300], None, 140, 0, True),
+])
+def test_tokens_that_no_node_sees_may_hold_anything(gpu, Hq, Hkv, d, T, contexts, counts, W, S, late):
+    """Pruned nodes, and the context between what the window reaches from the first place and from the first position given:
+    codes NaN, and scales that are no numbers of pages where that is all."""
+    print(f"unseen Hq{Hq} Hkv{Hkv} d{d} T{T} {contexts} {counts} W{W} S{S}", flush=True)
+    B, live = len(contexts), counts or [T] * len(contexts)
+    rng = np.random.default_rng(T + d)
+    at, sees = _masks(_parents(6, B, T), contexts, counts, W, S)
+    gone = rng.random((B, T)) < 0.4
+    gone[:, T // 3:T // 3 + 130] = T > 64   # whole pages of them
+    gone[:, 0] = True
+    sees &= ~gone[:, None, :]
+    if late:
+        at = np.array(contexts)[:, None] + np.array(live)[:, None] - 1 - rng.integers(0, 2, (B, T))
+    cache, table, L = _filled(14, contexts, T, Hkv, d, gpu, counts)
+    q = _randn(2, (B, Hq, T, d), gpu)
+    cnt = None if counts is None else _dev(np.array(counts), gpu)
+    args = dict(positions=_dev(at, gpu), counts=cnt, window=W, sinks=S)
+    want = ms.cache_tree_attn(cache, table, L, q, _dev(OT.words(sees), gpu), **args)
+    torch.cuda.synchronize()
+    _check(q, *want, cache, table, L, sees, at, counts, W, S)
+    odd = [float("nan"), float("inf"), -float("inf"), -1.0]
+    planted = 0
+    for b, none in enumerate(_unseen(sees, at, contexts, live, W, S)):
+        slots = np.flatnonzero(none)
+        planted += len(slots)
+        pages = _dev(table[b].cpu().numpy()[slots // 64], gpu).long()
+        where = _dev(slots % 64, gpu).long()
+        cache.k.view(torch.uint8)[pages, :, where] = 0x7f
+        cache.v.view(torch.uint8)[pages, :, :, where] = 0xff
+        for lp in range((len(none) + 63) // 64):
+            if none[64 * lp:64 * lp + 64].all():
+                cache.k_scale[int(table[b, lp])] = odd[lp % 4]
+                cache.v_scale[int(table[b, lp])] = odd[(lp + 1) % 4]
+    assert planted
+    got = ms.cache_tree_attn(cache, table, L, q, _dev(OT.words(sees), gpu), **args)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("T", [24, 7, 70])
 def test_magnitudes_of_queries_and_scales(gpu, T, d):
