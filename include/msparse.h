@@ -476,7 +476,9 @@ MSPARSE_API msparse_status msparse_rotate(int32_t batch, int32_t tokens, int32_t
 /* Paged 8-bit cache of keys and values, for decoding after a prefill.  A page
  * holds 64 tokens of every KV head as e4m3 codes (OCP float8, 4 exponent and 3
  * mantissa bits), with an fp32 scale per page and head for keys and one for
- * values: value = code * scale.  All memory is the caller's:
+ * values: value = code * scale.  Scales of tokens that a call sees are finite and above
+ * zero (an append writes powers of two), else its results are undefined.  All memory is the
+ * caller's:
  *   k        e4m3 [pages, heads_kv, 64, head_dim]
  *   v        e4m3 [pages, heads_kv, head_dim, 64]   (tokens contiguous)
  *   k_scale, v_scale  fp32 [pages, heads_kv]
