@@ -583,7 +583,9 @@ MSPARSE_API msparse_status msparse_tree_mask(int32_t batch, int32_t tokens, cons
  * the nodes' places count as the nearest of them).  A row behind the counts, or without a
  * key, gets out = 0 and lse = -inf.  All else as msparse_cache_attn: codes of tokens that no row
  * of the call sees (pruned nodes among them) may hold anything, and so may the scales of pages
- * that hold none but such. */
+ * that hold none but such.  A NaN among the values of a node that some row sees may reach every
+ * row of its sequence, those of other branches and of nodes before it too: a branch does not
+ * keep it to itself (a NaN key or query does stay with the rows that see it, or its own). */
 MSPARSE_API size_t msparse_cache_tree_attn_workspace(const msparse_cache* cache, int32_t heads_q, int32_t tokens);
 MSPARSE_API msparse_status msparse_cache_tree_attn(const msparse_cache* cache, int32_t heads_q, int32_t tokens,
                                                    int32_t window, int32_t sinks, float scale,

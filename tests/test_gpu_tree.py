@@ -327,6 +327,24 @@ def test_nan_outside_the_window_and_behind_the_nodes(gpu, d, T, W, S):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("d,T", [(64, 4), (128, 8), (64, 14), (128, 60)])
+def test_nan_keys_stay_with_the_rows_that_see_them(gpu, d, T):
+    Hq, Hkv, contexts = 8, 2, [300, 62]
+    at, sees = _masks(_parents(8, 2, T), contexts, None, 0, 0)
+    cache, table, L = _filled(15, contexts, T, Hkv, d, gpu, None)
+    q = _randn(3, (2, Hq, T, d), gpu)
+    seen = _dev(OT.words(sees), gpu)
+    want = ms.cache_tree_attn(cache, table, L, q, seen)
+    node = T // 2
+    for b, n in enumerate(contexts):
+        cache.k.view(torch.uint8)[int(table[b, (n + node) // 64]), :, (n + node) % 64, 3] = 0x7f
+    out, lse = ms.cache_tree_attn(cache, table, L, q, seen)
+    hit = torch.from_numpy(sees[:, :, node]).to(gpu)[:, None].expand(2, Hq, T)
+    assert hit.any() and not hit.all()
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], want[0][~hit]) and torch.equal(lse[~hit], want[1][~hit])
+
+
 def _unseen(sees, at, contexts, counts, W, S):
     """Of each sequence: which of its slots no node sees."""
     out = []
