@@ -6,6 +6,9 @@ import torch
 import paper_2510_18830_amd as ms
 from oracle import cache as OC
 from oracle import pages as OP
+from oracle import tree as OT
+from oracle import window as OW
+from tests.helpers import to_f64
 
 pytestmark = pytest.mark.gpu
 I32, BF = torch.int32, torch.bfloat16
@@ -408,3 +411,86 @@ def test_speculative_decoding_together(gpu, d, axes):
                 assert (np.abs(got - vv[h]) <= 2.0 ** -3 * np.abs(vv[h]) + 2.0 ** -9 * 2.0 ** -6).all(), (step, b, h)
     table, lens, refs, _ = ms.cache_fork(cache, table, lens, refs, torch.tensor([-1], dtype=I32, device=gpu))
     assert not refs.any() and (table == -1).all() and lens.tolist() == [0]
+
+
+def _attends(out, lse, q, want, lens):
+    """Within the bound of the attention's roundings (oracle/tree.py, oracle/cache.py)."""
+    ro, eo, rl = want
+    assert (np.abs(to_f64(out.contiguous().cpu()) - ro) <= eo).all()
+    gl = lse.double().cpu().numpy()
+    assert np.array_equal(np.isneginf(gl), np.isneginf(rl))
+    d, fine = q.shape[3], np.isfinite(rl)
+    reach = 8.0 * max(1.0, float(q.double().abs().max())) * np.sqrt(d)
+    assert np.abs(gl[fine] - rl[fine]).max() <= OW.lse_bound(int(lens.max()), d, reach)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,T,axes,W,S", [(4, 2, 64, 12, 1, 90, 4), (8, 2, 128, 70, 3, 0, 0), (4, 4, 64, 9, 2, 33, 0)])
+def test_every_step_of_speculative_decoding(gpu, Hq, Hkv, d, T, axes, W, S):
+    """The loop of all operators, each step's result against the oracle on what the cache held before it: forks, moves of
+    kept tokens and masks equal, attention within the bound of its roundings on the codes that the cache holds, and a token
+    appended behind the accepted ones attends to them as the oracle's does."""
+    print(f"every step Hq{Hq} Hkv{Hkv} d{d} T{T} axes{axes} W{W} S{S}", flush=True)
+    B, pages, width = 3, 90, 9
+    rng = np.random.default_rng(T)
+    g = torch.Generator().manual_seed(T)
+    rand = lambda *s: torch.randn(s, generator=g).to(BF).to(gpu)  # noqa: E731
+    freq = (10000.0 ** (-torch.arange(d // 2, dtype=torch.float64) * 2 / d)).float().to(gpu)
+    axis = (torch.arange(d // 2) % axes).to(I32).to(gpu)
+    many = lambda at: (at[None] * torch.arange(1, axes + 1, dtype=I32, device=gpu)[:, None, None]).contiguous()  # noqa: E731
+    cache = _pool(19, pages, Hkv, d, gpu)
+    table = torch.full((B, width), -1, dtype=I32, device=gpu)
+    lens, refs = torch.zeros(B, dtype=I32, device=gpu), torch.zeros(pages, dtype=I32, device=gpu)
+
+    def fork(src, room):
+        got = _fork(gpu, cache, table.cpu().numpy(), lens.tolist(), refs.cpu().numpy(), src, room)
+        assert not got[3].any()
+        return tuple(_dev(x, gpu) for x in got[:3])
+
+    prompt = [60, 64, 117]
+    table, lens, refs = fork([0, 1, 2], prompt)
+    at, counts = torch.arange(117, dtype=I32, device=gpu).expand(B, 117), _dev(np.array(prompt), gpu)
+    ms.cache_append(cache, table, lens, rand(B, Hkv, 117, d), rand(B, Hkv, 117, d), inv_freq=freq, counts=counts,
+                    positions=many(at), axis=axis)
+    lens = lens + counts
+    for step, src in enumerate(([0, 1, 2], [2, 0, 2], [0, 1, 2], [1, 1, 0])):
+        table, lens, refs = fork(src, [n + T + 1 for n in lens[list(src)].tolist()])
+        parents = (np.sqrt(rng.random((B, T))) * (np.arange(T) + 1)).astype(np.int64) - 1
+        nodes = rng.integers(1, T + 1, B)
+        q, k, v, cnt = rand(B, Hq, T, d), rand(B, Hkv, T, d), rand(B, Hkv, T, d), _dev(nodes, gpu)
+        gat, seen = ms.tree_mask(_dev(parents, gpu), lens, counts=cnt, window=W, sinks=S)
+        both = [OT.mask(parents[b], int(lens[b]), int(nodes[b]), W, S) for b in range(B)]
+        at, sees = np.stack([x[0] for x in both]), np.stack([x[1] for x in both])
+        assert np.array_equal(gat.cpu().numpy(), at) and np.array_equal(seen.cpu().numpy(), OT.words(sees))
+        qr = ms.cache_append(cache, table, lens, k, v, q=q, inv_freq=freq, counts=cnt, positions=many(gat), axis=axis)
+        total = lens + cnt
+        host, entries, n = _host(cache), table.cpu().numpy(), total.cpu().numpy()
+        # the nodes are there: V's values to half a step of e4m3, and below its normal range of the page's scale
+        for b in range(B):
+            for h in range(Hkv):
+                _, got, have = OC.gather(*host, entries[b][None], int(n[b]), 0, h)
+                x = to_f64(v[b:b + 1, h:h + 1, :nodes[b]].contiguous().cpu())[0, 0]
+                new = got[n[b] - nodes[b]:]
+                assert have.all() and (np.abs(new - x) <= 2.0 ** -4 * np.abs(x) + 2.0 ** -10 * host[3][:, h].max()).all()
+        out, lse = ms.cache_tree_attn(cache, table, total, qr, seen, positions=gat, counts=cnt, window=W, sinks=S)
+        torch.cuda.synchronize()
+        _attends(out, lse, qr, OT.attention(to_f64(qr.cpu()), *host, entries, n, sees, at, nodes, W, S, d ** -0.5), n)
+        path, kept = np.zeros((B, T), np.int64), []
+        for b in range(B):
+            line, u = [], int(rng.integers(0, nodes[b]))
+            while u >= 0:
+                line.append(u)
+                u = int(parents[b, u])
+            path[b, :len(line)] = line[::-1]
+            kept.append(len(line))
+        _keep(gpu, Hkv, d, T, n, [int(x) for x in nodes], path, kept, table=entries, cache=cache)
+        lens = lens + _dev(np.array(kept), gpu)
+        # the next token, behind the accepted ones
+        q1, k1, v1 = rand(B, Hq, 1, d), rand(B, Hkv, 1, d), rand(B, Hkv, 1, d)
+        qr = ms.cache_append(cache, table, lens, k1, v1, q=q1, inv_freq=freq, positions=many(lens[:, None]), axis=axis)
+        lens = lens + 1
+        out, lse = ms.cache_attn(cache, table, lens, qr, window=W, sinks=S)
+        torch.cuda.synchronize()
+        n = lens.cpu().numpy()
+        _attends(out, lse, qr, OC.attention(to_f64(qr.cpu()), *_host(cache), entries, n, W, S, d ** -0.5), n)
+    got = _fork(gpu, cache, table.cpu().numpy(), lens.tolist(), refs.cpu().numpy(), [-1], None)
+    assert not got[2].any() and (got[0] == -1).all()

@@ -9,6 +9,7 @@ import torch
 import paper_2510_18830_amd as ms
 from oracle import cache as OC
 from oracle import tree as OT
+from oracle import window as OW
 from tests.helpers import to_f64
 
 pytestmark = pytest.mark.gpu
@@ -172,6 +173,61 @@ def test_rotate_with_window_attention(gpu):
     p, f, a = pos.cpu().numpy(), freq.cpu().numpy(), axis.cpu().numpy()
     _check(dq, dqr, p, f, a, True)
     _check(dk, dkr, p, f, a, True)
+
+
+def _turn64(x, positions, freq, axis):
+    """x fp64 [H, N, d], differentiable; also |cos| and |sin| of the pairs."""
+    h = x.shape[2] // 2
+    ang = torch.from_numpy(positions[axis].T.astype(np.float64) * freq.astype(np.float64))   # [N, h]
+    c, s = ang.cos(), ang.sin()
+    return torch.cat([x[..., :h] * c - x[..., h:] * s, x[..., h:] * c + x[..., :h] * s], -1), c.abs().numpy(), s.abs().numpy()
+
+
+@pytest.mark.parametrize("Hq,Hkv,N,d,W,S,axes", [(4, 2, 90, 64, 30, 2, 2), (2, 2, 200, 128, 0, 0, 3), (7, 1, 333, 64, 100, 7, 1)])
+def test_a_layers_step_against_autograd(gpu, Hq, Hkv, N, d, W, S, axes):
+    """rotate, window attention, its backward, the gradients turned back: outputs and the gradients of the queries and keys
+    before the rotation against autograd in fp64 through all of it (the rotated tensors take the values that rotate rounded
+    to bf16, themselves checked).  Bounds: those of the attention (oracle/window.py), of two columns where they turn into
+    one, and the rotation's roundings."""
+    q, k, v, do = (_randn(i, (1, h, N, d), gpu) for i, h in enumerate((Hq, Hkv, Hkv, Hq)))
+    pos, freq = _positions(3, axes, 1, N, 2000, gpu), _freq(d, gpu)
+    axis = (torch.arange(d // 2) % axes).to(torch.int32).to(gpu)
+    qr, kr = ms.rotate(q, k, pos, freq, axis=axis)
+    win = ms.make_window(1, N, Hq, Hkv, d, W, S)
+    out, lse = ms.window_fwd(win, qr, kr, v)
+    dqr, dkr, dv = ms.window_bwd(win, qr, kr, v, out, do, lse)
+    dq, dk = ms.rotate(dqr, dkr, pos, freq, axis=axis, inverse=True)
+    torch.cuda.synchronize()
+    p, f, a = pos.cpu().numpy(), freq.cpu().numpy(), axis.cpu().numpy()
+    _check(qr, q, p, f, a, False)
+    _check(kr, k, p, f, a, False)
+    # autograd
+    leaf = [torch.from_numpy(_f64(t)[0]).requires_grad_() for t in (q, k, v)]
+    turned, rounded = [], [torch.from_numpy(_f64(t)[0]) for t in (qr, kr)]
+    for x, y in zip(leaf, rounded):
+        z, c, s = _turn64(x, p[:, 0], f, a)
+        turned.append(z + (y - z).detach())
+    G = Hq // Hkv
+    z = (turned[0].view(Hkv, G, N, d) @ turned[1].view(Hkv, 1, N, d).transpose(-1, -2)) * d ** -0.5
+    z = z.masked_fill(~torch.from_numpy(OW.mask(N, W, S)), -np.inf)
+    o = (torch.softmax(z, -1) @ leaf[2].view(Hkv, 1, N, d)).view(Hq, N, d)
+    (o * torch.from_numpy(_f64(do)[0])).sum().backward()
+    # bounds
+    host = [t.numpy() for t in rounded] + [_f64(v)[0], _f64(do)[0]]
+    _, eo, _, reach = OW.sequence_fwd(*host[:3], W, S, d ** -0.5)
+    (_, eq), (_, ek), (_, ev) = OW.sequence_bwd(*host, W, S, d ** -0.5)
+    assert (np.abs(_f64(out)[0] - o.detach().numpy()) <= eo).all()
+    want = torch.logsumexp(z.detach(), -1).view(Hq, N).numpy()
+    assert np.abs(lse[0].double().cpu().numpy() - want).max() <= OW.lse_bound(N, d, reach)
+    assert (np.abs(_f64(dv)[0] - leaf[2].grad.numpy()) <= ev).all()
+    h = d // 2
+    for got, before, x, e in ((dq, dqr, leaf[0], eq), (dk, dkr, leaf[1], ek)):
+        ref, g = x.grad.numpy(), np.abs(_f64(before)[0])
+        bound = np.concatenate([e[..., :h] * c + e[..., h:] * s, e[..., h:] * c + e[..., :h] * s], -1)
+        bound += 2.0 ** -22 * np.concatenate([g[..., :h] + g[..., h:]] * 2, -1)
+        bound += 2.0 ** -8 * (np.abs(ref) + bound)
+        err = np.abs(_f64(got)[0] - ref)
+        assert (err <= bound).all(), (err.max(), (err > bound).sum())
 
 
 def test_rotate_of_many_tokens(gpu):
