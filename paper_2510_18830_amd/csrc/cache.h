@@ -73,7 +73,7 @@ inline void share_heads(AppendArgs& a, int64_t pages) {
     a.kv_shares = even_shares(hkv, std::min(hkv, std::max({int64_t(4), hkv / 4, 600 / pages})));
     a.q_shares = a.q ? even_shares(steps, std::min(steps, std::max((steps + 5) / 6, 512 / pages - a.kv_shares))) : 0;
     // With positions given, angles cost more than a share of the heads saves where the card is full anyway (us: 2 x
-    // 20011 tokens, 28 over 4 heads 157 -> 139; 131072, 32 over 8 652 -> 568; 16 x 500, 28 over 4 41.7 -> 38.2; 64 x 64
+    // 20011 tokens, 28 over 4 heads 157 -> 138; 131072, 32 over 8 652 -> 568; 16 x 500, 28 over 4 41.7 -> 38.2; 64 x 64
     // 27.2 -> 26.7; but 40 x 64, 12 over 4 of 64 columns 11.2 -> 12.8, 64 x 16, 28 over 4 12.6 -> 14.7).
     if (a.pos.at && int64_t(a.c.B) * a.T >= 4096) {
         a.kv_shares = even_shares(hkv, std::min(hkv, std::max(int64_t(2), hkv / 8)));

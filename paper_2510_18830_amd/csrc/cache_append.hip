@@ -31,7 +31,7 @@ struct Split {
 };
 
 // AT: the tokens' positions are given, so that every angle is formed by itself (2 x 20011 tokens, 28 over 4 heads of
-// 128: 134 us, 115 where it follows from the one before).
+// 128: 138 us, 114 where it follows from the one before).
 template <int D, bool AT>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, D == 128 ? 3 : 4)))
 cache_append_kernel(AppendArgs a) {
