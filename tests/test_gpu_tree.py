@@ -364,6 +364,9 @@ def _unseen(sees, at, contexts, counts, W, S):
     (8, 2, 64, 45, [130, 500], None, 60, 2, True), (8, 2, 128, 45, [130, 500], [45, 40], 0, 0, False),
     (2, 2, 64, 200, [70, 500], [200, 190], 0, 0, False), (2, 2, 128, 200, [640, 30], None, 100, 70, True),
     (1, 1, 64, 1024, [30], None, 0, 0, False), (16, 2, 128, 130, [300], None, 140, 0, True),
+    (4, 1, 64, 4, [1500, 700], None, 600, 70, True), (8, 2, 128, 40, [5000, 700], None, 0, 0, False),
+    (8, 1, 64, 64, [20] * 77 + [4500] + [33] * 52, None, 0, 0, False),
+    (8, 1, 128, 64, [4200] + [70] * 129, None, 4100, 0, True),
 ])
 def test_tokens_that_no_node_sees_may_hold_anything(gpu, Hq, Hkv, d, T, contexts, counts, W, S, late):
     """Pruned nodes, and the context between what the window reaches from the first place and from the first position given:
