@@ -122,13 +122,14 @@ __device__ __forceinline__ void dma_rows(uint16_t* tile, const uint16_t* __restr
                                          int lane) {
     using T = DmaTile<D, P>;
     constexpr int NC = D / 8;
+    const uint32_t to = lds_addr(tile);
 #pragma unroll
     for (int j = 0; j < (T::kGroups + NW - 1) / NW; ++j) {
         const int g = wave + NW * j;
         if (T::kGroups % NW != 0 && g >= T::kGroups) break;
         const int r = g + T::kGroups * (lane / NC);
         const int c = lane % NC;
-        dma16(src + rows(r) * D + c * 8, lds_addr(tile + T::goff(g) / 2));
+        dma16(src + rows(r) * D + c * 8, to + T::goff(g));
     }
 }
 

@@ -268,11 +268,12 @@ __device__ __forceinline__ void dma_sequence(uint16_t* tile, const uint16_t* src
     using T = DmaTile<D, P>;
     constexpr int NC = D / 8;
     static_assert(T::kGroups % NW == 0, "whole instructions per wave");
+    const uint32_t to = lds_addr(tile);
 #pragma unroll
     for (int j = 0; j < T::kGroups / NW; ++j) {
         const int g = wave + NW * j;
         const int r = min(row0 + g + T::kGroups * (lane / NC), last);
-        dma16(src + r * stride + (lane % NC) * 8, lds_addr(tile + T::goff(g) / 2));
+        dma16(src + r * stride + (lane % NC) * 8, to + T::goff(g));
     }
 }
 
